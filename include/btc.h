@@ -59,12 +59,17 @@ enum {
     BTC_ERR_SCRATCH_LIMIT = 13       /* needs more than the built-in scratch array holds        */
 };
 
-/* Element types.  Complex values are (re, im) pairs of the stated part width. */
+/* Element types.  Complex values are (re, im) pairs of the stated part width.  The 16-bit types and the
+ * 32-bit integers serve the decoder operators only: contractions and elementwise operations answer
+ * NOT_SUPPORTED to a descriptor that carries one. */
 typedef enum {
     BTC_F32 = 0,
     BTC_F64 = 1,
     BTC_C32 = 2, /* 2 x float  (8 bytes)  */
-    BTC_C64 = 3  /* 2 x double (16 bytes) */
+    BTC_C64 = 3, /* 2 x double (16 bytes) */
+    BTC_F16 = 4, /* IEEE half             */
+    BTC_BF16 = 5,
+    BTC_I32 = 6
 } btc_dtype_t;
 
 typedef struct btc_handle_s *btc_handle_t;            /* Sec. "The Library Handle"            */
@@ -317,6 +322,69 @@ enum {
                                   label, chosen at execute time when strides and pointers allow  */
 };
 btc_error_t btc_elementwise_get_attr(btc_elementwise_t op, int32_t key, void *value, size_t len, size_t *needed);
+
+/* ---- Decoder operators (no counterpart in the paper) --------------------------------------------
+ *
+ * What stands between the contractions of a transformer decoder layer: the norm and rotation of each
+ * query and key head, the paged key-value cache, and the attention over it.  They follow the rules of
+ * the operations above: descriptors without data pointers (strides in elements, signed), validation and
+ * planning at creation, execute calls that take device pointers and a stream, allocate nothing and do
+ * not wait for the device (so they can be captured into a graph), workspaces supplied by the caller
+ * (256-byte aligned; contents need no initialisation; calls that may overlap in time need one each).
+ * Sums are kept in fp32 or wider and results rounded once to their type.
+ *
+ * `flags` arguments are NULL or a DEVICE int32 into which a call ORs what it found wrong in data that
+ * only the device can see; the offending entries are skipped, no access leaves its tensor.  The word is
+ * sticky: the caller clears it. */
+enum {
+    BTC_FLAG_BAD_PAGE = 1,      /* a page number outside the pool                                    */
+    BTC_FLAG_BAD_SLOT = 2,      /* a slot outside the pool (a negative slot only means: skip)        */
+    BTC_FLAG_BAD_SEQUENCE = 4,  /* a sequence number outside the table                               */
+    BTC_FLAG_BAD_LENGTH = 8,    /* a length or token count that is negative or beyond the table row  */
+    BTC_FLAG_POOL_EXHAUSTED = 16 /* fewer free pages than asked for                                  */
+};
+
+/* Head norm and rotary positions of queries and keys, keys and values written into cache pages in the
+ * same pass.  For every token t and head h, with x the head's D values:
+ *     n = x / sqrt(mean(x^2) + eps)    (norm != 0; otherwise n = x)
+ *     m = n * W                        (W: D values shared by the heads; NULL = ones)
+ *     (y_a, y_b) = multiplier * (m_a cos - m_b sin, m_b cos + m_a sin),  angle = positions[t] * frequencies[i]
+ * for the pairs i = 0..pairs-1, (a, b) = (i, i + pairs) in the HALF layout and (2i, 2i + 1) in the
+ * INTERLEAVED one; values from 2 * pairs on are not rotated (y = m).  The frequencies (radians per
+ * position, any values: each long-context scaling is a choice of them and of the multiplier) are a host
+ * array that is copied.  The angle is reduced exactly, in fixed point: no position is too long.
+ *   Xq [T, Hq, D] -> Yq [T, Hq, D]     required
+ *   Xk [T, Hk, D] -> Yk                both or neither (NULL)
+ *   Xv [T, Hv, Dv] -> Yv               both or neither; copied unchanged
+ * Yk and Yv have their input's extents, or are cache pages [P, S, H, D] (P pages of S tokens): token t
+ * then goes to page slots[t] / S, row slots[t] % S, and a negative slot drops the token's key and value
+ * (two tokens of one call with the same slot: either may stay).  One element type (F32, F16, BF16) for
+ * all; W has it too.  D and Dv up to 256.  Y may be the same memory as X with the same strides.
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING (elements of an output alias), NOT_SUPPORTED
+ * (type, head size, P * S beyond int32), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA.
+ *
+ * btc_rotary_execute: positions and slots are DEVICE int32 arrays of T entries (positions may be NULL
+ * when pairs == 0, slots when nothing is paged).
+ * btc_rotary_backward: from dY (laid out like Y) and X the gradients dX (laid out like X) and dW (D
+ * fp32 values, overwritten; NULL = not wanted) of sum(dY * Y).  Without a norm X is not read (NULL
+ * allowed) and there is no dW.  For operations without Xv and pages (NOT_SUPPORTED otherwise), whose X
+ * has no aliasing elements (D_ALIASING).  dX may be the same memory as dY with the same strides.  The
+ * result does not depend on scheduling: same inputs, same bits. */
+typedef struct btc_rotary_s *btc_rotary_t;
+enum { BTC_ROTARY_HALF = 0, BTC_ROTARY_INTERLEAVED = 1 };
+btc_error_t btc_create_rotary(btc_handle_t handle, int32_t layout, int32_t pairs, const double *frequencies,
+                              double multiplier, int32_t norm, double eps,
+                              btc_tensor_info_t Xq, btc_tensor_info_t Yq, btc_tensor_info_t Xk, btc_tensor_info_t Yk,
+                              btc_tensor_info_t Xv, btc_tensor_info_t Yv, btc_rotary_t *out);
+btc_error_t btc_destroy_rotary(btc_rotary_t *op);
+btc_error_t btc_rotary_workspace_size(btc_rotary_t op, size_t *bytes);   /* of btc_rotary_backward */
+btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t *positions, const int32_t *slots,
+                               const void *Wq, const void *Wk, const void *Xq, void *Yq, const void *Xk, void *Yk,
+                               const void *Xv, void *Yv, int32_t *flags);
+btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_t *positions, const void *Wq,
+                                const void *Wk, const void *Xq, const void *dYq, void *dXq, const void *Xk,
+                                const void *dYk, void *dXk, float *dWq, float *dWk, void *workspace,
+                                size_t workspace_bytes);
 
 /* Peak micro-benchmarks (no counterpart in the paper; the paper leaves benchmarks to future work, Sec.
  * "Outlook").  Measures what this device sustains with a kernel that does nothing else, so that the

@@ -35,7 +35,10 @@ ERR_OUT_OF_MEMORY = 12
 ERR_SCRATCH_LIMIT = 13
 
 F32, F64, C32, C64 = 0, 1, 2, 3
-DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16}
+F16, BF16, I32 = 4, 5, 6          # decoder operators only
+DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16, F16: 2, BF16: 2, I32: 4}
+FLAG_BAD_PAGE, FLAG_BAD_SLOT, FLAG_BAD_SEQUENCE, FLAG_BAD_LENGTH, FLAG_POOL_EXHAUSTED = 1, 2, 4, 8, 16
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 
 ATTR_KERNEL, ATTR_SPLIT_K, ATTR_TILE, ATTR_GROUPS, ATTR_GRID, ATTR_NUM_MODES, ATTR_SWAPPED = 1, 2, 3, 4, 5, 6, 7
 ATTR_DEVICE_ERROR = 8
@@ -56,6 +59,7 @@ EXPORTED = [
     "btc_status_get",
     "btc_destroy_status", "btc_explain_error", "btc_selftest_bounded_wait", "btc_measure_peak",
     "btc_create_elementwise", "btc_destroy_elementwise", "btc_elementwise_execute", "btc_elementwise_get_attr",
+    "btc_create_rotary", "btc_destroy_rotary", "btc_rotary_workspace_size", "btc_rotary_execute", "btc_rotary_backward",
 ]
 
 _vp = ctypes.c_void_p
@@ -88,6 +92,12 @@ _lib.btc_elementwise_get_attr.argtypes = [_vp, ctypes.c_int32, _vp, ctypes.c_siz
 _lib.btc_selftest_bounded_wait.argtypes = [_vp, _vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32),
                                            ctypes.POINTER(ctypes.c_int32)]
 _lib.btc_measure_peak.argtypes = [_vp, ctypes.c_int32, _vp, _vp, ctypes.c_size_t, ctypes.c_int32, ctypes.POINTER(ctypes.c_double)]
+_lib.btc_create_rotary.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_double), ctypes.c_double,
+                                   ctypes.c_int32, ctypes.c_double] + [_vp] * 6 + [ctypes.POINTER(_vp)]
+_lib.btc_destroy_rotary.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_rotary_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_rotary_execute.argtypes = [_vp] * 13
+_lib.btc_rotary_backward.argtypes = [_vp] * 14 + [ctypes.c_size_t]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -330,7 +340,8 @@ def dtype_code(torch_dtype) -> int:
     global _TORCH_DTYPE
     if _TORCH_DTYPE is None:
         import torch
-        _TORCH_DTYPE = {torch.float32: F32, torch.float64: F64, torch.complex64: C32, torch.complex128: C64}
+        _TORCH_DTYPE = {torch.float32: F32, torch.float64: F64, torch.complex64: C32, torch.complex128: C64,
+                        torch.float16: F16, torch.bfloat16: BF16, torch.int32: I32}
     return _TORCH_DTYPE[torch_dtype]
 
 
@@ -383,6 +394,101 @@ class Elementwise:
             self.close()
         except Exception:
             pass
+
+
+class _Operation:
+    """Common part of the decoder operators: the C object, its workspace size, its end."""
+
+    _kind = ""
+
+    def _size(self) -> int:
+        n = ctypes.c_size_t(0)
+        _check(getattr(_lib, f"btc_{self._kind}_workspace_size")(self._op, ctypes.byref(n)), f"btc_{self._kind}_workspace_size")
+        return n.value
+
+    def workspace_size(self) -> int:
+        return self._size()
+
+    def close(self):
+        if self._op:
+            getattr(_lib, f"btc_destroy_{self._kind}")(ctypes.byref(self._op))
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _info_or_null(info: Optional[TensorInfo]):
+    return info._t if info is not None else None
+
+
+class Rotary(_Operation):
+    """Head norm and rotary positions of queries (and keys), values passed through; see btc_create_rotary.
+
+    Yk and Yv of rank 4 are cache pages [pages, tokens per page, heads, head size]; execute then takes the
+    tokens' slots.  All data arguments are device pointers as integers (0 or None: absent)."""
+
+    _kind = "rotary"
+
+    def __init__(self, handle: Handle, frequencies: Sequence[float], Xq: TensorInfo, Yq: TensorInfo,
+                 Xk: Optional[TensorInfo] = None, Yk: Optional[TensorInfo] = None, Xv: Optional[TensorInfo] = None,
+                 Yv: Optional[TensorInfo] = None, interleaved: bool = False, norm: bool = False, eps: float = 1e-6,
+                 multiplier: float = 1.0):
+        self._op = _vp()
+        freq = [float(f) for f in frequencies]
+        _check(_lib.btc_create_rotary(
+            handle._h, ROTARY_INTERLEAVED if interleaved else ROTARY_HALF, len(freq),
+            (ctypes.c_double * max(len(freq), 1))(*freq), multiplier, int(norm), eps, Xq._t, Yq._t, _info_or_null(Xk),
+            _info_or_null(Yk), _info_or_null(Xv), _info_or_null(Yv), ctypes.byref(self._op)), "btc_create_rotary")
+
+    def execute(self, stream: int, positions: int, Wq: int, Wk: int, Xq: int, Yq: int, Xk: int = 0, Yk: int = 0,
+                Xv: int = 0, Yv: int = 0, slots: int = 0, flags: int = 0) -> None:
+        rc = _lib.btc_rotary_execute(self._op, stream, positions, slots, Wq, Wk, Xq, Yq, Xk, Yk, Xv, Yv, flags)
+        if rc:
+            raise BtcError(rc, "btc_rotary_execute")
+
+    def backward(self, stream: int, positions: int, Wq: int, Wk: int, Xq: int, dYq: int, dXq: int, Xk: int = 0,
+                 dYk: int = 0, dXk: int = 0, dWq: int = 0, dWk: int = 0, workspace: int = 0, workspace_bytes: int = 0) -> None:
+        rc = _lib.btc_rotary_backward(self._op, stream, positions, Wq, Wk, Xq, dYq, dXq, Xk, dYk, dXk, dWq, dWk,
+                                      workspace, workspace_bytes)
+        if rc:
+            raise BtcError(rc, "btc_rotary_backward")
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       original_length: int = 8192, slow: float = 1.0, fast: float = 32.0):
+    """(radians per position of each of the rotary_dim / 2 pairs, multiplier of the rotated values).
+
+    scaling stretches a context of `original_length` positions `factor` times:
+      None      frequencies base^(-2 i / rotary_dim)
+      "linear"  every frequency divided by factor
+      "base"    the base raised so that the slowest pair is stretched by factor and the fastest not at all
+      "bands"   pairs that turn at least `fast` times within the original context keep their frequency, pairs
+                that turn at most `slow` times are divided by factor, a linear ramp between; the rotated
+                values are multiplied by 0.1 ln(factor) + 1 (sharper attention over a longer context)"""
+    import math
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim is a positive even number")
+    if factor < 1.0:
+        raise ValueError("factor is at least 1")
+    half = rotary_dim // 2
+    if scaling == "base" and half > 1:
+        base = base * factor ** (rotary_dim / (rotary_dim - 2.0))
+    freq = [base ** (-2.0 * i / rotary_dim) for i in range(half)]
+    if scaling in (None, "base"):
+        return freq, 1.0
+    if scaling == "linear":
+        return [f / factor for f in freq], 1.0
+    if scaling == "bands":
+        out = []
+        for f in freq:
+            turns = original_length * f / (2.0 * math.pi)
+            keep = min(1.0, max(0.0, (turns - slow) / (fast - slow)))
+            out.append(f * keep + f / factor * (1.0 - keep))
+        return out, (0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0)
+    raise ValueError(f"unknown scaling {scaling!r}")
 
 
 def elementwise(handle: Handle, A, labelsA, B, C, labelsC, alpha=1.0, beta=0.0, conjA=False, conjB=False, stream: int = 0):

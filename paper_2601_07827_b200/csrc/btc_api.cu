@@ -16,6 +16,7 @@
 #include "generic_kernel.cuh"
 #include "kernel_params.h"
 #include "launchers.h"
+#include "objects.h"
 #include "skinny_layout.h"
 #include "plan.h"
 #include "tiled_f32_kernel.cuh"
@@ -28,15 +29,6 @@
 
 using namespace btc;
 
-
-struct btc_handle_s {
-    int device = -1;       // -1: no CUDA device (objects can be validated and planned, not run)
-    int sm_count = 148;
-};
-
-struct btc_tensor_info_s {
-    TensorDesc desc;
-};
 
 struct btc_status_s {
     int32_t kernel = 0, launches = 0, split_k = 1, variant = -1;
@@ -946,7 +938,7 @@ btc_error_t btc_create_tensor_info(btc_handle_t handle, btc_dtype_t dtype, int32
 {
     if (!handle || !out) return BTC_ERR_INVALID_ARGUMENT;
     if (rank < 0 || rank > BTC_MAX_RANK) return BTC_ERR_INVALID_ARGUMENT;
-    if (int(dtype) < 0 || int(dtype) > int(BTC_C64)) return BTC_ERR_INVALID_ARGUMENT;
+    if (int(dtype) < 0 || int(dtype) > int(BTC_I32)) return BTC_ERR_INVALID_ARGUMENT;
     if (rank > 0 && !extents) return BTC_ERR_INVALID_ARGUMENT;
     for (int i = 0; i < rank; ++i)
         if (extents[i] < 1) return BTC_ERR_INVALID_EXTENT;
@@ -984,6 +976,8 @@ btc_error_t btc_create_contraction(btc_handle_t handle, btc_tensor_info_t A, con
     if ((!labelsA && !A->desc.extent.empty()) || (!labelsB && !B->desc.extent.empty()) ||
         (!labelsD && !D->desc.extent.empty()) || (C && !labelsC && !C->desc.extent.empty()))
         return BTC_ERR_INVALID_ARGUMENT;
+    for (btc_tensor_info_t t : {A, B, C, D})
+        if (t && !dtype_is_contractible(t->desc.dtype)) return BTC_ERR_NOT_SUPPORTED;
     btc_contraction_s *op = new (std::nothrow) btc_contraction_s;
     if (!op) return BTC_ERR_OUT_OF_MEMORY;
     op->handle = *handle;
@@ -1856,6 +1850,8 @@ btc_error_t btc_create_elementwise(btc_handle_t handle, btc_tensor_info_t A, con
 {
     if (!handle || !A || !C || !out) return BTC_ERR_INVALID_ARGUMENT;
     if ((!labelsA && !A->desc.extent.empty()) || (!labelsC && !C->desc.extent.empty())) return BTC_ERR_INVALID_ARGUMENT;
+    for (btc_tensor_info_t t : {A, B, C})
+        if (t && !dtype_is_contractible(t->desc.dtype)) return BTC_ERR_NOT_SUPPORTED;
     btc_elementwise_s *op = new (std::nothrow) btc_elementwise_s;
     if (!op) return BTC_ERR_OUT_OF_MEMORY;
     op->handle = *handle;

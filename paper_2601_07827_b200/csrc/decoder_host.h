@@ -1,0 +1,45 @@
+// Host-side helpers of the decoder operators: argument checks shared by their C entry points.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+#include <exception>
+#include <new>
+
+#include "objects.h"
+
+namespace btc {
+
+inline bool decoder_type(btc_dtype_t t) { return t == BTC_F32 || t == BTC_F16 || t == BTC_BF16; }
+
+inline bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// |stride| * (extent - 1) summed stays far inside int64: the kernels form offsets without overflow tests
+inline bool spans_fit(const TensorDesc &t)
+{
+    const __int128 limit = __int128(1) << 60;
+    __int128 span = 0;
+    for (size_t i = 0; i < t.extent.size(); ++i) {
+        const __int128 s = t.stride[i] < 0 ? -__int128(t.stride[i]) : __int128(t.stride[i]);
+        span += s * (t.extent[i] - 1);
+        if (span > limit || s > limit) return false;
+    }
+    return true;
+}
+
+// Runs the body of a C entry point; nothing thrown inside (only allocation can throw) leaves it.
+template <typename F> btc_error_t guarded(F &&body)
+{
+    try {
+        return body();
+    } catch (const std::bad_alloc &) {
+        return BTC_ERR_OUT_OF_MEMORY;
+    } catch (const std::exception &) {
+        return BTC_ERR_INVALID_ARGUMENT;
+    }
+}
+
+inline btc_error_t launch_result() { return cudaGetLastError() == cudaSuccess ? BTC_SUCCESS : BTC_ERR_CUDA; }
+
+}  // namespace btc

@@ -14,28 +14,17 @@ size_t dtype_size(btc_dtype_t t)
     case BTC_F64: return 8;
     case BTC_C32: return 8;
     case BTC_C64: return 16;
+    case BTC_F16: return 2;
+    case BTC_BF16: return 2;
+    case BTC_I32: return 4;
     }
     return 0;
 }
 
 bool dtype_is_complex(btc_dtype_t t) { return t == BTC_C32 || t == BTC_C64; }
+bool dtype_is_contractible(btc_dtype_t t) { return t == BTC_F32 || t == BTC_F64 || dtype_is_complex(t); }
 
-namespace {
-
-inline int64_t iabs(int64_t x) { return x < 0 ? -x : x; }
-
-struct LabelRow {
-    int64_t label = 0, extent = 0;
-    int64_t sA = 0, sB = 0, sD = 0;
-    bool inA = false, inB = false, inD = false;
-};
-
-int find_label(const std::vector<LabelRow> &rows, int64_t label)
-{
-    for (size_t i = 0; i < rows.size(); ++i)
-        if (rows[i].label == label) return int(i);
-    return -1;
-}
+static inline int64_t iabs(int64_t x) { return x < 0 ? -x : x; }
 
 // Sufficient test that no two index tuples of D address the same element: with the modes of
 // extent > 1 sorted by |stride|, every stride must exceed the span of all smaller ones.
@@ -54,6 +43,21 @@ bool d_may_alias(const TensorDesc &D)
         span += p.first * (p.second - 1);
     }
     return false;
+}
+
+namespace {
+
+struct LabelRow {
+    int64_t label = 0, extent = 0;
+    int64_t sA = 0, sB = 0, sD = 0;
+    bool inA = false, inB = false, inD = false;
+};
+
+int find_label(const std::vector<LabelRow> &rows, int64_t label)
+{
+    for (size_t i = 0; i < rows.size(); ++i)
+        if (rows[i].label == label) return int(i);
+    return -1;
 }
 
 // Merge loop dimensions whose strides chain in every tensor: y follows x when

@@ -149,6 +149,10 @@ int make_elementwise_plan(const ElementwiseRequest &req, ElementwisePlan &plan);
 
 size_t dtype_size(btc_dtype_t t);
 bool dtype_is_complex(btc_dtype_t t);
+bool dtype_is_contractible(btc_dtype_t t);   // what contractions and elementwise operations accept
+
+// Sufficient test that no two index tuples address the same element (false: surely none do).
+bool d_may_alias(const TensorDesc &D);
 
 // Largest total number of table entries the tiled kernels accept before the planner falls back
 // to the generic kernel.

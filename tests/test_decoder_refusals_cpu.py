@@ -1,0 +1,101 @@
+"""What the decoder operators refuse, and their host-side helpers: no GPU needed."""
+import math
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2601_07827_b200 import build
+    build.build()
+    from paper_2601_07827_b200 import api as _api
+    return _api
+
+
+@pytest.fixture(scope="module")
+def handle(api):
+    return api.Handle()
+
+
+def code(api, fn):
+    with pytest.raises(api.BtcError) as e:
+        fn()
+    return e.value.code
+
+
+def dense(api, h, dtype, *shape, strides=None):
+    if strides is None:
+        strides, s = [], 1
+        for x in reversed(shape):
+            strides.insert(0, s)
+            s *= x
+    return api.TensorInfo(h, dtype, shape, strides)
+
+
+def test_decoder_types_are_refused_by_contractions(api, handle):
+    for dt in (api.F16, api.BF16, api.I32):
+        a = dense(api, handle, dt, 4, 4)
+        assert code(api, lambda: api.Contraction(handle, a, "ik", a, "kj", None, None, a, "ij", alpha=None)) == api.ERR_NOT_SUPPORTED
+        assert code(api, lambda: api.Elementwise(handle, a, "ij", None, a, "ji", alpha=None, beta=None)) == api.ERR_NOT_SUPPORTED
+
+
+def test_rotary_refusals(api, handle):
+    E, B = api, api.BF16
+    t = lambda *s, dt=B, st=None: dense(api, handle, dt, *s, strides=st)  # noqa: E731
+    f = [0.1] * 4
+    make = lambda *a, **k: code(api, lambda: api.Rotary(handle, *a, **k))  # noqa: E731
+    assert make(f, t(4, 2, 8, dt=E.F64), t(4, 2, 8, dt=E.F64)) == E.ERR_NOT_SUPPORTED
+    assert make(f, t(4, 2, 8), t(4, 2, 8, dt=E.F16)) == E.ERR_NOT_SUPPORTED
+    assert make(f, t(4, 2, 8), t(4, 3, 8)) == E.ERR_EXTENT_MISMATCH
+    assert make(f, t(4, 2, 8), t(5, 2, 8)) == E.ERR_EXTENT_MISMATCH
+    assert make(f, t(4, 2, 6), t(4, 2, 6)) == E.ERR_INVALID_ARGUMENT            # more pairs than the head has
+    assert make(f, t(4, 2, 264), t(4, 2, 264)) == E.ERR_NOT_SUPPORTED
+    assert make(f, t(8, 8), t(8, 8)) == E.ERR_INVALID_ARGUMENT
+    assert make(f, t(2, 3, 2, 8), t(2, 3, 2, 8)) == E.ERR_INVALID_ARGUMENT
+    assert make(f, t(6, 2, 8), t(2, 3, 2, 8)) == E.ERR_INVALID_ARGUMENT         # queries go to no pages
+    assert make(f, t(4, 2, 8), t(4, 2, 8, st=(16, 0, 1))) == E.ERR_D_ALIASING
+    assert make(f, t(4, 2, 8), t(4, 2, 8), Xk=t(4, 1, 8)) == E.ERR_INVALID_ARGUMENT
+    assert make(f, t(4, 2, 8), t(4, 2, 8), Xk=t(4, 1, 16), Yk=t(4, 1, 16)) == E.ERR_EXTENT_MISMATCH
+    assert make(f, t(4, 2, 8), t(4, 2, 8), Xk=t(4, 1, 8), Yk=t(9, 16, 1, 8), Xv=t(4, 1, 8), Yv=t(9, 8, 1, 8)) == E.ERR_EXTENT_MISMATCH
+    assert make(f, t(4, 2, 8), t(4, 2, 8), Xk=t(4, 1, 8), Yk=t(1 << 28, 16, 1, 8)) == E.ERR_NOT_SUPPORTED
+    assert make(f, t(4, 2, 8, st=(1 << 62, 8, 1)), t(4, 2, 8)) == E.ERR_NOT_SUPPORTED
+    assert make([float("nan")], t(4, 2, 8), t(4, 2, 8)) == E.ERR_INVALID_ARGUMENT
+    assert make(f, t(4, 2, 8), t(4, 2, 8), multiplier=float("inf")) == E.ERR_INVALID_ARGUMENT
+    assert make(f, t(4, 2, 8), t(4, 2, 8), norm=True, eps=-1.0) == E.ERR_INVALID_ARGUMENT
+
+    op = api.Rotary(handle, f, t(4, 2, 8), t(4, 2, 8), t(4, 1, 8), t(9, 16, 1, 8))
+    run = lambda *a, **k: code(api, lambda: op.execute(0, *a, **k))  # noqa: E731
+    assert run(0, 0, 0, 256, 512, 256, 512, slots=256) == E.ERR_INVALID_ARGUMENT     # no positions
+    assert run(256, 0, 0, 256, 512, 256, 512) == E.ERR_INVALID_ARGUMENT              # no slots
+    assert run(256, 0, 0, 256, 512, 0, 0, slots=256) == E.ERR_INVALID_ARGUMENT       # no keys
+    assert run(256, 256, 0, 256, 512, 256, 512, slots=256) == E.ERR_INVALID_ARGUMENT  # a weight without a norm
+    assert run(256, 0, 0, 257, 512, 256, 512, slots=256) == E.ERR_MISALIGNED
+    assert run(258, 0, 0, 256, 512, 256, 512, slots=256) == E.ERR_MISALIGNED
+    assert code(api, lambda: op.backward(0, 256, 0, 0, 256, 256, 256, 256, 256, 256)) == E.ERR_NOT_SUPPORTED   # paged
+
+    op = api.Rotary(handle, f, t(4, 2, 8), t(4, 2, 8), norm=True)
+    back = lambda *a, **k: code(api, lambda: op.backward(0, *a, **k))  # noqa: E731
+    assert op.workspace_size() > 0
+    assert back(256, 0, 0, 0, 256, 256) == E.ERR_INVALID_ARGUMENT                    # a norm needs X
+    assert back(256, 0, 0, 256, 256, 256, dWq=256) == E.ERR_WORKSPACE_TOO_SMALL
+    assert back(256, 0, 0, 256, 256, 256, dWq=256, workspace=128, workspace_bytes=1 << 30) == E.ERR_MISALIGNED
+    assert back(256, 0, 0, 256, 256, 256, dWq=258, workspace=256, workspace_bytes=1 << 30) == E.ERR_MISALIGNED
+    plain = api.Rotary(handle, f, t(4, 2, 8), t(4, 2, 8))
+    assert plain.workspace_size() == 0
+    assert code(api, lambda: plain.backward(0, 256, 0, 0, 0, 256, 256, dWq=256)) == E.ERR_INVALID_ARGUMENT
+
+
+def test_rotary_frequencies(api):
+    f, m = api.rotary_frequencies(8)
+    assert m == 1.0 and f == [10000.0 ** (-i / 4) for i in range(4)]
+    g, m = api.rotary_frequencies(8, scaling="linear", factor=4.0)
+    assert m == 1.0 and all(math.isclose(a, b / 4) for a, b in zip(g, f))
+    g, m = api.rotary_frequencies(8, scaling="base", factor=4.0)
+    assert m == 1.0 and g[0] == f[0] and math.isclose(g[-1], f[-1] / 4)
+    g, m = api.rotary_frequencies(64, scaling="bands", factor=8.0, original_length=4096)
+    f, _ = api.rotary_frequencies(64)
+    assert g[0] == f[0] and math.isclose(g[-1], f[-1] / 8) and math.isclose(m, 0.1 * math.log(8) + 1)
+    assert all(a / 8 * (1 - 1e-12) <= b <= a for a, b in zip(f, g))
+    for bad in (dict(rotary_dim=7), dict(rotary_dim=8, factor=0.5), dict(rotary_dim=8, scaling="other")):
+        with pytest.raises(ValueError):
+            api.rotary_frequencies(**bad)

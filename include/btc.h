@@ -386,6 +386,32 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
                                 const void *dYk, void *dXk, float *dWq, float *dWk, void *workspace,
                                 size_t workspace_bytes);
 
+/* Attention of one new token per sequence over a paged key-value cache.  For every sequence n and query
+ * head h (sharing key head h / (Hq / Hk) with its neighbours), with j running over the visible tokens:
+ *     O[n,h] = sum_j p_j V_j,  p = softmax_j(scale * Q[n,h] . K_j),  lse[n,h] = log sum_j exp(scale * Q[n,h] . K_j)
+ * Token j of sequence n lies in page table[n, j / S], row j % S.  Visible are the last min(lengths[n], window)
+ * tokens below lengths[n] (window == 0: all).  A sequence that sees nothing (length 0) gets O = 0 and
+ * lse = -inf, as does one whose scores are all -inf.  What lies in pages beyond the visible tokens (NaN
+ * included) has no influence.  Tokens whose table entry is no page of the pool are not visible
+ * (BTC_FLAG_BAD_PAGE); lengths below zero count as zero, lengths beyond the table row as the row's
+ * capacity (BTC_FLAG_BAD_LENGTH).
+ *   Q [N, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
+ *   D and Dv up to 256; table [N, M] I32.  lengths: DEVICE int32[N]; lse: DEVICE float[N * Hq] or NULL.
+ * fp32 products are formed from three TF32 tensor-core products (as in contractions); 16-bit operations round
+ * once, at the output.  Infinite keys give infinite scores; an infinite visible value gives infinities or NaN.  The
+ * result does not depend on scheduling.  Lengths are read on the device only: one
+ * captured graph serves all steps of a growing cache.
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA. */
+typedef struct btc_paged_attention_s *btc_paged_attention_t;
+btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q, btc_tensor_info_t K,
+                                       btc_tensor_info_t V, btc_tensor_info_t table, btc_tensor_info_t O, double scale,
+                                       int32_t window, btc_paged_attention_t *out);
+btc_error_t btc_destroy_paged_attention(btc_paged_attention_t *op);
+btc_error_t btc_paged_attention_workspace_size(btc_paged_attention_t op, size_t *bytes);
+btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_stream, const void *Q, const void *K,
+                                        const void *V, const int32_t *table, const int32_t *lengths, void *O, float *lse,
+                                        void *workspace, size_t workspace_bytes, int32_t *flags);
+
 /* Peak micro-benchmarks (no counterpart in the paper; the paper leaves benchmarks to future work, Sec.
  * "Outlook").  Measures what this device sustains with a kernel that does nothing else, so that the
  * roofline fraction of a contraction can be quoted against a figure taken on the same device in the

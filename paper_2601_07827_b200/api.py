@@ -60,6 +60,8 @@ EXPORTED = [
     "btc_destroy_status", "btc_explain_error", "btc_selftest_bounded_wait", "btc_measure_peak",
     "btc_create_elementwise", "btc_destroy_elementwise", "btc_elementwise_execute", "btc_elementwise_get_attr",
     "btc_create_rotary", "btc_destroy_rotary", "btc_rotary_workspace_size", "btc_rotary_execute", "btc_rotary_backward",
+    "btc_create_paged_attention", "btc_destroy_paged_attention", "btc_paged_attention_workspace_size",
+    "btc_paged_attention_execute",
 ]
 
 _vp = ctypes.c_void_p
@@ -98,6 +100,10 @@ _lib.btc_destroy_rotary.argtypes = [ctypes.POINTER(_vp)]
 _lib.btc_rotary_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.btc_rotary_execute.argtypes = [_vp] * 13
 _lib.btc_rotary_backward.argtypes = [_vp] * 14 + [ctypes.c_size_t]
+_lib.btc_create_paged_attention.argtypes = [_vp] * 6 + [ctypes.c_double, ctypes.c_int32, ctypes.POINTER(_vp)]
+_lib.btc_destroy_paged_attention.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_paged_attention_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_paged_attention_execute.argtypes = [_vp] * 10 + [ctypes.c_size_t, _vp]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -489,6 +495,31 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: Optional
             out.append(f * keep + f / factor * (1.0 - keep))
         return out, (0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0)
     raise ValueError(f"unknown scaling {scaling!r}")
+
+
+class PagedAttention(_Operation):
+    """Attention of one new token per sequence over a paged cache; see btc_create_paged_attention.
+
+    Q [N, Hq, D], K [pages, tokens per page, Hk, D], V [pages, tokens per page, Hk, Dv], table [N, M] int32,
+    O [N, Hq, Dv].  scale: 1 / sqrt(D) when not given; window: last tokens that are visible (0: all)."""
+
+    _kind = "paged_attention"
+
+    def __init__(self, handle: Handle, Q: TensorInfo, K: TensorInfo, V: TensorInfo, table: TensorInfo, O: TensorInfo,
+                 scale: Optional[float] = None, window: int = 0):
+        self._op = _vp()
+        if scale is None:
+            scale = float(Q.extents[-1]) ** -0.5 if Q.extents else 1.0
+        _check(_lib.btc_create_paged_attention(handle._h, Q._t, K._t, V._t, table._t, O._t, scale, window,
+                                               ctypes.byref(self._op)), "btc_create_paged_attention")
+
+    def execute(self, stream: int, Q: int, K: int, V: int, table: int, lengths: int, O: int, lse: int = 0,
+                workspace: int = 0, workspace_bytes: int = 0, flags: int = 0) -> None:
+        """Device pointers as integers; lengths int32 [N] on the device; lse float32 [N, Hq] or 0."""
+        rc = _lib.btc_paged_attention_execute(self._op, stream, Q, K, V, table, lengths, O, lse, workspace,
+                                              workspace_bytes, flags)
+        if rc:
+            raise BtcError(rc, "btc_paged_attention_execute")
 
 
 def elementwise(handle: Handle, A, labelsA, B, C, labelsC, alpha=1.0, beta=0.0, conjA=False, conjB=False, stream: int = 0):

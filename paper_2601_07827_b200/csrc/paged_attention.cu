@@ -1,0 +1,198 @@
+// C entry points of the paged attention operator (paged_attention_kernel.cuh).
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <cmath>
+#include <cstring>
+
+#include "decoder_host.h"
+#include "paged_attention_kernel.cuh"
+
+using namespace btc;
+
+struct btc_paged_attention_s {
+    btc_handle_s handle;
+    TensorDesc q, k, v, table, o;
+    double scale = 1.0;
+    int32_t window = 0;
+    int32_t dp = 64, nt = 1;       // padded head size, blocks of 8 query heads per item
+    int64_t blocks = 1;            // items per key head
+};
+
+namespace {
+
+size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : 2; }
+
+// CTAs of the first kernel: one per SM (shared memory admits no second)
+int ctas_of(const btc_paged_attention_s &op) { return std::min(op.handle.sm_count, kJoinMaxCtas); }
+
+int64_t slot_floats(const btc_paged_attention_s &op) { return int64_t(8 * op.nt) * op.dp + 16 * op.nt; }
+
+size_t workspace_bytes_of(const btc_paged_attention_s &op)
+{
+    const size_t ctas = size_t(ctas_of(op));
+    return ctas * 2 * size_t(slot_floats(op)) * sizeof(float) + ctas * 2 * sizeof(int32_t);
+}
+
+bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
+{
+    const size_t r = t.extent.size();
+    if (t.stride[r - 1] != 1) return false;
+    for (size_t i = 0; i + 1 < r; ++i)
+        if (t.stride[i] % elements != 0) return false;
+    return true;
+}
+
+template <typename T, int DP, int NT>
+btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t st)
+{
+    typedef AttentionShape<T, DP, NT> Shape;
+    static std::atomic<bool> configured[64] = {};
+    const int slot = device & 63;
+    if (!configured[slot].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(paged_attention_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::SMEM) != cudaSuccess) {
+            cudaGetLastError();
+            return BTC_ERR_CUDA;
+        }
+        configured[slot].store(true, std::memory_order_relaxed);
+    }
+    paged_attention_kernel<T, DP, NT><<<unsigned(ctas), Shape::WARPS * 32, Shape::SMEM, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return BTC_ERR_CUDA;
+    // the joining kernel is set up while the first one runs and waits for its end on the device
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(ctas), 8 * NT);
+    cfg.blockDim = dim3(DP);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, DP, NT>, p, ctas) != cudaSuccess) {
+        cudaGetLastError();
+        return BTC_ERR_CUDA;
+    }
+    return BTC_SUCCESS;
+}
+
+template <typename T> btc_error_t launch_typed(const btc_paged_attention_s &op, const AttentionParams &p, cudaStream_t st)
+{
+    const int dev = op.handle.device, ctas = ctas_of(op);
+    if (op.dp == 64) return op.nt == 1 ? launch<T, 64, 1>(p, dev, ctas, st) : launch<T, 64, 2>(p, dev, ctas, st);
+    if (op.dp == 128) return op.nt == 1 ? launch<T, 128, 1>(p, dev, ctas, st) : launch<T, 128, 2>(p, dev, ctas, st);
+    return launch<T, 256, 1>(p, dev, ctas, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q, btc_tensor_info_t K,
+                                       btc_tensor_info_t V, btc_tensor_info_t table, btc_tensor_info_t O, double scale,
+                                       int32_t window, btc_paged_attention_t *out)
+{
+    if (!handle || !Q || !K || !V || !table || !O || !out) return BTC_ERR_INVALID_ARGUMENT;
+    if (window < 0 || !std::isfinite(scale)) return BTC_ERR_INVALID_ARGUMENT;
+    return guarded([&]() -> btc_error_t {
+        const TensorDesc &q = Q->desc, &k = K->desc, &v = V->desc, &t = table->desc, &o = O->desc;
+        if (q.extent.size() != 3 || k.extent.size() != 4 || v.extent.size() != 4 || t.extent.size() != 2 || o.extent.size() != 3)
+            return BTC_ERR_INVALID_ARGUMENT;
+        if (!decoder_type(q.dtype) || k.dtype != q.dtype || v.dtype != q.dtype || o.dtype != q.dtype || t.dtype != BTC_I32)
+            return BTC_ERR_NOT_SUPPORTED;
+        if (k.extent[3] != q.extent[2] || o.extent[2] != v.extent[3] || o.extent[0] != q.extent[0] || o.extent[1] != q.extent[1] ||
+            t.extent[0] != q.extent[0] || v.extent[0] != k.extent[0] || v.extent[1] != k.extent[1] || v.extent[2] != k.extent[2] ||
+            q.extent[1] % k.extent[2] != 0)
+            return BTC_ERR_EXTENT_MISMATCH;
+        if (q.extent[2] > kAttnMaxDim || v.extent[3] > kAttnMaxDim) return BTC_ERR_NOT_SUPPORTED;
+        if (k.extent[0] > INT32_MAX || k.extent[1] > INT32_MAX || t.extent[1] > INT32_MAX || q.extent[0] > INT32_MAX / 2 ||
+            q.extent[1] > INT32_MAX / 2 || q.extent[1] * o.extent[2] > INT32_MAX / 2)
+            return BTC_ERR_NOT_SUPPORTED;
+        for (const TensorDesc *d : {&q, &k, &v, &t, &o})
+            if (!spans_fit(*d)) return BTC_ERR_NOT_SUPPORTED;
+        if (d_may_alias(o)) return BTC_ERR_D_ALIASING;
+        btc_paged_attention_s op;
+        op.handle = *handle;
+        op.q = q; op.k = k; op.v = v; op.table = t; op.o = o;
+        op.scale = scale;
+        op.window = window;
+        const int64_t dim = std::max(q.extent[2], v.extent[3]), group = q.extent[1] / k.extent[2];
+        op.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
+        // Groups of more than 8 heads take 16 at a time, so that the cache is read once per 16 heads; heads of more
+        // than 128 elements 8 at a time (the output of 16 would not fit the registers)
+        op.nt = group > 8 && op.dp <= 128 ? 2 : 1;
+        op.blocks = (group + 8 * op.nt - 1) / (8 * op.nt);
+        if (__int128(q.extent[0]) * k.extent[2] * op.blocks > INT32_MAX) return BTC_ERR_NOT_SUPPORTED;
+        btc_paged_attention_s *kept = new (std::nothrow) btc_paged_attention_s(std::move(op));
+        if (!kept) return BTC_ERR_OUT_OF_MEMORY;
+        *out = kept;
+        return BTC_SUCCESS;
+    });
+}
+
+btc_error_t btc_destroy_paged_attention(btc_paged_attention_t *op)
+{
+    if (!op) return BTC_ERR_INVALID_ARGUMENT;
+    delete *op;
+    *op = nullptr;
+    return BTC_SUCCESS;
+}
+
+btc_error_t btc_paged_attention_workspace_size(btc_paged_attention_t op, size_t *bytes)
+{
+    if (!op || !bytes) return BTC_ERR_INVALID_ARGUMENT;
+    *bytes = workspace_bytes_of(*op);
+    return BTC_SUCCESS;
+}
+
+btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_stream, const void *Q, const void *K,
+                                        const void *V, const int32_t *table, const int32_t *lengths, void *O, float *lse,
+                                        void *workspace, size_t workspace_bytes, int32_t *flags)
+{
+    if (!op || !Q || !K || !V || !table || !lengths || !O) return BTC_ERR_INVALID_ARGUMENT;
+    const size_t es = esize(op->q.dtype);
+    for (const void *x : {Q, K, V, static_cast<const void *>(O)})
+        if (!aligned_to(x, es)) return BTC_ERR_MISALIGNED;
+    if (!aligned_to(table, 4) || !aligned_to(lengths, 4) || !aligned_to(lse, 4) || !aligned_to(flags, 4)) return BTC_ERR_MISALIGNED;
+    if (!workspace || workspace_bytes < workspace_bytes_of(*op)) return BTC_ERR_WORKSPACE_TOO_SMALL;
+    if (!aligned_to(workspace, 256)) return BTC_ERR_MISALIGNED;
+    if (op->handle.device < 0) return BTC_ERR_CUDA;
+
+    AttentionParams p;
+    std::memset(static_cast<void *>(&p), 0, sizeof p);
+    p.q = Q; p.k = K; p.v = V; p.o = O;
+    p.table = table; p.lengths = lengths; p.lse = lse; p.flags = flags;
+    const int64_t ctas = ctas_of(*op);
+    p.partial = static_cast<float *>(workspace);
+    p.partial_item = reinterpret_cast<int32_t *>(p.partial + ctas * 2 * slot_floats(*op));
+    p.q_n = op->q.stride[0]; p.q_h = op->q.stride[1]; p.q_d = op->q.stride[2];
+    p.o_n = op->o.stride[0]; p.o_h = op->o.stride[1]; p.o_d = op->o.stride[2];
+    p.k_page = op->k.stride[0]; p.k_slot = op->k.stride[1]; p.k_head = op->k.stride[2]; p.k_d = op->k.stride[3];
+    p.v_page = op->v.stride[0]; p.v_slot = op->v.stride[1]; p.v_head = op->v.stride[2]; p.v_d = op->v.stride[3];
+    p.table_n = op->table.stride[0]; p.table_j = op->table.stride[1];
+    p.sequences = int32_t(op->q.extent[0]);
+    p.heads = int32_t(op->q.extent[1]);
+    p.key_heads = int32_t(op->k.extent[2]);
+    p.group = p.heads / p.key_heads;
+    p.blocks = int32_t(op->blocks);
+    p.dim_k = int32_t(op->k.extent[3]);
+    p.dim_v = int32_t(op->v.extent[3]);
+    p.pages = int32_t(op->k.extent[0]);
+    p.columns = int32_t(op->table.extent[1]);
+    p.window = op->window;
+    p.page.set(op->k.extent[1]);
+    p.room = int32_t(std::min<int64_t>(op->table.extent[1] * op->k.extent[1], 0x7ffffff0));
+    const int64_t vec = int64_t(16 / es);
+    p.vec_k = rows_allow_vectors(op->k, vec) && aligned_to(K, 16);
+    p.vec_v = rows_allow_vectors(op->v, vec) && aligned_to(V, 16);
+    p.whole_tiles = p.vec_k && p.vec_v && op->k.extent[1] % kAttnTok == 0;
+    p.vec_q = es == 2 && p.dim_k % 2 == 0 && rows_allow_vectors(op->q, 2) && aligned_to(Q, 4);
+    p.scale_log2 = float(op->scale * 1.4426950408889634);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    switch (op->q.dtype) {
+    case BTC_F32: return launch_typed<float>(*op, p, st);
+    case BTC_F16: return launch_typed<__half>(*op, p, st);
+    default: return launch_typed<__nv_bfloat16>(*op, p, st);
+    }
+}
+
+}  // extern "C"

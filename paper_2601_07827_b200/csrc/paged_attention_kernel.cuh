@@ -1,0 +1,793 @@
+// Attention of one new token per sequence over a paged key-value cache.
+//
+//   o[h] = sum_j softmax_j(scale q[h] . k_j) v_j   over the visible tokens j of the sequence
+//
+// Every visible key and value is read once and used by the query heads that share it: 2 * group
+// multiply-adds per element, far below what the tensor cores need to be busy, so the pass is bound by
+// HBM and everything here serves to keep copies in flight:
+//   * a warp is a pipeline of its own: it copies tiles of 16 tokens (keys and values of one key head) into
+//     a ring of `STAGES` buffers with 16-byte cp.async and consumes them without any CTA barrier.  Eight
+//     warps with two tiles of 8 KB in flight each are 128 KB per SM.
+//   * S^T = K Q^T and O^T = V^T P^T with mma.sync: tokens are the M side of the first product and head
+//     elements that of the second, so 8 query heads fill the N side (with the heads on the M side half
+//     of each product would be padding for groups of 8), and P needs only a transpose of 8 x 8 blocks.
+//     The products are a few percent of the time; mma.sync keeps them in registers of the warp that
+//     copied the tile, where tcgen05's 128-row tiles would be 15/16 empty.
+//   * 16-bit types: P is split in two (p = hi + lo, products with both), so that the result carries
+//     one rounding, that of the output.  fp32: each product is formed from three TF32 products
+//     (x = hi + lo; lo * lo is dropped, at most 2^-22 of the product), as in the contractions.
+//   * running maximum, sum and output in fp32 (the flash form); the output is rescaled only when a maximum moved.
+// Work.  The tiles of all (sequence, key head) pairs form one list; CTAs and in them warps take equal
+// contiguous ranges of it, whatever the lengths are, found on the device from a prefix sum of the tile
+// counts (the host never reads a length).  What a warp cannot finish is merged in shared memory by its
+// CTA, what a CTA cannot finish goes to the workspace and a second small kernel joins it, in a fixed order.
+#pragma once
+
+#include "../../include/btc.h"
+#include "decoder_common.cuh"
+
+namespace btc {
+
+constexpr int kAttnTok = 16;                 // tokens per tile
+constexpr int kAttnMaxDim = 256;
+
+struct AttentionParams {
+    const void *q, *k, *v;
+    void *o;
+    const int32_t *table, *lengths;
+    float *lse;                              // [sequences][query heads] or NULL
+    int32_t *flags;
+    float *partial;                          // workspace: [CTA][2][8 NT heads x DP values, then maxima, then sums]
+    int32_t *partial_item;                   // workspace: [CTA][2] item, -1: none
+    int64_t q_n, q_h, q_d, o_n, o_h, o_d;
+    int64_t k_page, k_slot, k_head, k_d, v_page, v_slot, v_head, v_d;
+    int64_t table_n, table_j;
+    int32_t sequences, heads, key_heads, group, blocks;   // blocks: groups of 8 NT query heads per key head
+    int32_t dim_k, dim_v, pages, columns;
+    int32_t window;                          // 0: everything up to the length is visible
+    int32_t room;                            // tokens a table row can hold
+    int32_t whole_tiles;                     // vec_k and vec_v, and pages of whole tiles
+    int32_t vec_k, vec_v, vec_q;             // 16-byte copies of keys / values, 4-byte loads of queries
+    FastDiv page;
+    float scale_log2;                        // scale * log2(e)
+};
+
+// per-warp ring and per-CTA warps by size of the padded head: about 200 KB of shared memory in every form
+template <typename T, int DP, int NT> struct AttentionShape {
+    static constexpr int ROW = DP * int(sizeof(T));              // bytes of a token's row of one tensor
+    static constexpr int STAGE = 2 * kAttnTok * ROW;             // keys and values
+    static constexpr int DEPOSIT = 8 * NT * DP * 4;              // an unfinished item's output
+    static constexpr int WARPS = STAGE <= 4096 ? 8 : STAGE <= 8192 ? (NT == 1 ? 8 : 7) : STAGE <= 16384 ? 4 : 3;
+    static constexpr int STAGES = STAGE <= 4096 ? 6 : STAGE <= 16384 ? 3 : 2;
+    static constexpr int RING = STAGES * STAGE;
+    static constexpr int SMEM = WARPS * (RING + DEPOSIT);
+    static_assert(RING >= DEPOSIT + 2 * WARPS * 3 * 8 * NT * 4, "the last item's deposit, and warp 0's joint figures, take the ring");
+    static_assert(WARPS * DEPOSIT >= (WARPS * 32 + 1) * 8, "the prefix sum takes the first items' place");
+};
+
+template <typename T> struct AttentionBias { static constexpr float value = 0.f; };
+// f16 products: probabilities are kept 2^10 times larger (they cancel against the sum), so that values down to
+// 2^-24 of the largest stay normal numbers
+template <> struct AttentionBias<__half> { static constexpr float value = 10.f; };
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], unsigned addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], unsigned addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x = hi + lo with hi rounded to TF32's 11 significant bits (so that |lo| <= 2^-11 |x|); the tensor core ignores the
+// low 13 bits of what it is given, hence lo is rounded by adding half a unit: 2^-22 |x| is left out
+__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t &hi, uint32_t &lo)
+{
+    hi = (x + 0x1000u) & 0xffffe000u;
+    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
+}
+__device__ __forceinline__ void mma8_split(float (&c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], uint32_t x0, uint32_t x1)
+{
+    uint32_t h0, l0, h1, l1;
+    split_tf32(x0, h0, l0);
+    split_tf32(x1, h1, l1);
+    mma8_tf32(c, al, h0, h1);
+    mma8_tf32(c, ah, l0, l1);
+    mma8_tf32(c, ah, h0, h1);
+}
+// copies `bytes` (0..16) and fills the rest of the 16 with zeros
+__device__ __forceinline__ void cp_async_part(unsigned dst, const void *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// visible tokens [begin, end) of a sequence, and its tiles, which start at multiples of 16 tokens
+struct AttentionSpan {
+    int32_t begin, end, first_tile, tiles;
+    __device__ __forceinline__ void set(const AttentionParams &p, int32_t length)
+    {
+        const int32_t room = p.room;
+        end = length < 0 ? 0 : (length > room ? room : length);
+        begin = p.window > 0 && end > p.window ? end - p.window : 0;
+        first_tile = begin / kAttnTok;
+        tiles = end / kAttnTok + (end % kAttnTok != 0) - first_tile;
+    }
+};
+
+// A place in the list of tiles: sequence, head block, tile; the same in every lane.
+struct AttentionCursor {
+    int32_t seq, hb, tile;                   // tile counted from the span's first
+    int32_t key_head, block;                 // hb = key_head * blocks + block
+    AttentionSpan span;
+    __device__ __forceinline__ void next(const AttentionParams &p)
+    {
+        if (++tile < span.tiles) return;
+        tile = 0;
+        ++hb;
+        if (++block < p.blocks) return;
+        block = 0;
+        if (++key_head < p.key_heads) return;
+        hb = key_head = 0;
+        span.tiles = 0;
+        while (span.tiles == 0 && ++seq < p.sequences) span.set(p, p.lengths[seq]);
+    }
+};
+
+template <typename T, int DP, int NT> struct AttentionWarp {
+    typedef AttentionShape<T, DP, NT> Shape;
+    static constexpr int ROW = Shape::ROW;
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int KSTEPS = F32 ? DP / 8 : DP / 16;
+    static constexpr int MT = DP / 16;
+
+    const AttentionParams &p;
+    unsigned ring;                           // shared-memory address of the warp's ring
+    int lane;
+    uint32_t q[NT][KSTEPS][2];               // the queries as N-side operand
+    float o[MT][NT][4];                      // O^T: rows head elements, columns query heads
+    float m[NT][2], l[NT][2];                // running maximum (of scale * score * log2 e) and this thread's part of the sum
+
+    __device__ __forceinline__ AttentionWarp(const AttentionParams &params, unsigned ring_addr, int lane_)
+        : p(params), ring(ring_addr), lane(lane_) {}
+
+    __device__ __forceinline__ static unsigned swizzled(int row, int chunk) { return unsigned(row * ROW + ((chunk ^ (row & 7)) << 4)); }
+
+    // page number and row in the page of token `tile * 16 + lane % 16`; -1 where the token is not visible or has no page
+    __device__ __forceinline__ int32_t look_up(const AttentionCursor &c, int32_t &row) const
+    {
+        const int32_t t = (c.span.first_tile + c.tile) * kAttnTok + (lane & 15);
+        if (t < c.span.begin || t >= c.span.end) { row = 0; return -1; }
+        const uint32_t j = p.page.div(uint32_t(t));
+        row = t - int32_t(j * p.page.d);
+        const int32_t page = p.table[c.seq * p.table_n + int64_t(j) * p.table_j];
+        if (page < 0 || page >= p.pages) {
+            if (p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
+            return -1;
+        }
+        return page;
+    }
+
+    // start the copies of a tile whose 16 rows are all there, in one page: an address step and a copy per row
+    __device__ __forceinline__ void copy_whole(unsigned dst, const T *src, int64_t s_slot, int dim) const
+    {
+        constexpr int CHUNKS = ROW / 16, PER = 16 / int(sizeof(T));
+        constexpr int STEP = CHUNKS >= 32 ? 1 : 32 / CHUNKS, COLS = CHUNKS >= 32 ? CHUNKS / 32 : 1;
+        const int sub = CHUNKS >= 32 ? 0 : lane / CHUNKS, chunk0 = CHUNKS >= 32 ? lane : lane % CHUNKS;
+#pragma unroll
+        for (int c0 = 0; c0 < COLS; ++c0) {
+            const int chunk = chunk0 + 32 * c0;
+            const int left = (dim - chunk * PER) * int(sizeof(T)), bytes = left < 0 ? 0 : (left < 16 ? left : 16);
+            const T *at = src + sub * s_slot + (bytes ? chunk * PER : 0);
+            const unsigned to = dst + sub * ROW + ((chunk ^ sub) << 4);       // = swizzled(sub, chunk): rows r0 + sub only flip bits 4 to 6
+#pragma unroll
+            for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
+                cp_async_part((to ^ ((r0 & 7) << 4)) + r0 * ROW, at, bytes);
+                at += STEP * s_slot;
+            }
+        }
+    }
+    // start the copies of a tile; rows without a token are zeros
+    __device__ __forceinline__ void copy_tensor(unsigned dst, const T *base, int64_t s_page, int64_t s_slot, int64_t s_d,
+                                                int dim, bool vec, int32_t page, int32_t row) const
+    {
+        constexpr int CHUNKS = ROW / 16, PER = 16 / int(sizeof(T));
+        if (vec) {
+            constexpr int STEP = CHUNKS >= 32 ? 1 : 32 / CHUNKS;      // rows a warp's copy instruction covers
+            constexpr int COLS = CHUNKS >= 32 ? CHUNKS / 32 : 1;
+            const int sub = CHUNKS >= 32 ? 0 : lane / CHUNKS;
+#pragma unroll
+            for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
+                const int r = r0 + sub;
+                const int32_t pg = __shfl_sync(0xffffffffu, page, r), rw = __shfl_sync(0xffffffffu, row, r);
+                const T *src = base + (pg < 0 ? 0 : pg * s_page + rw * s_slot);
+#pragma unroll
+                for (int c0 = 0; c0 < COLS; ++c0) {
+                    const int chunk = CHUNKS >= 32 ? lane + 32 * c0 : lane % CHUNKS;
+                    const int left = (dim - chunk * PER) * int(sizeof(T));
+                    const int bytes = pg < 0 || left <= 0 ? 0 : (left < 16 ? left : 16);
+                    cp_async_part(dst + swizzled(r, chunk), bytes ? src + chunk * PER : base, bytes);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int r = 0; r < kAttnTok; ++r) {
+                const int32_t pg = __shfl_sync(0xffffffffu, page, r), rw = __shfl_sync(0xffffffffu, row, r);
+                const T *src = base + (pg < 0 ? 0 : pg * s_page + rw * s_slot);
+                for (int d = lane; d < DP; d += 32) {
+                    T x = from_f32<T>(0.f);
+                    if (pg >= 0 && d < dim) x = src[d * s_d];
+                    const unsigned at = dst + swizzled(r, d / PER) + unsigned(d % PER) * unsigned(sizeof(T));
+                    if constexpr (F32) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
+                    else asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(*reinterpret_cast<const unsigned short *>(&x)) : "memory");
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void copy_tile(const AttentionCursor &c, int stage, int32_t page, int32_t row, uint32_t mask) const
+    {
+        const unsigned dst = ring + unsigned(stage) * Shape::STAGE;
+        const T *k = static_cast<const T *>(p.k) + c.key_head * p.k_head, *v = static_cast<const T *>(p.v) + c.key_head * p.v_head;
+        if (p.whole_tiles && mask == 0xffffu) {
+            // the page holds a multiple of 16 tokens, so `page` is the same in every lane and lane 0 has the first row
+            const int64_t first = __shfl_sync(0xffffffffu, row, 0);
+            copy_whole(dst, k + page * p.k_page + first * p.k_slot, p.k_slot, p.dim_k);
+            copy_whole(dst + kAttnTok * ROW, v + page * p.v_page + first * p.v_slot, p.v_slot, p.dim_v);
+            return;
+        }
+        copy_tensor(dst, k, p.k_page, p.k_slot, p.k_d, p.dim_k, p.vec_k, page, row);
+        copy_tensor(dst + kAttnTok * ROW, v, p.v_page, p.v_slot, p.v_d, p.dim_v, p.vec_v, page, row);
+    }
+
+    __device__ __forceinline__ int first_head(const AttentionCursor &c, int &count) const
+    {
+        count = min(8 * NT, p.group - c.block * 8 * NT);
+        return c.key_head * p.group + c.block * 8 * NT;
+    }
+
+    __device__ __forceinline__ void begin_item(const AttentionCursor &c)
+    {
+        int count;
+        const int h0 = first_head(c, count);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int h = nt * 8 + lane / 4;
+            const T *src = static_cast<const T *>(p.q) + c.seq * p.q_n + int64_t(h0 + (h < count ? h : 0)) * p.q_h;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t x = 0;
+                    if constexpr (F32) {
+                        const int d = ks * 8 + half * 4 + lane % 4;
+                        if (h < count && d < p.dim_k) x = __float_as_uint(src[d * p.q_d]);
+                    } else {
+                        const int d = ks * 16 + half * 8 + 2 * (lane % 4);
+                        if (h < count && d < p.dim_k) {
+                            if (p.vec_q) {
+                                x = *reinterpret_cast<const uint32_t *>(src + d);
+                            } else {
+                                x = *reinterpret_cast<const unsigned short *>(src + d * p.q_d);
+                                if (d + 1 < p.dim_k) x |= uint32_t(*reinterpret_cast<const unsigned short *>(src + (d + 1) * p.q_d)) << 16;
+                            }
+                        }
+                    }
+                    q[nt][ks][half] = x;
+                }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) { m[nt][j] = -INFINITY; l[nt][j] = 0.f; }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[mt][nt][j] = 0.f;
+        }
+    }
+
+    // The scores of a tile by plain fp32 products.  A split infinity is inf + NaN, so a tile with a score that is not
+    // a number is computed again here, where infinite keys give infinite scores.
+    __device__ __noinline__ static void plain_scores(const AttentionParams &p, const AttentionCursor &c, int h0, int count,
+                                                     unsigned keys, int lane, float (*s)[4])
+    {
+        for (int nt = 0; nt < NT; ++nt)
+            for (int j = 0; j < 2; ++j) {
+                const int h = nt * 8 + 2 * (lane & 3) + j;
+                const float *src = static_cast<const float *>(p.q) + c.seq * p.q_n + int64_t(h0 + (h < count ? h : 0)) * p.q_h;
+                float x = 0.f, y = 0.f;
+                for (int d = 0; d < p.dim_k; ++d) {
+                    float k0, k1;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k0) : "r"(keys + swizzled(lane >> 2, d >> 2) + unsigned(d & 3) * 4u) : "memory");
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k1) : "r"(keys + swizzled((lane >> 2) + 8, d >> 2) + unsigned(d & 3) * 4u) : "memory");
+                    const float qd = src[d * p.q_d];
+                    x = fmaf(k0, qd, x);
+                    y = fmaf(k1, qd, y);
+                }
+                s[nt][j] = x;
+                s[nt][j + 2] = y;
+            }
+    }
+
+    // one tile; bit r of `seen`: token r counts
+    __device__ __forceinline__ void tile(const AttentionCursor &cur, int stage, uint32_t seen)
+    {
+        const unsigned ks_base = ring + unsigned(stage) * Shape::STAGE, vs_base = ks_base + kAttnTok * ROW;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
+        {
+            // rows are ROW bytes on a ring aligned to them: stepping to the next pair of chunks flips address bits
+            const unsigned at = ks_base + swizzled(((lane >> 3) & 1) * 8 + (lane & 7), lane >> 4);
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) {
+                uint32_t a[4];
+                ldsm4(a, at ^ (ks << 5));
+                if constexpr (F32) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) split_tf32(a[j], hi[j], lo[j]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma8_split(s[nt], hi, lo, q[nt][ks][0], q[nt][ks][1]);
+                } else {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma16(s[nt], a, q[nt][ks][0], q[nt][ks][1], T());
+                }
+            }
+        }
+        if constexpr (F32) {
+            bool odd = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) odd |= s[nt][j] != s[nt][j];
+            if (__any_sync(0xffffffffu, odd)) {
+                int count;
+                const int h0 = first_head(cur, count);
+                float again[NT][4];
+                plain_scores(p, cur, h0, count, ks_base, lane, again);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[nt][j] = again[nt][j];
+            }
+        }
+        const bool ok0 = (seen >> (lane >> 2)) & 1, ok1 = (seen >> ((lane >> 2) + 8)) & 1;
+        float alpha[NT][2];
+        bool moved = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float &s0 = s[nt][j], &s1 = s[nt][j + 2];
+                s0 = ok0 ? s0 * p.scale_log2 : -INFINITY;
+                s1 = ok1 ? s1 * p.scale_log2 : -INFINITY;
+                float top = fmaxf(s0, s1);
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                top = fmaxf(top, m[nt][j]);
+                // nothing seen yet (or every score is -inf): subtract 0, the probabilities are exp2(-inf) = 0
+                const float base = (top == -INFINITY ? 0.f : top) - AttentionBias<T>::value;
+                alpha[nt][j] = m[nt][j] == top ? 1.f : exp2f(m[nt][j] - top);
+                moved |= alpha[nt][j] != 1.f;
+                m[nt][j] = top;
+                s0 = exp2f(s0 - base);
+                s1 = exp2f(s1 - base);
+                l[nt][j] = l[nt][j] * alpha[nt][j] + (s0 + s1);
+            }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[mt][nt][j] *= alpha[nt][j & 1];
+        }
+        if constexpr (F32) {
+            // P (rows tokens, columns heads) -> N-side operand: token lane % 4 (+ 4, + 8, + 12) of head lane / 4
+            uint32_t b[NT][2][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int src = (half * 4 + (lane & 3)) * 4 + (lane >> 3);
+                        const float x = __shfl_sync(0xffffffffu, s[nt][2 * ks], src), y = __shfl_sync(0xffffffffu, s[nt][2 * ks + 1], src);
+                        b[nt][ks][half] = __float_as_uint((lane >> 2) & 1 ? y : x);
+                    }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    uint32_t hi[4], lo[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int d = mt * 16 + (j & 1) * 8 + (lane >> 2), t = ks * 8 + (j >> 1) * 4 + (lane & 3);
+                        uint32_t x;
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(vs_base + swizzled(t, d >> 2) + unsigned(d & 3) * 4u) : "memory");
+                        split_tf32(x, hi[j], lo[j]);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma8_split(o[mt][nt], hi, lo, b[nt][ks][0], b[nt][ks][1]);
+                }
+        } else {
+            uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float x = s[nt][2 * half], y = s[nt][2 * half + 1];
+                    const float xh = to_f32(from_f32<T>(x)), yh = to_f32(from_f32<T>(y));
+                    hi[nt][half] = transpose8x8(pack2(xh, yh, T()));
+                    lo[nt][half] = transpose8x8(pack2(x - xh, y - yh, T()));
+                }
+            const unsigned at = vs_base + swizzled((lane >> 4) * 8 + (lane & 7), (lane >> 3) & 1);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                uint32_t a[4];
+                ldsm4_trans(a, at ^ (mt << 5));
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma16(o[mt][nt], a, hi[nt][0], hi[nt][1], T());
+                    mma16(o[mt][nt], a, lo[nt][0], lo[nt][1], T());
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish_sums()
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float &x = l[nt][j];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+            }
+    }
+    __device__ __forceinline__ void write_out(const AttentionCursor &c) const
+    {
+        int count;
+        const int h0 = first_head(c, count);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int h = nt * 8 + 2 * (lane & 3) + j;
+                if (h >= count) continue;
+                const float inv = l[nt][j] == 0.f ? 0.f : 1.f / l[nt][j];
+                T *dst = static_cast<T *>(p.o) + c.seq * p.o_n + int64_t(h0 + h) * p.o_h;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int d = mt * 16 + half * 8 + (lane >> 2);
+                        if (d < p.dim_v) dst[d * p.o_d] = from_f32<T>(o[mt][nt][2 * half + j] * inv);
+                    }
+                if (p.lse && lane < 4)
+                    p.lse[int64_t(c.seq) * p.heads + h0 + h] = l[nt][j] == 0.f ? -INFINITY
+                        : (m[nt][j] - AttentionBias<T>::value + log2f(l[nt][j])) * 0.6931471805599453f;
+            }
+    }
+    // an unfinished item: output, maxima and sums to shared memory
+    __device__ __forceinline__ void deposit(float *out, float *stats) const
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int h = nt * 8 + 2 * (lane & 3) + j;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        out[h * DP + mt * 16 + half * 8 + (lane >> 2)] = o[mt][nt][2 * half + j];
+                if (lane < 4) {
+                    stats[h] = m[nt][j];
+                    stats[8 * NT + h] = l[nt][j];
+                }
+            }
+    }
+};
+
+// what a part with maximum m counts in a whole with maximum top >= m (a part that saw nothing has m = -inf and o = l = 0)
+__device__ __forceinline__ float join_weight(float m, float top) { return m == top ? 1.f : exp2f(m - top); }
+
+// element d of head h of an item (8 NT = `per` heads) from its joined sums
+template <typename T>
+__device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t item, int per, int h, int d, float o, float m, float l)
+{
+    const int head_blocks = p.key_heads * p.blocks;
+    const int seq = item / head_blocks, hb = item - seq * head_blocks;
+    const int kh = hb / p.blocks, in_group = (hb - kh * p.blocks) * per + h;
+    if (in_group >= p.group) return;
+    const int head = kh * p.group + in_group;
+    if (d < p.dim_v)
+        static_cast<T *>(p.o)[seq * p.o_n + int64_t(head) * p.o_h + d * p.o_d] = from_f32<T>(l == 0.f ? 0.f : o / l);
+    if (d == 0 && p.lse)
+        p.lse[int64_t(seq) * p.heads + head] = l == 0.f ? -INFINITY : (m - AttentionBias<T>::value + log2f(l)) * 0.6931471805599453f;
+}
+
+template <typename T, int DP, int NT>
+__global__ void __launch_bounds__(AttentionShape<T, DP, NT>::WARPS * 32, 1)
+paged_attention_kernel(const __grid_constant__ AttentionParams p)
+{
+    typedef AttentionShape<T, DP, NT> Shape;
+    constexpr int W = Shape::WARPS, THREADS = W * 32, STAGES = Shape::STAGES, H = 8 * NT;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ float stats[2 * W][2 * H];
+    __shared__ int32_t dep_item[2 * W];
+    __shared__ int32_t first_item, last_item;                  // items of the CTA's range that it does not hold whole; -1: none
+    int64_t *scan = reinterpret_cast<int64_t *>(smem + W * Shape::RING);     // until the ranges are known
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int head_blocks = p.key_heads * p.blocks;
+
+    // the combining kernel may set itself up while this one runs
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // tiles of all sequences: thread i sums sequences [i * per, (i + 1) * per), then a prefix sum over the threads
+    const int per = (p.sequences + THREADS - 1) / THREADS;
+    {
+        int64_t mine = 0;
+        for (int i = 0; i < per; ++i) {
+            const int s = tid * per + i;
+            if (s >= p.sequences) break;
+            const int32_t length = p.lengths[s];
+            AttentionSpan span;
+            span.set(p, length);
+            mine += span.tiles;
+            if (blockIdx.x == 0 && p.flags && (length < 0 || length > p.room)) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+        }
+        int64_t x = mine;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, k);
+            if (lane >= k) x += y;
+        }
+        scan[tid + 1] = x;
+        if (tid == 0) { scan[0] = 0; first_item = last_item = -1; }
+        if (tid < 2 * W) dep_item[tid] = -1;
+        __syncthreads();
+        int64_t before = 0;
+        for (int w = 0; w < warp; ++w) before += scan[(w + 1) * 32];
+        __syncthreads();
+        scan[tid + 1] = x + before;
+        __syncthreads();
+    }
+    // sequences with nothing to see
+    for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
+        AttentionSpan span;
+        span.set(p, p.lengths[s]);
+        if (span.tiles == 0) {
+            for (int e = tid; e < p.heads * p.dim_v; e += THREADS) {
+                const int h = e / p.dim_v, d = e - h * p.dim_v;
+                static_cast<T *>(p.o)[s * p.o_n + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
+            }
+            if (p.lse)
+                for (int h = tid; h < p.heads; h += THREADS) p.lse[int64_t(s) * p.heads + h] = -INFINITY;
+        }
+    }
+
+    // equal ranges of the list of tiles, at least one tile per warp of the CTAs that take part
+    const int64_t total = scan[THREADS] * head_blocks;
+    int64_t ctas = (total + W - 1) / W;
+    if (ctas > gridDim.x) ctas = gridDim.x;
+    int64_t lo = 0, hi = 0, cta_lo = 0, cta_hi = 0;
+    if (blockIdx.x < ctas) {
+        const int64_t each = total / ctas, more = total - each * ctas;
+        cta_lo = each * blockIdx.x + min(int64_t(blockIdx.x), more);
+        cta_hi = cta_lo + each + (int64_t(blockIdx.x) < more ? 1 : 0);
+        const int64_t n = cta_hi - cta_lo, we = n / W, wm = n - we * W;
+        lo = cta_lo + we * warp + min(int64_t(warp), wm);
+        hi = lo + we + (warp < wm ? 1 : 0);
+    }
+
+    const unsigned ring = static_cast<unsigned>(__cvta_generic_to_shared(smem)) + unsigned(warp) * Shape::RING;
+    float *deposit_first = reinterpret_cast<float *>(smem + W * Shape::RING) + warp * (Shape::DEPOSIT / 4);
+    float *deposit_last = reinterpret_cast<float *>(smem + warp * Shape::RING);
+
+    AttentionCursor cur;
+    if (lo < hi) {
+        // where the range begins: the thread whose sequences hold it, then walk those sequences
+        int a = 0, b = THREADS;                                 // scan[a] * head_blocks <= lo < scan[b] * head_blocks
+        while (b - a > 1) {
+            const int c = (a + b) / 2;
+            if (scan[c] * head_blocks <= lo) a = c; else b = c;
+        }
+        int64_t at = lo - scan[a] * head_blocks;
+        cur.seq = a * per;
+        cur.span.set(p, p.lengths[cur.seq]);
+        while (at >= int64_t(cur.span.tiles) * head_blocks && cur.seq + 1 < p.sequences) {
+            at -= int64_t(cur.span.tiles) * head_blocks;
+            cur.span.set(p, p.lengths[++cur.seq]);
+        }
+        cur.hb = int32_t(at / cur.span.tiles);
+        cur.tile = int32_t(at - int64_t(cur.hb) * cur.span.tiles);
+        cur.key_head = cur.hb / p.blocks;
+        cur.block = cur.hb - cur.key_head * p.blocks;
+        // does the CTA's range begin inside an item?
+        if (warp == 0 && cur.tile != 0 && lane == 0) first_item = cur.seq * head_blocks + cur.hb;
+    }
+    __syncthreads();
+
+    if (lo < hi) {
+        AttentionWarp<T, DP, NT> w(p, ring, lane);
+        const int64_t n = hi - lo;
+        AttentionCursor ahead = cur;                            // the tile whose page numbers are in `page`, `row`
+        int64_t issued = 0;
+        int32_t row, page = w.look_up(ahead, row);
+        // tokens that count: seen[k] belongs to the tile k steps ahead of the one being consumed
+        uint32_t seen[STAGES];
+        auto issue = [&](int stage, uint32_t &mask) {
+            mask = 0;
+            if (issued < n) {
+                mask = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
+                w.copy_tile(ahead, stage, page, row, mask);
+                if (++issued < n) {
+                    ahead.next(p);
+                    page = w.look_up(ahead, row);
+                }
+            }
+            cp_async_commit();
+        };
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; ++k) issue(k, seen[k]);
+        w.begin_item(cur);
+        bool began_here = cur.tile == 0;                        // the current item's first tile is in this warp's range
+        int stage = 0;
+        for (int64_t i = 0; i < n; ++i) {
+            cp_async_wait_group<STAGES - 2>();
+            __syncwarp();                                       // every lane's copies have landed, the oldest stage is free
+            issue(stage == 0 ? STAGES - 1 : stage - 1, seen[STAGES - 1]);
+            w.tile(cur, stage, seen[0]);
+#pragma unroll
+            for (int k = 0; k + 1 < STAGES; ++k) seen[k] = seen[k + 1];
+            if (++stage == STAGES) stage = 0;
+            const bool item_ends = cur.tile + 1 == cur.span.tiles;
+            if (item_ends || i + 1 == n) {
+                w.finish_sums();
+                if (item_ends && began_here) {
+                    w.write_out(cur);
+                } else {
+                    // an item that began in an earlier range goes to its own place; one that began here and is cut
+                    // off is the last, so that it can have the ring, which nothing uses any more
+                    const int slot = began_here ? 1 : 0;
+                    if (slot) cp_async_wait_group<0>();
+                    __syncwarp();
+                    w.deposit(slot ? deposit_last : deposit_first, stats[2 * warp + slot]);
+                    if (lane == 0) {
+                        dep_item[2 * warp + slot] = cur.seq * head_blocks + cur.hb;
+                        if (i + 1 == n && hi == cta_hi && !item_ends) last_item = cur.seq * head_blocks + cur.hb;
+                    }
+                }
+                if (i + 1 < n) {
+                    cur.next(p);
+                    w.begin_item(cur);
+                    began_here = true;
+                }
+            } else {
+                ++cur.tile;
+            }
+        }
+        cp_async_wait_group<0>();
+    }
+    __syncthreads();
+
+    float (*joined)[2 * H] = reinterpret_cast<float (*)[2 * H]>(smem + Shape::DEPOSIT);     // behind warp 0's deposit in its ring
+    float (*weight)[H] = reinterpret_cast<float (*)[H]>(smem + Shape::DEPOSIT + 2 * W * 2 * H * 4);
+    // join what the warps left: first each deposit's weight against the largest maximum of its item ...
+    const int64_t slot_floats = H * DP + 2 * H;
+    if (tid < 2) p.partial_item[2 * blockIdx.x + tid] = tid == 0 ? first_item : (last_item == first_item ? -1 : last_item);
+    if (blockIdx.x >= ctas) return;
+    for (int e = tid; e < 2 * W * H; e += THREADS) {
+        const int i = e / H, h = e - i * H;
+        const int32_t item = dep_item[i];
+        if (item < 0) continue;
+        float top = -INFINITY, sum = 0.f;
+        for (int j = 0; j < 2 * W; ++j)
+            if (dep_item[j] == item) top = fmaxf(top, stats[j][h]);
+        for (int j = 0; j < 2 * W; ++j)
+            if (dep_item[j] == item) sum += stats[j][H + h] * join_weight(stats[j][h], top);
+        weight[i][h] = join_weight(stats[i][h], top);
+        joined[i][h] = top;
+        joined[i][H + h] = sum;
+    }
+    __syncthreads();
+    // ... then the sums, an element (head, head element) per thread
+    for (int e = tid; e < H * DP; e += THREADS) {
+        const int h = e / DP, d = e - h * DP;
+        int i = 0;
+        while (i < 2 * W) {
+            const int32_t item = dep_item[i];
+            if (item < 0) { ++i; continue; }
+            const float m = joined[i][h], l = joined[i][H + h];
+            float o = 0.f;
+            for (; i < 2 * W && (dep_item[i] == item || dep_item[i] < 0); ++i) {
+                if (dep_item[i] < 0) continue;
+                const float *src = (i & 1) ? reinterpret_cast<const float *>(smem + (i >> 1) * Shape::RING)
+                                           : reinterpret_cast<const float *>(smem + W * Shape::RING) + (i >> 1) * (Shape::DEPOSIT / 4);
+                o = fmaf(src[e], weight[i][h], o);
+            }
+            if (item == first_item || item == last_item) {
+                float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * slot_floats;
+                out[e] = o;
+                if (d == 0) { out[H * DP + h] = m; out[H * DP + H + h] = l; }
+            } else {
+                write_joined<T>(p, item, H, h, d, o, m, l);
+            }
+        }
+    }
+}
+
+// Items that span CTAs: block (c, h) joins head h of the item that begins in CTA c's range and ends in a later
+// one's: CTA c's second slot, then the first slots of the CTAs after it while they carry the same item.
+constexpr int kJoinMaxCtas = 1024;
+template <typename T, int DP, int NT>
+__global__ void __launch_bounds__(DP) paged_attention_join_kernel(const __grid_constant__ AttentionParams p, int ctas)
+{
+    constexpr int H = 8 * NT;
+    constexpr int64_t slot_floats = H * DP + 2 * H;
+    __shared__ int32_t parts;
+    __shared__ float weight[kJoinMaxCtas], sums[kJoinMaxCtas], tops[DP / 32];
+    const int c = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int32_t item = p.partial_item[2 * c + 1];
+    if (item < 0) return;
+    if (d == 0) parts = ctas - c;
+    __syncthreads();
+    // part 0 is CTA c's second slot, part i CTA c + i's first; the first CTA without the item ends it
+    float top = -INFINITY;
+    for (int i = d; i < ctas - c; i += DP)
+        if (i > 0 && p.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
+    __syncthreads();
+    const int n = parts;
+    const float *first = p.partial + 2 * int64_t(c) * slot_floats;
+    auto part = [&](int i) { return first + (i == 0 ? slot_floats : 2 * int64_t(i) * slot_floats); };
+    for (int i = d; i < n; i += DP) {
+        weight[i] = part(i)[H * DP + h];
+        sums[i] = part(i)[H * DP + H + h];
+        top = fmaxf(top, weight[i]);
+    }
+    for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    if ((d & 31) == 0) tops[d / 32] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < DP / 32; ++w) top = fmaxf(top, tops[w]);
+    for (int i = d; i < n; i += DP) weight[i] = join_weight(weight[i], top);
+    __syncthreads();
+    float o = 0.f, l = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+        o = fmaf(part(i)[h * DP + d], weight[i], o);
+        l = fmaf(sums[i], weight[i], l);
+    }
+    write_joined<T>(p, item, H, h, d, o, top, l);
+}
+
+}  // namespace btc

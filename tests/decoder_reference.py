@@ -43,3 +43,45 @@ def rotary_backward(x, w, pos, freq, mult, interleaved, norm, eps, dy):
     n = xd * r
     g = dm * w.double() if w is not None else dm
     return r * (g - n * (g * n).mean(-1, keepdim=True)), (dm * n).sum((0, 1))
+
+
+def attention(q, k, v, table, lengths, scale, window, pages_ok=None):
+    """q [N, Hq, D], k / v [P, S, Hk, *], lengths as given; returns float64 o [N, Hq, Dv], lse [N, Hq], and per
+    (sequence, head) the scale of the error bound: sum p|v| [N, Hq, Dv], max_j scale sum_d |q k|, max |s|, tokens."""
+    N, Hq, D = q.shape
+    P, S, Hk, _ = k.shape
+    Dv = v.shape[-1]
+    group = Hq // Hk
+    o = torch.zeros(N, Hq, Dv, dtype=torch.float64)
+    lse = torch.full((N, Hq), float("-inf"), dtype=torch.float64)
+    size = torch.zeros(N, Hq, Dv, dtype=torch.float64)
+    moduli, top, count = torch.zeros(N, Hq), torch.zeros(N, Hq), torch.zeros(N, Hq)
+    for n in range(N):
+        length = max(0, min(int(lengths[n]), table.shape[1] * S))
+        low = max(0, length - window) if window else 0
+        tokens = [(int(table[n, j // S]), j % S) for j in range(low, length)]
+        tokens = [(p, r) for p, r in tokens if 0 <= p < P]
+        if not tokens:
+            continue
+        pg, rw = torch.tensor([t[0] for t in tokens]), torch.tensor([t[1] for t in tokens])
+        for h in range(Hq):
+            kk, vv, qq = k[pg, rw, h // group].double(), v[pg, rw, h // group].double(), q[n, h].double()
+            s = kk @ qq * scale
+            p = torch.softmax(s, 0)
+            o[n, h], lse[n, h] = p @ vv, torch.logsumexp(s, 0)
+            size[n, h] = p @ vv.abs()
+            moduli[n, h] = (kk.abs() @ qq.abs()).max() * abs(scale)
+            top[n, h], count[n, h] = s.abs().max(), len(tokens)
+    return o, lse, size, moduli, top, count
+
+
+def attention_bounds(o, lse, size, moduli, top, count, dim, dtype):
+    """Largest errors allowed (see test_gpu_paged_attention.py)."""
+    split = {torch.float32: 2.0 ** -20, torch.float16: 2.0 ** -20, torch.bfloat16: 2.0 ** -15}[dtype]
+    score = (2 * dim + 8) * E32 * moduli + 4 * E32 * top + 8 * E32
+    if dtype == torch.float32:
+        score = score + 2.0 ** -20 * moduli
+    chain = 4 * (count / 16 + 64) * E32
+    rel = 2 * score + split + chain
+    return (UNIT[dtype] * o.abs() + rel[..., None].double() * size + FLOOR[dtype] + 1e-300,
+            score.double() + 4 * E32 * lse.abs().nan_to_num(0, 0, 0) + chain.double())

@@ -99,3 +99,36 @@ def test_rotary_frequencies(api):
     for bad in (dict(rotary_dim=7), dict(rotary_dim=8, factor=0.5), dict(rotary_dim=8, scaling="other")):
         with pytest.raises(ValueError):
             api.rotary_frequencies(**bad)
+
+
+def test_paged_attention_refusals(api, handle):
+    E, B = api, api.BF16
+    t = lambda *s, dt=B, st=None: dense(api, handle, dt, *s, strides=st)  # noqa: E731
+    i = lambda *s: dense(api, handle, api.I32, *s)  # noqa: E731
+    make = lambda *a, **k: code(api, lambda: api.PagedAttention(handle, *a, **k))  # noqa: E731
+    q, k, v, tab, o = t(3, 8, 64), t(9, 16, 2, 64), t(9, 16, 2, 32), i(3, 5), t(3, 8, 32)
+    op = api.PagedAttention(handle, q, k, v, tab, o)
+    assert op.workspace_size() > 0
+    assert make(t(3, 8, 64, dt=E.F64), k, v, tab, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, t(9, 16, 2, 64, dt=E.F16), v, tab, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, k, v, t(3, 5, dt=E.F32), o) == E.ERR_NOT_SUPPORTED
+    assert make(t(8, 64), k, v, tab, o) == E.ERR_INVALID_ARGUMENT
+    assert make(q, k, v, i(4, 5), o) == E.ERR_EXTENT_MISMATCH
+    assert make(t(3, 7, 64), k, v, tab, t(3, 7, 32)) == E.ERR_EXTENT_MISMATCH        # 7 heads over 2 key heads
+    assert make(q, k, t(9, 8, 2, 32), tab, o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, t(8, 16, 2, 32), tab, o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, t(9, 16, 2, 32), v, tab, o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, v, tab, t(3, 8, 64)) == E.ERR_EXTENT_MISMATCH
+    assert make(t(3, 8, 257), t(9, 16, 2, 257), v, tab, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, k, v, tab, t(3, 8, 32, st=(0, 32, 1))) == E.ERR_D_ALIASING
+    assert make(q, k, v, tab, o, window=-1) == E.ERR_INVALID_ARGUMENT
+    assert make(q, k, v, tab, o, scale=float("nan")) == E.ERR_INVALID_ARGUMENT
+    assert make(q, t(9, 16, 2, 64, st=(1 << 61, 128, 64, 1)), v, tab, o) == E.ERR_NOT_SUPPORTED
+    n = op.workspace_size()
+    run = lambda *a, **k: code(api, lambda: op.execute(0, *a, **k))  # noqa: E731
+    assert run(256, 256, 256, 256, 0, 256, workspace=256, workspace_bytes=n) == E.ERR_INVALID_ARGUMENT
+    assert run(256, 256, 256, 256, 256, 256) == E.ERR_WORKSPACE_TOO_SMALL
+    assert run(256, 256, 256, 256, 256, 256, workspace=256, workspace_bytes=n - 1) == E.ERR_WORKSPACE_TOO_SMALL
+    assert run(256, 256, 256, 256, 256, 256, workspace=128, workspace_bytes=n) == E.ERR_MISALIGNED
+    assert run(257, 256, 256, 256, 256, 256, workspace=256, workspace_bytes=n) == E.ERR_MISALIGNED
+    assert run(256, 256, 256, 258, 256, 256, workspace=256, workspace_bytes=n) == E.ERR_MISALIGNED

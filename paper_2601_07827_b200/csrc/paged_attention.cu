@@ -60,8 +60,8 @@ btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t 
     if (cudaGetLastError() != cudaSuccess) return BTC_ERR_CUDA;
     // the joining kernel is set up while the first one runs and waits for its end on the device
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(ctas), 8 * NT);
-    cfg.blockDim = dim3(DP);
+    cfg.gridDim = dim3(unsigned(ctas));
+    cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -79,6 +79,8 @@ template <typename T> btc_error_t launch_typed(const btc_paged_attention_s &op, 
 {
     const int dev = op.handle.device, ctas = ctas_of(op);
     if (op.dp == 64) return op.nt == 1 ? launch<T, 64, 1>(p, dev, ctas, st) : launch<T, 64, 2>(p, dev, ctas, st);
+    if constexpr (sizeof(T) == 4)
+        if (op.dp == 96) return op.nt == 1 ? launch<T, 96, 1>(p, dev, ctas, st) : launch<T, 96, 2>(p, dev, ctas, st);
     if (op.dp == 128) return op.nt == 1 ? launch<T, 128, 1>(p, dev, ctas, st) : launch<T, 128, 2>(p, dev, ctas, st);
     return launch<T, 256, 1>(p, dev, ctas, st);
 }
@@ -116,7 +118,8 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
         op.scale = scale;
         op.window = window;
         const int64_t dim = std::max(q.extent[2], v.extent[3]), group = q.extent[1] / k.extent[2];
-        op.dp = dim <= 64 ? 64 : (dim <= 128 ? 128 : 256);
+        // fp32 heads of 65 to 96 elements have a size of their own because products and shared memory bound them
+        op.dp = dim <= 64 ? 64 : (dim <= 96 && q.dtype == BTC_F32 ? 96 : (dim <= 128 ? 128 : 256));
         // Groups of more than 8 heads take 16 at a time, so that the cache is read once per 16 heads; heads of more
         // than 128 elements 8 at a time (the output of 16 would not fit the registers)
         op.nt = group > 8 && op.dp <= 128 ? 2 : 1;

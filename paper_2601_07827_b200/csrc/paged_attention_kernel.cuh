@@ -52,14 +52,17 @@ struct AttentionParams {
     float scale_log2;                        // scale * log2(e)
 };
 
-// per-warp ring and per-CTA warps by size of the padded head: about 200 KB of shared memory in every form
+// Per-warp ring and warps of a CTA: as many as 224 KB of shared memory hold.  fp32 tiles of 12 KB and more take
+// two stages and more warps instead of three (a tile is then 1000 instructions of products; what is
+// in flight, one tile of every warp, is still 96 KB).
 template <typename T, int DP, int NT> struct AttentionShape {
     static constexpr int ROW = DP * int(sizeof(T));              // bytes of a token's row of one tensor
     static constexpr int STAGE = 2 * kAttnTok * ROW;             // keys and values
     static constexpr int DEPOSIT = 8 * NT * DP * 4;              // an unfinished item's output
-    static constexpr int WARPS = STAGE <= 4096 ? 8 : STAGE <= 8192 ? (NT == 1 ? 8 : 7) : STAGE <= 16384 ? 4 : 3;
-    static constexpr int STAGES = STAGE <= 4096 ? 6 : STAGE <= 16384 ? 3 : 2;
+    static constexpr int STAGES = STAGE <= 4096 ? 6 : (sizeof(T) == 4 && STAGE > 8192 ? 2 : 3);
     static constexpr int RING = STAGES * STAGE;
+    static constexpr int FIT = 224 * 1024 / (RING + DEPOSIT);
+    static constexpr int WARPS = FIT < 8 ? FIT : 8;
     static constexpr int SMEM = WARPS * (RING + DEPOSIT);
     static_assert(RING >= DEPOSIT + 2 * WARPS * 3 * 8 * NT * 4, "the last item's deposit, and warp 0's joint figures, take the ring");
     static_assert(WARPS * DEPOSIT >= (WARPS * 32 + 1) * 8, "the prefix sum takes the first items' place");
@@ -108,14 +111,16 @@ __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t &hi, uint32_t &l
     hi = (x + 0x1000u) & 0xffffe000u;
     lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
 }
-__device__ __forceinline__ void mma8_split(float (&c)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], uint32_t x0, uint32_t x1)
+// the products with x0, x1: lo * hi, hi * lo and hi * hi, each into an accumulator
+__device__ __forceinline__ void mma8_split(float (&c_lh)[4], float (&c_hl)[4], float (&c_hh)[4], const uint32_t (&ah)[4],
+                                           const uint32_t (&al)[4], uint32_t x0, uint32_t x1)
 {
     uint32_t h0, l0, h1, l1;
     split_tf32(x0, h0, l0);
     split_tf32(x1, h1, l1);
-    mma8_tf32(c, al, h0, h1);
-    mma8_tf32(c, ah, l0, l1);
-    mma8_tf32(c, ah, h0, h1);
+    mma8_tf32(c_lh, al, h0, h1);
+    mma8_tf32(c_hl, ah, l0, l1);
+    mma8_tf32(c_hh, ah, h0, h1);
 }
 // copies `bytes` (0..16) and fills the rest of the 16 with zeros
 __device__ __forceinline__ void cp_async_part(unsigned dst, const void *src, int bytes)
@@ -191,55 +196,66 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         return page;
     }
 
+    // Which chunks of 16 bytes of which rows this lane copies: a copy instruction of the warp covers STEP rows
+    // (a part of one where a row has more than 32 chunks; rows of 24 chunks leave 8 lanes idle).
+    static constexpr int CHUNKS = ROW / 16, PER = 16 / int(sizeof(T));
+    static constexpr int STEP = CHUNKS >= 32 ? 1 : 32 / CHUNKS, COLS = CHUNKS >= 32 ? CHUNKS / 32 : 1;
+    static_assert(CHUNKS % 32 == 0 || CHUNKS < 32, "whole copy instructions");
+    __device__ __forceinline__ int my_sub() const { return STEP == 1 ? 0 : lane / CHUNKS; }
+    __device__ __forceinline__ int my_chunk() const { return STEP == 1 ? lane : lane % CHUNKS; }
+    __device__ __forceinline__ bool idle() const { return 32 % CHUNKS != 0 && CHUNKS < 32 && lane >= STEP * CHUNKS; }
+    __device__ __forceinline__ static int chunk_bytes(int chunk, int dim)
+    {
+        const int left = (dim - chunk * PER) * int(sizeof(T));
+        return left < 0 ? 0 : (left < 16 ? left : 16);
+    }
+
     // start the copies of a tile whose 16 rows are all there, in one page: an address step and a copy per row
     __device__ __forceinline__ void copy_whole(unsigned dst, const T *src, int64_t s_slot, int dim) const
     {
-        constexpr int CHUNKS = ROW / 16, PER = 16 / int(sizeof(T));
-        constexpr int STEP = CHUNKS >= 32 ? 1 : 32 / CHUNKS, COLS = CHUNKS >= 32 ? CHUNKS / 32 : 1;
-        const int sub = CHUNKS >= 32 ? 0 : lane / CHUNKS, chunk0 = CHUNKS >= 32 ? lane : lane % CHUNKS;
+        const int sub = my_sub();
 #pragma unroll
         for (int c0 = 0; c0 < COLS; ++c0) {
-            const int chunk = chunk0 + 32 * c0;
-            const int left = (dim - chunk * PER) * int(sizeof(T)), bytes = left < 0 ? 0 : (left < 16 ? left : 16);
+            const int chunk = my_chunk() + 32 * c0, bytes = chunk_bytes(chunk, dim);
             const T *at = src + sub * s_slot + (bytes ? chunk * PER : 0);
             const unsigned to = dst + sub * ROW + ((chunk ^ sub) << 4);       // = swizzled(sub, chunk): rows r0 + sub only flip bits 4 to 6
+            if (!idle()) {
 #pragma unroll
-            for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
-                cp_async_part((to ^ ((r0 & 7) << 4)) + r0 * ROW, at, bytes);
-                at += STEP * s_slot;
+                for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
+                    cp_async_part((to ^ ((r0 & 7) << 4)) + r0 * ROW, at, bytes);
+                    at += STEP * s_slot;
+                }
             }
         }
     }
-    // start the copies of a tile; rows without a token are zeros
-    __device__ __forceinline__ void copy_tensor(unsigned dst, const T *base, int64_t s_page, int64_t s_slot, int64_t s_d,
-                                                int dim, bool vec, int32_t page, int32_t row) const
+    // start the copies of any tile; rows without a token (bit clear in `mask`) are zeros
+    __device__ __forceinline__ void copy_rows(unsigned dst, const T *base, int64_t s_page, int64_t s_slot, int64_t s_d,
+                                              int dim, bool vec, int32_t page, int32_t row, uint32_t mask) const
     {
-        constexpr int CHUNKS = ROW / 16, PER = 16 / int(sizeof(T));
+        const int64_t offset = page < 0 ? 0 : page * s_page + row * s_slot;      // of row lane % 16
         if (vec) {
-            constexpr int STEP = CHUNKS >= 32 ? 1 : 32 / CHUNKS;      // rows a warp's copy instruction covers
-            constexpr int COLS = CHUNKS >= 32 ? CHUNKS / 32 : 1;
-            const int sub = CHUNKS >= 32 ? 0 : lane / CHUNKS;
-#pragma unroll
+            const int sub = my_sub();
+#pragma unroll 4
             for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
-                const int r = r0 + sub;
-                const int32_t pg = __shfl_sync(0xffffffffu, page, r), rw = __shfl_sync(0xffffffffu, row, r);
-                const T *src = base + (pg < 0 ? 0 : pg * s_page + rw * s_slot);
+                const int r = r0 + (idle() ? 0 : sub);
+                const T *src = base + __shfl_sync(0xffffffffu, offset, r);
+                const bool there = (mask >> r) & 1;
 #pragma unroll
                 for (int c0 = 0; c0 < COLS; ++c0) {
-                    const int chunk = CHUNKS >= 32 ? lane + 32 * c0 : lane % CHUNKS;
-                    const int left = (dim - chunk * PER) * int(sizeof(T));
-                    const int bytes = pg < 0 || left <= 0 ? 0 : (left < 16 ? left : 16);
-                    cp_async_part(dst + swizzled(r, chunk), bytes ? src + chunk * PER : base, bytes);
+                    const int chunk = my_chunk() + 32 * c0;
+                    const int bytes = there ? chunk_bytes(chunk, dim) : 0;
+                    if (!idle()) cp_async_part(dst + swizzled(r, chunk), bytes ? src + chunk * PER : base, bytes);
                 }
             }
         } else {
 #pragma unroll 1
             for (int r = 0; r < kAttnTok; ++r) {
-                const int32_t pg = __shfl_sync(0xffffffffu, page, r), rw = __shfl_sync(0xffffffffu, row, r);
-                const T *src = base + (pg < 0 ? 0 : pg * s_page + rw * s_slot);
+                const T *src = base + __shfl_sync(0xffffffffu, offset, r);
+                const bool there = (mask >> r) & 1;
+#pragma unroll 1
                 for (int d = lane; d < DP; d += 32) {
                     T x = from_f32<T>(0.f);
-                    if (pg >= 0 && d < dim) x = src[d * s_d];
+                    if (there && d < dim) x = src[d * s_d];
                     const unsigned at = dst + swizzled(r, d / PER) + unsigned(d % PER) * unsigned(sizeof(T));
                     if constexpr (F32) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
                     else asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(*reinterpret_cast<const unsigned short *>(&x)) : "memory");
@@ -258,8 +274,8 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             copy_whole(dst + kAttnTok * ROW, v + page * p.v_page + first * p.v_slot, p.v_slot, p.dim_v);
             return;
         }
-        copy_tensor(dst, k, p.k_page, p.k_slot, p.k_d, p.dim_k, p.vec_k, page, row);
-        copy_tensor(dst + kAttnTok * ROW, v, p.v_page, p.v_slot, p.v_d, p.dim_v, p.vec_v, page, row);
+        copy_rows(dst, k, p.k_page, p.k_slot, p.k_d, p.dim_k, p.vec_k, page, row, mask);
+        copy_rows(dst + kAttnTok * ROW, v, p.v_page, p.v_slot, p.v_d, p.dim_v, p.vec_v, page, row, mask);
     }
 
     __device__ __forceinline__ int first_head(const AttentionCursor &c, int &count) const
@@ -333,29 +349,41 @@ template <typename T, int DP, int NT> struct AttentionWarp {
     __device__ __forceinline__ void tile(const AttentionCursor &cur, int stage, uint32_t seen)
     {
         const unsigned ks_base = ring + unsigned(stage) * Shape::STAGE, vs_base = ks_base + kAttnTok * ROW;
-        float s[NT][4];
+        // the products of even and odd steps (fp32: the three kinds of partial products) go to accumulators of their
+        // own: one chain of dependent MMAs would cost more time than everything else in a tile
+        constexpr int CHAINS = F32 ? 3 : 2;
+        float s[NT][4], part[NT][CHAINS][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
+            for (int i = 0; i < CHAINS; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) part[nt][i][j] = 0.f;
         {
-            // rows are ROW bytes on a ring aligned to them: stepping to the next pair of chunks flips address bits
+            // the next pair of chunks flips address bits 5 and 6, the next 128 bytes of the row are a step
             const unsigned at = ks_base + swizzled(((lane >> 3) & 1) * 8 + (lane & 7), lane >> 4);
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) {
                 uint32_t a[4];
-                ldsm4(a, at ^ (ks << 5));
+                ldsm4(a, (at ^ ((ks & 3) << 5)) + (ks >> 2) * 128);
                 if constexpr (F32) {
                     uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) split_tf32(a[j], hi[j], lo[j]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma8_split(s[nt], hi, lo, q[nt][ks][0], q[nt][ks][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma8_split(part[nt][0], part[nt][1], part[nt][2], hi, lo, q[nt][ks][0], q[nt][ks][1]);
                 } else {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma16(s[nt], a, q[nt][ks][0], q[nt][ks][1], T());
+                    for (int nt = 0; nt < NT; ++nt) mma16(part[nt][ks & 1], a, q[nt][ks][0], q[nt][ks][1], T());
                 }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[nt][j] = part[nt][1][j] + part[nt][0][j];
+                    if constexpr (F32) s[nt][j] += part[nt][2][j];
+                }
         }
         if constexpr (F32) {
             bool odd = false;
@@ -432,7 +460,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                         split_tf32(x, hi[j], lo[j]);
                     }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma8_split(o[mt][nt], hi, lo, b[nt][ks][0], b[nt][ks][1]);
+                    for (int nt = 0; nt < NT; ++nt) mma8_split(o[mt][nt], o[mt][nt], o[mt][nt], hi, lo, b[nt][ks][0], b[nt][ks][1]);
                 }
         } else {
             uint32_t hi[NT][2], lo[NT][2];
@@ -449,7 +477,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 uint32_t a[4];
-                ldsm4_trans(a, at ^ (mt << 5));
+                ldsm4_trans(a, (at ^ ((mt & 3) << 5)) + (mt >> 2) * 128);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma16(o[mt][nt], a, hi[nt][0], hi[nt][1], T());
@@ -519,17 +547,21 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 // what a part with maximum m counts in a whole with maximum top >= m (a part that saw nothing has m = -inf and o = l = 0)
 __device__ __forceinline__ float join_weight(float m, float top) { return m == top ? 1.f : exp2f(m - top); }
 
-// element d of head h of an item (8 NT = `per` heads) from its joined sums
+// elements d..d+3 of head h of an item (8 NT = `per` heads) from its joined sums
 template <typename T>
-__device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t item, int per, int h, int d, float o, float m, float l)
+__device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t item, int per, int h, int d, const float4 &o, float m, float l)
 {
     const int head_blocks = p.key_heads * p.blocks;
     const int seq = item / head_blocks, hb = item - seq * head_blocks;
     const int kh = hb / p.blocks, in_group = (hb - kh * p.blocks) * per + h;
     if (in_group >= p.group) return;
     const int head = kh * p.group + in_group;
-    if (d < p.dim_v)
-        static_cast<T *>(p.o)[seq * p.o_n + int64_t(head) * p.o_h + d * p.o_d] = from_f32<T>(l == 0.f ? 0.f : o / l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *dst = static_cast<T *>(p.o) + seq * p.o_n + int64_t(head) * p.o_h;
+    const float v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (d + j < p.dim_v) dst[(d + j) * p.o_d] = from_f32<T>(l == 0.f ? 0.f : v[j] * inv);
     if (d == 0 && p.lse)
         p.lse[int64_t(seq) * p.heads + head] = l == 0.f ? -INFINITY : (m - AttentionBias<T>::value + log2f(l)) * 0.6931471805599453f;
 }
@@ -644,30 +676,30 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         int32_t row, page = w.look_up(ahead, row);
         // tokens that count: seen[k] belongs to the tile k steps ahead of the one being consumed
         uint32_t seen[STAGES];
-        auto issue = [&](int stage, uint32_t &mask) {
-            mask = 0;
+#pragma unroll
+        for (int k = 0; k < STAGES; ++k) seen[k] = 0;
+        w.begin_item(cur);
+        bool began_here = cur.tile == 0;                        // the current item's first tile is in this warp's range
+        int stage = 0, into = 0;
+        // one step: start the copies of tile i + STAGES - 1, consume tile i (the first STAGES - 1 steps only copy)
+        for (int64_t i = 1 - STAGES; i < n; ++i) {
+            cp_async_wait_group<STAGES - 2>();
+            __syncwarp();                                       // every lane's copies have landed, the oldest stage is free
+#pragma unroll
+            for (int k = 0; k + 1 < STAGES; ++k) seen[k] = seen[k + 1];
+            seen[STAGES - 1] = 0;
             if (issued < n) {
-                mask = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
-                w.copy_tile(ahead, stage, page, row, mask);
+                seen[STAGES - 1] = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
+                w.copy_tile(ahead, into, page, row, seen[STAGES - 1]);
+                if (++into == STAGES) into = 0;
                 if (++issued < n) {
                     ahead.next(p);
                     page = w.look_up(ahead, row);
                 }
             }
             cp_async_commit();
-        };
-#pragma unroll
-        for (int k = 0; k < STAGES - 1; ++k) issue(k, seen[k]);
-        w.begin_item(cur);
-        bool began_here = cur.tile == 0;                        // the current item's first tile is in this warp's range
-        int stage = 0;
-        for (int64_t i = 0; i < n; ++i) {
-            cp_async_wait_group<STAGES - 2>();
-            __syncwarp();                                       // every lane's copies have landed, the oldest stage is free
-            issue(stage == 0 ? STAGES - 1 : stage - 1, seen[STAGES - 1]);
+            if (i < 0) continue;
             w.tile(cur, stage, seen[0]);
-#pragma unroll
-            for (int k = 0; k + 1 < STAGES; ++k) seen[k] = seen[k + 1];
             if (++stage == STAGES) stage = 0;
             const bool item_ends = cur.tile + 1 == cur.span.tiles;
             if (item_ends || i + 1 == n) {
@@ -701,93 +733,128 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
 
     float (*joined)[2 * H] = reinterpret_cast<float (*)[2 * H]>(smem + Shape::DEPOSIT);     // behind warp 0's deposit in its ring
     float (*weight)[H] = reinterpret_cast<float (*)[H]>(smem + Shape::DEPOSIT + 2 * W * 2 * H * 4);
-    // join what the warps left: first each deposit's weight against the largest maximum of its item ...
-    const int64_t slot_floats = H * DP + 2 * H;
+    // join what the warps left: first each deposit's weight against the largest maximum of its item (a warp takes a
+    // head, a lane a deposit; the deposits of an item are neighbours) ...
     if (tid < 2) p.partial_item[2 * blockIdx.x + tid] = tid == 0 ? first_item : (last_item == first_item ? -1 : last_item);
     if (blockIdx.x >= ctas) return;
-    for (int e = tid; e < 2 * W * H; e += THREADS) {
-        const int i = e / H, h = e - i * H;
-        const int32_t item = dep_item[i];
-        if (item < 0) continue;
-        float top = -INFINITY, sum = 0.f;
-        for (int j = 0; j < 2 * W; ++j)
-            if (dep_item[j] == item) top = fmaxf(top, stats[j][h]);
-        for (int j = 0; j < 2 * W; ++j)
-            if (dep_item[j] == item) sum += stats[j][H + h] * join_weight(stats[j][h], top);
-        weight[i][h] = join_weight(stats[i][h], top);
-        joined[i][h] = top;
-        joined[i][H + h] = sum;
+    for (int h = warp; h < H; h += W) {
+        const bool mine = lane < 2 * W && dep_item[lane < 2 * W ? lane : 0] >= 0;
+        const int32_t item = mine ? dep_item[lane] : -1 - lane;
+        const float m = mine ? stats[lane][h] : -INFINITY, l = mine ? stats[lane][H + h] : 0.f;
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < 2 * W; ++j) {
+            const float x = __shfl_sync(0xffffffffu, m, j);
+            if (__shfl_sync(0xffffffffu, item, j) == item) top = fmaxf(top, x);
+        }
+        const float share = join_weight(m, top);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2 * W; ++j) {
+            const float x = __shfl_sync(0xffffffffu, l * share, j);
+            if (__shfl_sync(0xffffffffu, item, j) == item) sum += x;
+        }
+        if (mine) {
+            weight[lane][h] = share;
+            joined[lane][h] = top;
+            joined[lane][H + h] = sum;
+        }
     }
     __syncthreads();
-    // ... then the sums, an element (head, head element) per thread
-    for (int e = tid; e < H * DP; e += THREADS) {
+    // ... then the sums, four elements of a head per thread
+    for (int e = 4 * tid; e < H * DP; e += 4 * THREADS) {
         const int h = e / DP, d = e - h * DP;
-        int i = 0;
-        while (i < 2 * W) {
-            const int32_t item = dep_item[i];
-            if (item < 0) { ++i; continue; }
-            const float m = joined[i][h], l = joined[i][H + h];
-            float o = 0.f;
-            for (; i < 2 * W && (dep_item[i] == item || dep_item[i] < 0); ++i) {
-                if (dep_item[i] < 0) continue;
-                const float *src = (i & 1) ? reinterpret_cast<const float *>(smem + (i >> 1) * Shape::RING)
-                                           : reinterpret_cast<const float *>(smem + W * Shape::RING) + (i >> 1) * (Shape::DEPOSIT / 4);
-                o = fmaf(src[e], weight[i][h], o);
-            }
+        int32_t item = -1;
+        int last = 0;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto flush = [&]() {
+            if (item < 0) return;
+            const float m = joined[last][h], l = joined[last][H + h];
             if (item == first_item || item == last_item) {
-                float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * slot_floats;
-                out[e] = o;
+                float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * (H * DP + 2 * H);
+                *reinterpret_cast<float4 *>(out + e) = o;
                 if (d == 0) { out[H * DP + h] = m; out[H * DP + H + h] = l; }
             } else {
                 write_joined<T>(p, item, H, h, d, o, m, l);
             }
+        };
+#pragma unroll 1
+        for (int i = 0; i < 2 * W; ++i) {
+            const int32_t here = dep_item[i];
+            if (here < 0) continue;
+            if (here != item) {
+                flush();
+                item = here;
+                o = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            const unsigned char *src = (i & 1) ? smem + (i >> 1) * Shape::RING : smem + W * Shape::RING + (i >> 1) * Shape::DEPOSIT;
+            const float4 x = reinterpret_cast<const float4 *>(src)[e / 4];
+            const float share = weight[i][h];
+            o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
+            last = i;
         }
+        flush();
     }
 }
 
-// Items that span CTAs: block (c, h) joins head h of the item that begins in CTA c's range and ends in a later
-// one's: CTA c's second slot, then the first slots of the CTAs after it while they carry the same item.
-constexpr int kJoinMaxCtas = 1024;
+// Items that span CTAs: block c joins the item that begins in CTA c's range and ends in a later one's: CTA c's
+// second slot, then the first slots of the CTAs after it while they carry the same item.  A thread takes four
+// elements of a head; the threads beyond the elements split the parts among them, so that a long sequence alone
+// (148 parts) is a few rounds of loads.
+constexpr int kJoinMaxCtas = 1024, kJoinThreads = 1024;
 template <typename T, int DP, int NT>
-__global__ void __launch_bounds__(DP) paged_attention_join_kernel(const __grid_constant__ AttentionParams p, int ctas)
+__global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const __grid_constant__ AttentionParams p, int ctas)
 {
-    constexpr int H = 8 * NT;
+    constexpr int H = 8 * NT, QUADS = H * DP / 4, SPLIT = kJoinThreads / QUADS;
     constexpr int64_t slot_floats = H * DP + 2 * H;
+    static_assert(QUADS * SPLIT <= kJoinThreads && SPLIT >= 2, "");
     __shared__ int32_t parts;
-    __shared__ float weight[kJoinMaxCtas], sums[kJoinMaxCtas], tops[DP / 32];
-    const int c = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+    __shared__ float tops[H], totals[H];
+    __shared__ float4 sums[SPLIT - 1][QUADS];
+    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int32_t item = p.partial_item[2 * c + 1];
     if (item < 0) return;
-    if (d == 0) parts = ctas - c;
+    if (tid == 0) parts = ctas - c;
     __syncthreads();
     // part 0 is CTA c's second slot, part i CTA c + i's first; the first CTA without the item ends it
-    float top = -INFINITY;
-    for (int i = d; i < ctas - c; i += DP)
-        if (i > 0 && p.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
+    for (int i = tid + 1; i < ctas - c; i += kJoinThreads)
+        if (p.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
     __syncthreads();
     const int n = parts;
     const float *first = p.partial + 2 * int64_t(c) * slot_floats;
     auto part = [&](int i) { return first + (i == 0 ? slot_floats : 2 * int64_t(i) * slot_floats); };
-    for (int i = d; i < n; i += DP) {
-        weight[i] = part(i)[H * DP + h];
-        sums[i] = part(i)[H * DP + H + h];
-        top = fmaxf(top, weight[i]);
+    // a warp takes a head's maxima and sums
+    for (int h = tid / 32; h < H; h += kJoinThreads / 32) {
+        float top = -INFINITY;
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, part(i)[H * DP + h]);
+        for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        float l = 0.f;
+        for (int i = lane; i < n; i += 32) l = fmaf(part(i)[H * DP + H + h], join_weight(part(i)[H * DP + h], top), l);
+        for (int k = 1; k < 32; k <<= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
+        if (lane == 0) { tops[h] = top; totals[h] = l; }
     }
-    for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-    if ((d & 31) == 0) tops[d / 32] = top;
     __syncthreads();
+    const int split = tid / QUADS, quad = tid - split * QUADS, h = quad * 4 / DP, d = quad * 4 - h * DP;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (split < SPLIT) {
+        const float top = tops[h];
+#pragma unroll 4
+        for (int i = split; i < n; i += SPLIT) {
+            const float4 x = *reinterpret_cast<const float4 *>(part(i) + quad * 4);
+            const float share = join_weight(part(i)[H * DP + h], top);
+            o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
+        }
+        if (split > 0) sums[split - 1][quad] = o;
+    }
+    __syncthreads();
+    if (split > 0) return;
 #pragma unroll
-    for (int w = 0; w < DP / 32; ++w) top = fmaxf(top, tops[w]);
-    for (int i = d; i < n; i += DP) weight[i] = join_weight(weight[i], top);
-    __syncthreads();
-    float o = 0.f, l = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-        o = fmaf(part(i)[h * DP + d], weight[i], o);
-        l = fmaf(sums[i], weight[i], l);
+    for (int k = 0; k < SPLIT - 1; ++k) {
+        const float4 x = sums[k][quad];
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
-    write_joined<T>(p, item, H, h, d, o, top, l);
+    write_joined<T>(p, item, H, h, d, o, tops[h], totals[h]);
 }
 
 }  // namespace btc

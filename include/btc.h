@@ -412,6 +412,50 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
                                         const void *V, const int32_t *table, const int32_t *lengths, void *O, float *lse,
                                         void *workspace, size_t workspace_bytes, int32_t *flags);
 
+/* Pages of a key-value cache: allocation, copy on write, forking, freeing, compaction, copies.  The state is the
+ * caller's device memory: a table [N, M] I32 of page numbers (one row per sequence; entry j < ceil(length / S) is a
+ * page, the others are -1), lengths int32[N], and refs int32[P], the number of table entries that name a page (0:
+ * free).  Everything runs on the device in stream order; the host reads nothing.  Results are deterministic: free
+ * pages are taken lowest number first, in the order of the sequences.
+ *
+ * btc_create_pages: `layouts` descriptors (1..4) of cache tensors whose first mode is the page (extent P, the same
+ * in all; any element type, rank and strides, no two elements at one place); the table's descriptor; page_tokens = S.
+ * `tensors` arguments are HOST arrays of `count` DEVICE pointers (a multiple of `layouts`; entry i has layout
+ * i % layouts): typically keys and values of every layer.  count 0: only the state changes.
+ *
+ * extend   sequence n takes new_tokens[n] more tokens (DEVICE int32[N]): missing pages are allocated; a partly filled
+ *          last page that other sequences share (refs > 1 when the call starts) is replaced by a copy, in all
+ *          tensors.  slots (DEVICE int32[N * max_new]) receives page * S + row of each new token, -1 for the rest of a
+ *          row.  A sequence with more than max_new tokens, whose row is too short, or whose length or last page is
+ *          invalid takes no part (BTC_FLAG_BAD_LENGTH, BTC_FLAG_BAD_PAGE); of the others, the first one whose pages do not fit
+ *          and all after it get nothing (BTC_FLAG_POOL_EXHAUSTED).  What gets nothing is left as it was.
+ * fork     row dst[i] becomes a copy of row src[i] (DEVICE int32[count]) and shares its pages.  dst rows must be
+ *          empty (length 0; BTC_FLAG_BAD_SEQUENCE otherwise); no dst may occur twice or as a src of the same call.
+ * free     the listed sequences give up their pages; their rows become -1, their lengths 0.
+ * compact  with L pages in use, the pages numbered L and higher move to the free ones below L, in order; table and
+ *          refs follow, contents are copied in all tensors.  Afterwards pages 0..L-1 are in use.
+ * copy     pairs (DEVICE int32[count * 2]: source, destination): contents of page to page in all tensors; a negative
+ *          number skips the pair.  No destination may occur twice or as a source of the same call.
+ * Workspace (extend, compact): btc_pages_workspace_size.
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED (P * S beyond int32, more than 8 separate dimensions
+ * in a page, pages of 2^31 units), MISALIGNED, WORKSPACE_TOO_SMALL, CUDA. */
+typedef struct btc_pages_s *btc_pages_t;
+btc_error_t btc_create_pages(btc_handle_t handle, int32_t layouts, const btc_tensor_info_t *pages, btc_tensor_info_t table,
+                             int32_t page_tokens, btc_pages_t *out);
+btc_error_t btc_destroy_pages(btc_pages_t *op);
+btc_error_t btc_pages_workspace_size(btc_pages_t op, size_t *bytes);
+btc_error_t btc_pages_extend(btc_pages_t op, void *cuda_stream, const int32_t *new_tokens, int32_t *table, int32_t *lengths,
+                             int32_t *refs, int32_t *slots, int32_t max_new, void *const *tensors, int32_t count,
+                             void *workspace, size_t workspace_bytes, int32_t *flags);
+btc_error_t btc_pages_fork(btc_pages_t op, void *cuda_stream, const int32_t *src, const int32_t *dst, int32_t count,
+                           int32_t *table, int32_t *lengths, int32_t *refs, int32_t *flags);
+btc_error_t btc_pages_free(btc_pages_t op, void *cuda_stream, const int32_t *sequences, int32_t count, int32_t *table,
+                           int32_t *lengths, int32_t *refs, int32_t *flags);
+btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table, int32_t *refs, void *const *tensors,
+                              int32_t count, void *workspace, size_t workspace_bytes, int32_t *flags);
+btc_error_t btc_pages_copy(btc_pages_t op, void *cuda_stream, const int32_t *pairs, int32_t pair_count,
+                           void *const *tensors, int32_t count, int32_t *flags);
+
 /* Peak micro-benchmarks (no counterpart in the paper; the paper leaves benchmarks to future work, Sec.
  * "Outlook").  Measures what this device sustains with a kernel that does nothing else, so that the
  * roofline fraction of a contraction can be quoted against a figure taken on the same device in the

@@ -62,6 +62,8 @@ EXPORTED = [
     "btc_create_rotary", "btc_destroy_rotary", "btc_rotary_workspace_size", "btc_rotary_execute", "btc_rotary_backward",
     "btc_create_paged_attention", "btc_destroy_paged_attention", "btc_paged_attention_workspace_size",
     "btc_paged_attention_execute",
+    "btc_create_pages", "btc_destroy_pages", "btc_pages_workspace_size", "btc_pages_extend", "btc_pages_fork",
+    "btc_pages_free", "btc_pages_compact", "btc_pages_copy",
 ]
 
 _vp = ctypes.c_void_p
@@ -104,6 +106,15 @@ _lib.btc_create_paged_attention.argtypes = [_vp] * 6 + [ctypes.c_double, ctypes.
 _lib.btc_destroy_paged_attention.argtypes = [ctypes.POINTER(_vp)]
 _lib.btc_paged_attention_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.btc_paged_attention_execute.argtypes = [_vp] * 10 + [ctypes.c_size_t, _vp]
+_i32 = ctypes.c_int32
+_lib.btc_create_pages.argtypes = [_vp, _i32, ctypes.POINTER(_vp), _vp, _i32, ctypes.POINTER(_vp)]
+_lib.btc_destroy_pages.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_pages_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_pages_extend.argtypes = [_vp] * 7 + [_i32, _vp, _i32, _vp, ctypes.c_size_t, _vp]
+_lib.btc_pages_fork.argtypes = [_vp] * 4 + [_i32] + [_vp] * 4
+_lib.btc_pages_free.argtypes = [_vp] * 3 + [_i32] + [_vp] * 4
+_lib.btc_pages_compact.argtypes = [_vp] * 5 + [_i32, _vp, ctypes.c_size_t, _vp]
+_lib.btc_pages_copy.argtypes = [_vp] * 3 + [_i32, _vp, _i32, _vp]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -520,6 +531,55 @@ class PagedAttention(_Operation):
                                               workspace_bytes, flags)
         if rc:
             raise BtcError(rc, "btc_paged_attention_execute")
+
+
+class Pages(_Operation):
+    """Pages of a key-value cache: extend, fork, free, compact, copy; see btc_create_pages.
+
+    pages: the TensorInfo of the cache tensors [P, ...], or a list of them when they differ (entry i of a `tensors`
+    list then has layout i % len(pages)).  table: TensorInfo [N, M] int32.  All data arguments are device pointers as
+    integers, `tensors` a list of them."""
+
+    _kind = "pages"
+
+    def __init__(self, handle: Handle, pages, table: TensorInfo, page_tokens: int):
+        self._op = _vp()
+        layouts = list(pages) if isinstance(pages, (list, tuple)) else [pages]
+        arr = (_vp * max(len(layouts), 1))(*[t._t for t in layouts])
+        _check(_lib.btc_create_pages(handle._h, len(layouts), arr, table._t, page_tokens, ctypes.byref(self._op)), "btc_create_pages")
+
+    @staticmethod
+    def _pointers(tensors):
+        return (_vp * len(tensors))(*tensors) if tensors else None
+
+    def extend(self, stream: int, new_tokens: int, table: int, lengths: int, refs: int, slots: int, max_new: int,
+               tensors: Sequence[int] = (), workspace: int = 0, workspace_bytes: int = 0, flags: int = 0) -> None:
+        rc = _lib.btc_pages_extend(self._op, stream, new_tokens, table, lengths, refs, slots, max_new, self._pointers(tensors),
+                                   len(tensors), workspace, workspace_bytes, flags)
+        if rc:
+            raise BtcError(rc, "btc_pages_extend")
+
+    def fork(self, stream: int, src: int, dst: int, count: int, table: int, lengths: int, refs: int, flags: int = 0) -> None:
+        rc = _lib.btc_pages_fork(self._op, stream, src, dst, count, table, lengths, refs, flags)
+        if rc:
+            raise BtcError(rc, "btc_pages_fork")
+
+    def free(self, stream: int, sequences: int, count: int, table: int, lengths: int, refs: int, flags: int = 0) -> None:
+        rc = _lib.btc_pages_free(self._op, stream, sequences, count, table, lengths, refs, flags)
+        if rc:
+            raise BtcError(rc, "btc_pages_free")
+
+    def compact(self, stream: int, table: int, refs: int, tensors: Sequence[int] = (), workspace: int = 0,
+                workspace_bytes: int = 0, flags: int = 0) -> None:
+        rc = _lib.btc_pages_compact(self._op, stream, table, refs, self._pointers(tensors), len(tensors), workspace,
+                                    workspace_bytes, flags)
+        if rc:
+            raise BtcError(rc, "btc_pages_compact")
+
+    def copy(self, stream: int, pairs: int, count: int, tensors: Sequence[int], flags: int = 0) -> None:
+        rc = _lib.btc_pages_copy(self._op, stream, pairs, count, self._pointers(tensors), len(tensors), flags)
+        if rc:
+            raise BtcError(rc, "btc_pages_copy")
 
 
 def elementwise(handle: Handle, A, labelsA, B, C, labelsC, alpha=1.0, beta=0.0, conjA=False, conjB=False, stream: int = 0):

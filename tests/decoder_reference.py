@@ -85,3 +85,82 @@ def attention_bounds(o, lse, size, moduli, top, count, dim, dtype):
     rel = 2 * score + split + chain
     return (UNIT[dtype] * o.abs() + rel[..., None].double() * size + FLOOR[dtype] + 1e-300,
             score.double() + 4 * E32 * lse.abs().nan_to_num(0, 0, 0) + chain.double())
+
+
+class PagesState:
+    """The bookkeeping of cache pages, one step at a time (plain Python)."""
+
+    def __init__(self, table, lengths, refs, page_tokens):
+        self.table = [list(map(int, r)) for r in table]
+        self.lengths, self.refs, self.S = list(map(int, lengths)), list(map(int, refs)), page_tokens
+        self.columns, self.P = len(self.table[0]), len(self.refs)
+
+    def free(self, sequences):
+        for s in sequences:
+            if not 0 <= s < len(self.table):
+                continue
+            for j, p in enumerate(self.table[s]):
+                if 0 <= p < self.P:
+                    self.refs[p] -= 1
+                self.table[s][j] = -1
+            self.lengths[s] = 0
+
+    def fork(self, src, dst):
+        for a, b in zip(src, dst):
+            if not (0 <= a < len(self.table) and 0 <= b < len(self.table)) or a == b or self.lengths[b] != 0:
+                continue
+            self.table[b], self.lengths[b] = list(self.table[a]), self.lengths[a]
+            for p in self.table[a]:
+                if p >= 0:
+                    self.refs[p] += 1
+
+    def extend(self, new, most):
+        """Returns (slots, copies)."""
+        S, room = self.S, self.columns * self.S
+        empty = [p for p in range(self.P) if self.refs[p] == 0]
+        refs_before = list(self.refs)
+        slots, copies, at, stopped = [], [], 0, False
+        for s, add in enumerate(new):
+            length = self.lengths[s]
+            row = [-1] * most
+            slots.append(row)
+            if add <= 0 or length < 0 or add > most or length + add > room:
+                continue
+            held = -(-length // S)
+            partial = length % S != 0
+            last = self.table[s][held - 1] if partial else -1
+            if partial and not 0 <= last < self.P:
+                continue
+            copy = partial and refs_before[last] > 1
+            need = -(-(length + add) // S) - held + int(copy)
+            if stopped or at + need > len(empty):
+                stopped = True
+                continue
+            if copy:
+                fresh = empty[at]
+                at += 1
+                copies.append((last, fresh))
+                self.refs[last] -= 1
+                self.refs[fresh] = 1
+                self.table[s][held - 1] = fresh
+            for j in range(held, -(-(length + add) // S)):
+                self.table[s][j] = empty[at]
+                self.refs[empty[at]] = 1
+                at += 1
+            for i in range(add):
+                t = length + i
+                row[i] = self.table[s][t // S] * S + t % S
+            self.lengths[s] = length + add
+        return slots, copies
+
+    def compact(self):
+        live = sum(r > 0 for r in self.refs)
+        holes = [p for p in range(live) if self.refs[p] <= 0]
+        late = [p for p in range(live, self.P) if self.refs[p] > 0]
+        to = dict(zip(late, holes))
+        for row in self.table:
+            for j, p in enumerate(row):
+                row[j] = to.get(p, p)
+        for a, b in to.items():
+            self.refs[b], self.refs[a] = self.refs[a], 0
+        return list(to.items())

@@ -132,3 +132,44 @@ def test_paged_attention_refusals(api, handle):
     assert run(256, 256, 256, 256, 256, 256, workspace=128, workspace_bytes=n) == E.ERR_MISALIGNED
     assert run(257, 256, 256, 256, 256, 256, workspace=256, workspace_bytes=n) == E.ERR_MISALIGNED
     assert run(256, 256, 256, 258, 256, 256, workspace=256, workspace_bytes=n) == E.ERR_MISALIGNED
+
+
+def test_pages_refusals(api, handle):
+    E = api
+    t = lambda *s, dt=api.BF16, st=None: dense(api, handle, dt, *s, strides=st)  # noqa: E731
+    tab = dense(api, handle, api.I32, 3, 5)
+    make = lambda *a: code(api, lambda: api.Pages(handle, *a))  # noqa: E731
+    op = api.Pages(handle, [t(9, 16, 2, 64), t(9, 16, 2, 32, dt=E.F64)], tab, 16)
+    n = op.workspace_size()
+    assert n > 0
+    assert make([], tab, 16) == E.ERR_INVALID_ARGUMENT
+    assert make([t(9, 4)] * 5, tab, 16) == E.ERR_INVALID_ARGUMENT
+    assert make(t(9, 4), tab, 0) == E.ERR_INVALID_ARGUMENT
+    assert make(t(), tab, 16) == E.ERR_INVALID_ARGUMENT
+    assert make(t(9, 4), t(3, 5), 16) == E.ERR_NOT_SUPPORTED
+    assert make(t(9, 4), dense(api, handle, api.I32, 3, 5, 2), 16) == E.ERR_INVALID_ARGUMENT
+    assert make([t(9, 4), t(8, 4)], tab, 16) == E.ERR_EXTENT_MISMATCH
+    assert make(t(9, 4, st=(4, 0)), tab, 16) == E.ERR_D_ALIASING
+    assert make(t(9, 4), dense(api, handle, api.I32, 3, 5, strides=(0, 1)), 16) == E.ERR_D_ALIASING
+    assert make(t(1 << 28, 4), tab, 16) == E.ERR_NOT_SUPPORTED
+    assert make(t(2, 1 << 16, 1 << 16), tab, 16) == E.ERR_NOT_SUPPORTED
+    many = (3, 2, 2, 2, 2, 2, 2, 2, 2, 2)
+    assert make(t(*many, st=[3 ** 10] + [3 ** i for i in range(9)]), tab, 16) == E.ERR_NOT_SUPPORTED
+    ok = dict(workspace=256, workspace_bytes=n)
+    ext = lambda *a, **k: code(api, lambda: op.extend(0, *a, **k))  # noqa: E731
+    assert ext(0, 256, 256, 256, 256, 1, [256, 256], **ok) == E.ERR_INVALID_ARGUMENT
+    assert ext(256, 256, 256, 256, 256, 0, [256, 256], **ok) == E.ERR_INVALID_ARGUMENT
+    assert ext(256, 256, 256, 256, 256, 1, [256], **ok) == E.ERR_INVALID_ARGUMENT           # two layouts, one tensor
+    assert ext(256, 256, 256, 256, 256, 1, [256, 0], **ok) == E.ERR_INVALID_ARGUMENT
+    assert ext(256, 256, 256, 256, 256, 1, [257, 256], **ok) == E.ERR_MISALIGNED
+    assert ext(256, 256, 256, 256, 256, 1, [256, 256]) == E.ERR_WORKSPACE_TOO_SMALL
+    assert ext(256, 256, 256, 256, 256, 1, [256, 256], workspace=128, workspace_bytes=n) == E.ERR_MISALIGNED
+    assert ext(256, 258, 256, 256, 256, 1, [256, 256], **ok) == E.ERR_MISALIGNED
+    assert code(api, lambda: op.compact(0, 256, 0, [256, 256], **ok)) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.compact(0, 256, 256, [256, 256])) == E.ERR_WORKSPACE_TOO_SMALL
+    assert code(api, lambda: op.fork(0, 0, 256, 1, 256, 256, 256)) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.fork(0, 256, 256, -1, 256, 256, 256)) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.free(0, 0, 1, 256, 256, 256)) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.free(0, 256, 1, 256, 0, 256)) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.copy(0, 0, 1, [256, 256])) == E.ERR_INVALID_ARGUMENT
+    assert code(api, lambda: op.copy(0, 256, 1, [256, 256, 256])) == E.ERR_INVALID_ARGUMENT

@@ -17,29 +17,21 @@ template <> __device__ __forceinline__ float from_f32<float>(float x) { return x
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// a 16-byte vector as fp32 values and back (one rounding to nearest even per value)
-__device__ __forceinline__ void unpack16(const uint4 &r, float (&v)[4], float)
+// Vectors of 16 or 8 bytes as fp32 values and back (one rounding to nearest even per value).
+template <int BYTES> struct VectorOf;
+template <> struct VectorOf<16> { typedef uint4 type; };
+template <> struct VectorOf<8> { typedef uint2 type; };
+
+__device__ __forceinline__ void unpack_word(uint32_t w, float &lo, float &hi, __half)
 {
-    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    lo = f.x;
+    hi = f.y;
 }
-__device__ __forceinline__ void unpack16(const uint4 &r, float (&v)[8], __half)
+__device__ __forceinline__ void unpack_word(uint32_t w, float &lo, float &hi, __nv_bfloat16)
 {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-    }
-}
-__device__ __forceinline__ void unpack16(const uint4 &r, float (&v)[8], __nv_bfloat16)
-{
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
 }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half)
 {
@@ -51,14 +43,46 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16)
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-__device__ __forceinline__ uint4 pack16(const float (&v)[4], float)
+template <typename T, int V> __device__ __forceinline__ void unpack_vector(const typename VectorOf<V * int(sizeof(T))>::type &r, float (&v)[V])
 {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    constexpr int WORDS = V * int(sizeof(T)) / 4;
+    uint32_t w[WORDS];
+    w[0] = r.x; w[1] = r.y;
+    if constexpr (WORDS == 4) { w[2] = r.z; w[3] = r.w; }
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(w[i]);
+        else unpack_word(w[i], v[2 * i], v[2 * i + 1], T());
+    }
 }
-template <typename T> __device__ __forceinline__ uint4 pack16(const float (&v)[8], T)
+template <typename T, int V> __device__ __forceinline__ typename VectorOf<V * int(sizeof(T))>::type pack_vector(const float (&v)[V])
 {
-    return make_uint4(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()), pack2(v[4], v[5], T()), pack2(v[6], v[7], T()));
+    constexpr int WORDS = V * int(sizeof(T)) / 4;
+    uint32_t w[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+        else w[i] = pack2(v[2 * i], v[2 * i + 1], T());
+    }
+    if constexpr (WORDS == 4) return make_uint4(w[0], w[1], w[2], w[3]);
+    else return make_uint2(w[0], w[1]);
 }
+
+// Two fp32 operations in one instruction, each half rounded like its scalar form.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)),
+        "l"(*reinterpret_cast<const uint64_t *>(&c)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
+    return *reinterpret_cast<const float2 *>(&r);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31 without a divide: q = (n * mul) >> shift in 64 bits, with
 // shift = 31 + ceil(log2 d) and mul = ceil(2^shift / d) <= 2^32 - 1 (exact because mul * d - 2^shift < d)

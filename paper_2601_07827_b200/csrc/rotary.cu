@@ -23,34 +23,41 @@ struct btc_rotary_s {
 
 namespace {
 
-constexpr int kBackwardCtasPerSm = 4;
+constexpr int kBackwardCtasPerSm = 2;   // what the registers allow to run at once
 
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : 2; }
 
-// The vector kernels need: pairs and the unrotated rest in whole vectors per lane, heads contiguous, every other
-// stride a multiple of 16 bytes.  (Base addresses are looked at when a call is made.)
-bool strides_allow_vectors(const btc_rotary_s &op)
+// Do vectors of v elements fit: pairs and the unrotated rest in whole vectors per lane, at most 32 lanes to a head,
+// heads contiguous, every other stride a multiple of the vector.  (Base addresses are looked at when a call is made.)
+bool strides_allow_vectors(const btc_rotary_s &op, int64_t v)
 {
-    const int64_t v = int64_t(16 / esize(op.dtype));
     for (int i = 0; i < 3; ++i) {
         if (!op.has[i]) continue;
         const int64_t dim = op.x[i].extent[2], pairs = i < 2 ? op.pairs : 0;
-        if (pairs % v != 0 || (dim - 2 * pairs) % (2 * v) != 0) return false;
+        if (pairs % v != 0 || (dim - 2 * pairs) % (2 * v) != 0 || dim > 64 * v) return false;
         for (const TensorDesc *t : {&op.x[i], &op.y[i]}) {
             const size_t r = t->extent.size();
             if (t->stride[r - 1] != 1) return false;
             for (size_t k = 0; k + 1 < r; ++k)
-                if (t->stride[k] % v != 0) return false;
+                if (t->extent[k] > 1 && t->stride[k] % v != 0) return false;
         }
     }
     return true;
 }
 
-int lanes_log2_for(const btc_rotary_s &op, bool vector)
+// bytes per access of a call whose addresses are multiples of `aligned`: 16, 8, or 0 for single elements
+int vector_bytes(const btc_rotary_s &op, uintptr_t addresses)
 {
-    if (!vector) return 5;
+    for (int bytes = 16; bytes >= 8; bytes /= 2)
+        if (addresses % uintptr_t(bytes) == 0 && strides_allow_vectors(op, int64_t(bytes / int(esize(op.dtype))))) return bytes;
+    return 0;
+}
+
+int lanes_log2_for(const btc_rotary_s &op, int bytes)
+{
+    if (bytes == 0) return 5;
     int64_t most = 1;
-    const int64_t v = int64_t(16 / esize(op.dtype));
+    const int64_t v = bytes / int64_t(esize(op.dtype));
     for (int i = 0; i < 3; ++i)
         if (op.has[i]) most = std::max(most, op.x[i].extent[2] / (2 * v));
     int k = 0;
@@ -58,20 +65,18 @@ int lanes_log2_for(const btc_rotary_s &op, bool vector)
     return k;
 }
 
-// Heads per unit: as many as 8 (the angles are then computed once for eight heads) while the units still give
-// every SM 1024 threads; few tokens are spread one head to a group instead, because then only latency counts.
-int heads_per_unit(const btc_rotary_s &op, int lanes_log2, int parts)
+// Tokens a CTA takes at a time: so many that a group of lanes has `items` heads to do (the angles, the barrier and the
+// address work are then spread over them) as long as that leaves `ctas` CTAs; few tokens go one to a CTA,
+// because then only latency counts.
+int tokens_per_cta(int64_t tokens, int64_t heads, int lanes_log2, int items, int64_t ctas)
 {
-    for (int hu = 8; hu > 1; hu /= 2) {
-        int64_t units = 0;
-        for (int i = 0; i < parts; ++i)
-            if (op.has[i]) units += (op.x[i].extent[1] + hu - 1) / hu;
-        if ((op.tokens * units) << lanes_log2 >= int64_t(op.handle.sm_count) * 1024) return hu;
-    }
-    return 1;
+    const int64_t groups = kRotaryThreads >> lanes_log2;
+    int64_t n = std::min<int64_t>(kRotaryMaxTokens, std::max<int64_t>(1, items * groups / heads));
+    while (n > 1 && (tokens + n - 1) / n < ctas) n = (n + 1) / 2;
+    return int(n);
 }
 
-void fill_part(const btc_rotary_s &op, int i, int hu, RotaryPart &p)
+void fill_part(const btc_rotary_s &op, int i, RotaryPart &p)
 {
     const TensorDesc &x = op.x[i], &y = op.y[i];
     p.x_t = x.stride[0]; p.x_h = x.stride[1]; p.x_d = x.stride[2];
@@ -84,27 +89,28 @@ void fill_part(const btc_rotary_s &op, int i, int hu, RotaryPart &p)
     p.pairs = i < 2 ? op.pairs : 0;
     p.rest_pairs = (p.dim - 2 * p.pairs + 1) / 2;
     p.copy = i == 2;
-    p.units = (p.heads + hu - 1) / hu;
+    p.inv_dim = 1.f / float(p.dim);
+    p.head.set(p.heads);
 }
 
-template <typename T, bool VECTOR>
+template <typename T, int V>
 void launch_forward(const RotaryParams &p, bool interleaved, unsigned blocks, cudaStream_t st)
 {
-    if (interleaved) rotary_forward_kernel<T, VECTOR, true><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else rotary_forward_kernel<T, VECTOR, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    if (interleaved) rotary_forward_kernel<T, V, true><<<blocks, kRotaryThreads, 0, st>>>(p);
+    else rotary_forward_kernel<T, V, false><<<blocks, kRotaryThreads, 0, st>>>(p);
 }
-template <typename T, bool VECTOR>
+template <typename T, int V>
 void launch_backward(const RotaryParams &p, bool interleaved, unsigned blocks, cudaStream_t st)
 {
-    if (interleaved) rotary_backward_kernel<T, VECTOR, true><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else rotary_backward_kernel<T, VECTOR, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    if (interleaved) rotary_backward_kernel<T, V, true><<<blocks, kRotaryThreads, 0, st>>>(p);
+    else rotary_backward_kernel<T, V, false><<<blocks, kRotaryThreads, 0, st>>>(p);
 }
 
-#define BTC_ROTARY_DISPATCH(F, dtype, vector, ...)                                  \
-    do {                                                                            \
-        if ((dtype) == BTC_F32) (vector) ? F<float, true>(__VA_ARGS__) : F<float, false>(__VA_ARGS__);                  \
-        else if ((dtype) == BTC_F16) (vector) ? F<__half, true>(__VA_ARGS__) : F<__half, false>(__VA_ARGS__);           \
-        else (vector) ? F<__nv_bfloat16, true>(__VA_ARGS__) : F<__nv_bfloat16, false>(__VA_ARGS__);                     \
+#define BTC_ROTARY_DISPATCH(F, dtype, bytes, ...)                                                                        \
+    do {                                                                                                                 \
+        if ((dtype) == BTC_F32) (bytes) == 16 ? F<float, 4>(__VA_ARGS__) : (bytes) == 8 ? F<float, 2>(__VA_ARGS__) : F<float, 1>(__VA_ARGS__);                 \
+        else if ((dtype) == BTC_F16) (bytes) == 16 ? F<__half, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__half, 4>(__VA_ARGS__) : F<__half, 1>(__VA_ARGS__);         \
+        else (bytes) == 16 ? F<__nv_bfloat16, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__nv_bfloat16, 4>(__VA_ARGS__) : F<__nv_bfloat16, 1>(__VA_ARGS__);            \
     } while (0)
 
 }  // namespace
@@ -215,7 +221,8 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
     if (!op) return BTC_ERR_INVALID_ARGUMENT;
     const void *X[3] = {Xq, Xk, Xv}, *W[3] = {Wq, Wk, nullptr};
     void *Y[3] = {Yq, Yk, Yv};
-    bool any_paged = false, vector = strides_allow_vectors(*op);
+    bool any_paged = false;
+    uintptr_t addresses = 0;
     const size_t es = esize(op->dtype);
     for (int i = 0; i < 3; ++i) {
         if (!op->has[i]) {
@@ -226,7 +233,7 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
         if (!X[i] || !Y[i] || (W[i] && !op->norm)) return BTC_ERR_INVALID_ARGUMENT;
         for (const void *q : {X[i], static_cast<const void *>(Y[i]), W[i]}) {
             if (!aligned_to(q, es)) return BTC_ERR_MISALIGNED;
-            vector = vector && aligned_to(q, 16);
+            addresses |= reinterpret_cast<uintptr_t>(q);
         }
     }
     if ((op->pairs > 0 && !positions) || (any_paged && !slots)) return BTC_ERR_INVALID_ARGUMENT;
@@ -235,24 +242,29 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
 
     RotaryParams p;
     std::memset(static_cast<void *>(&p), 0, sizeof p);
-    p.lanes_log2 = lanes_log2_for(*op, vector);
-    const int hu = heads_per_unit(*op, p.lanes_log2, 3);
+    const int bytes = vector_bytes(*op, addresses);
+    p.lanes_log2 = lanes_log2_for(*op, bytes);
+    int64_t blocks = 0;
     for (int i = 0; i < 3; ++i) {
         if (!op->has[i]) continue;
-        fill_part(*op, i, hu, p.part[i]);
-        p.part[i].x = X[i]; p.part[i].y = Y[i]; p.part[i].w = W[i];
-        p.units_per_token += uint32_t(p.part[i].units);
+        RotaryPart &part = p.part[i];
+        fill_part(*op, i, part);
+        part.x = X[i]; part.y = Y[i]; part.w = W[i];
+        if (part.heads > INT32_MAX / kRotaryMaxTokens / 2) return BTC_ERR_NOT_SUPPORTED;
+        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 8, int64_t(op->handle.sm_count) * 6);
+        const int64_t ctas = (op->tokens + part.cta_tokens - 1) / part.cta_tokens;
+        if (ctas > INT32_MAX / 4) return BTC_ERR_NOT_SUPPORTED;
+        part.ctas = uint32_t(ctas);
+        blocks += ctas;
     }
     p.pos = positions; p.slots = slots; p.freq = op->d_freq; p.flags = flags;
     p.tokens = op->tokens;
-    p.heads_per_unit = uint32_t(hu);
+    p.pairs = op->pairs;
+    p.pair.set(std::max(op->pairs, 1));
     p.norm = op->norm; p.eps = float(op->eps); p.mult = float(op->multiplier);
     p.page.set(op->page_tokens);
     p.slot_count = int32_t(op->pages * op->page_tokens);
-    const int64_t groups = kRotaryThreads >> p.lanes_log2;
-    const int64_t blocks = (op->tokens * p.units_per_token + groups - 1) / groups;
-    if (blocks > INT32_MAX) return BTC_ERR_NOT_SUPPORTED;
-    BTC_ROTARY_DISPATCH(launch_forward, op->dtype, vector, p, op->layout == BTC_ROTARY_INTERLEAVED, unsigned(blocks),
+    BTC_ROTARY_DISPATCH(launch_forward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED, unsigned(blocks),
                         static_cast<cudaStream_t>(cuda_stream));
     return launch_result();
 }
@@ -268,7 +280,7 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
     const void *X[2] = {Xq, Xk}, *dY[2] = {dYq, dYk}, *W[2] = {Wq, Wk};
     void *dX[2] = {dXq, dXk};
     float *dW[2] = {dWq, dWk};
-    bool vector = strides_allow_vectors(*op);
+    uintptr_t addresses = 0;
     const size_t es = esize(op->dtype);
     for (int i = 0; i < 2; ++i) {
         if (!op->has[i]) {
@@ -279,7 +291,7 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
         if (!aligned_to(dW[i], 4)) return BTC_ERR_MISALIGNED;
         for (const void *q : {op->norm ? X[i] : nullptr, dY[i], static_cast<const void *>(dX[i]), W[i]}) {
             if (!aligned_to(q, es)) return BTC_ERR_MISALIGNED;
-            vector = vector && aligned_to(q, 16);
+            addresses |= reinterpret_cast<uintptr_t>(q);
         }
     }
     if (op->pairs > 0 && !positions) return BTC_ERR_INVALID_ARGUMENT;
@@ -293,38 +305,52 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
 
     RotaryParams p;
     std::memset(static_cast<void *>(&p), 0, sizeof p);
-    p.lanes_log2 = lanes_log2_for(*op, vector);
-    const int hu = heads_per_unit(*op, p.lanes_log2, 2);
-    const int64_t groups = kRotaryThreads >> p.lanes_log2;
+    const int bytes = vector_bytes(*op, addresses);
+    p.lanes_log2 = lanes_log2_for(*op, bytes);
     const int64_t most = int64_t(op->handle.sm_count) * kBackwardCtasPerSm;
     int64_t all_heads = 0;
     for (int i = 0; i < 2; ++i)
         if (op->has[i]) all_heads += op->x[i].extent[1];
+    if (all_heads > INT32_MAX / kRotaryMaxTokens / 2) return BTC_ERR_NOT_SUPPORTED;
     for (int i = 0; i < 2; ++i) {
         if (!op->has[i]) continue;
-        fill_part(*op, i, hu, p.part[i]);
-        p.part[i].x = X[i]; p.part[i].dy = dY[i]; p.part[i].y = dX[i]; p.part[i].w = W[i];
-        // each part gets CTAs by its share of the heads, at least one, at most one per group of units
-        const int64_t blocks = (op->tokens * p.part[i].units + groups - 1) / groups;
-        int64_t share = (most - 1) * p.part[i].heads / all_heads;
-        share = std::max<int64_t>(1, std::min(share, most - 1));
-        p.ctas[i] = uint32_t(std::min(blocks, share));
+        RotaryPart &part = p.part[i];
+        fill_part(*op, i, part);
+        part.x = X[i]; part.dy = dY[i]; part.y = dX[i]; part.w = W[i];
+        // each part gets CTAs by its share of the heads, at least one, at most one per block of tokens
+        const int64_t share = std::max<int64_t>(1, std::min(most - 1, ((most - 1) * part.heads + all_heads / 2) / all_heads));
+        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 8, share);
+        part.ctas = uint32_t(std::min<int64_t>(share, (op->tokens + part.cta_tokens - 1) / part.cta_tokens));
     }
     p.pos = positions; p.freq = op->d_freq;
     p.partial = sums ? static_cast<float *>(workspace) : nullptr;
     p.tokens = op->tokens;
-    p.heads_per_unit = uint32_t(hu);
+    p.pairs = op->pairs;
+    p.pair.set(std::max(op->pairs, 1));
     p.norm = op->norm; p.eps = float(op->eps); p.mult = float(op->multiplier);
     p.page.set(1);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    BTC_ROTARY_DISPATCH(launch_backward, op->dtype, vector, p, op->layout == BTC_ROTARY_INTERLEAVED,
-                        unsigned(p.ctas[0] + p.ctas[1]), st);
+    BTC_ROTARY_DISPATCH(launch_backward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED,
+                        unsigned(p.part[0].ctas + p.part[1].ctas), st);
     const btc_error_t rc = launch_result();
     if (rc != BTC_SUCCESS || !sums) return rc;
+    // the summing kernel is set up while the first one runs and waits for its end on the device
     const int dim = int(op->x[0].extent[2]);
-    rotary_weight_gradient_kernel<<<dim3(unsigned((dim + 31) / 32), 2), 1024, 0, st>>>(
-        p.partial, int(p.ctas[0]), int(p.ctas[1]), dim, dWq, dWk);
-    return launch_result();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned((dim + kRotaryGradColumns - 1) / kRotaryGradColumns), 2);
+    cfg.blockDim = dim3(kRotaryGradThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, rotary_weight_gradient_kernel, static_cast<const float *>(p.partial), int(p.part[0].ctas),
+                           int(p.part[1].ctas), dim, dWq, dWk) != cudaSuccess) {
+        cudaGetLastError();
+        return BTC_ERR_CUDA;
+    }
+    return BTC_SUCCESS;
 }
 
 }  // extern "C"

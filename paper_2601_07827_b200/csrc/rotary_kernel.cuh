@@ -9,13 +9,13 @@
 // and does a few operations per value: it is bound by memory, for a handful of tokens by latency.
 //
 // Layout.  A value's partner in the rotation and the head's sum of squares must meet, so a head is owned
-// by a group of 2^k neighbouring lanes, a lane holding whole pairs: with 16-byte vectors lane c holds
-// pairs [c V, (c + 1) V), V = 16 bytes / element, i.e. two vectors (at c V and c V + pairs in the half
-// layout, neighbours in the interleaved one), so the rotation needs no exchange and the norm k shuffles.
-// The angle's cosine and sine depend on the token and the pair only: a group keeps them in registers
-// over the `heads_per_unit` heads that it takes of one token.
-// Heads whose sizes, strides or addresses do not allow 16-byte vectors run the same code with one
-// element per access, a warp per head, lane l holding pairs l, l + 32, l + 64, l + 96.
+// by a group of 2^k neighbouring lanes, a lane holding whole pairs: with vectors of V elements lane c holds
+// pairs [c V, (c + 1) V), i.e. two vectors (at c V and c V + pairs in the half layout, neighbours in the
+// interleaved one), so the rotation needs no exchange and the norm k shuffles.  Vectors are 16 bytes where
+// sizes, strides and addresses allow, else 8; what allows neither runs the same code with one element per
+// access, a warp per head, lane l holding pairs l, l + 32, l + 64, l + 96.
+// The angles depend on token and pair only: a CTA takes a few tokens with all their heads and computes each
+// angle once, into shared memory (computed by every group for itself they were a quarter of all instructions).
 #pragma once
 
 #include "../../include/btc.h"
@@ -25,6 +25,7 @@ namespace btc {
 
 constexpr int kRotaryMaxDim = 256;
 constexpr int kRotaryThreads = 256;
+constexpr int kRotaryMaxTokens = 16;     // tokens a CTA takes at a time
 
 struct RotaryPart {
     const void *x;                 // input [T, heads, dim]
@@ -37,7 +38,10 @@ struct RotaryPart {
     int32_t pairs, rest_pairs;     // rotated pairs; pairs of values that are not rotated (the last may lack its second)
     int32_t copy;                  // 1: values pass through unchanged (bit for bit)
     int32_t paged;
-    int32_t units;                 // groups of heads per token
+    float inv_dim;
+    uint32_t ctas;                 // CTAs of the part, tokens a CTA takes at a time
+    int32_t cta_tokens;
+    FastDiv head;                  // heads
 };
 
 struct RotaryParams {
@@ -47,13 +51,13 @@ struct RotaryParams {
     int32_t *flags;
     float *partial;                // backward: [CTA][kRotaryMaxDim] sums of dm n of the CTA's part
     int64_t tokens;
-    uint32_t units_per_token, heads_per_unit;
+    int32_t pairs;                 // of queries and keys
     int32_t lanes_log2;            // lanes per head
     int32_t norm;
     float eps, mult;
     FastDiv page;                  // tokens per page
     int32_t slot_count;            // slots in the pool
-    uint32_t ctas[2];              // backward: CTAs of the query part / key part
+    FastDiv pair;                  // pairs
 };
 
 // cos and sin of position * frequency.  The product is taken in units of 2^-64 turn modulo one turn, which
@@ -66,11 +70,35 @@ __device__ __forceinline__ void rotary_angle(int32_t pos, uint64_t freq, float m
     s *= mult;
 }
 
+// Where a CTA keeps the angles of its tokens: with vectors in the order in which the lanes' 16-byte (or 8-byte) reads
+// are neighbours.  V = 1: one element per access.
+template <int V> __device__ __forceinline__ int angle_place(int pair)
+{
+    constexpr int Q = V >= 4 ? 4 : V;
+    if (V <= 4) return pair;
+    const int chunk = pair / V, j = pair % V;
+    return (j / Q) * (kRotaryMaxDim / 2 / V * Q) + chunk * Q + j % Q;
+}
+template <int V>
+__device__ __forceinline__ void angles_to_shared(const RotaryParams &p, int64_t first, int tokens, float *c, float *s)
+{
+    for (int e = threadIdx.x; e < tokens * p.pairs; e += kRotaryThreads) {
+        const int t = int(p.pair.div(uint32_t(e))), i = e - t * p.pairs;
+        float x, y;
+        rotary_angle(p.pos[first + t], p.freq[i], p.mult, x, y);
+        const int at = t * (kRotaryMaxDim / 2) + angle_place<V>(i);
+        c[at] = x;
+        s[at] = y;
+    }
+}
+
 // The pairs of one lane: N slots, their element positions, and loads and stores that present slot j as (a[j], b[j]).
-template <typename T, bool VECTOR, bool INTERLEAVED> struct RotaryLane {
-    static constexpr int V = 16 / int(sizeof(T));
+// V: elements per access (1: the scalar form).
+template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
+    static constexpr bool VECTOR = V > 1;
     static constexpr int N = VECTOR ? V : 4;
-    struct Raw { uint4 a, b; };
+    typedef typename VectorOf<VECTOR ? V * int(sizeof(T)) : 16>::type Vec;
+    struct Raw { Vec a, b; };
     int ea, eb;                    // VECTOR: element offsets of the two vectors
     bool active, rotated;          // VECTOR: the lane has pairs; they are rotated
     int lane, pairs, rest, dim;
@@ -88,7 +116,6 @@ template <typename T, bool VECTOR, bool INTERLEAVED> struct RotaryLane {
         }
     }
     __device__ __forceinline__ bool slot_rotated(int j) const { return VECTOR ? rotated : lane + 32 * j < pairs; }
-    __device__ __forceinline__ int slot_pair(int j) const { return VECTOR ? lane * V + j : lane + 32 * j; }
     // scalar form: element positions of slot j (dim or more: absent)
     __device__ __forceinline__ void slot_elements(int j, int &a, int &b) const
     {
@@ -102,73 +129,96 @@ template <typename T, bool VECTOR, bool INTERLEAVED> struct RotaryLane {
             b = q < rest ? 2 * pairs + rest + q : dim;
         }
     }
-    __device__ __forceinline__ Raw load_raw(const T *row) const
+    __device__ __forceinline__ static Raw zero()
     {
         Raw r;
-        r.a = r.b = make_uint4(0, 0, 0, 0);
+        r.a = Vec();
+        r.b = Vec();
+        return r;
+    }
+    __device__ __forceinline__ Raw load_raw(const T *row) const
+    {
+        Raw r = zero();
         if (active) {
-            r.a = *reinterpret_cast<const uint4 *>(row + ea);
-            r.b = *reinterpret_cast<const uint4 *>(row + eb);
+            r.a = *reinterpret_cast<const Vec *>(row + ea);
+            r.b = *reinterpret_cast<const Vec *>(row + eb);
         }
         return r;
     }
-    __device__ __forceinline__ void unpack(const Raw &r, float (&a)[N], float (&b)[N]) const
+    __device__ __forceinline__ void store_raw(T *row, const Raw &r) const
+    {
+        if (active) {
+            *reinterpret_cast<Vec *>(row + ea) = r.a;
+            *reinterpret_cast<Vec *>(row + eb) = r.b;
+        }
+    }
+    // slots 2i and 2i + 1 are the halves of a[i] and b[i]
+    static constexpr int N2 = N / 2;
+    __device__ __forceinline__ void unpack(const Raw &r, float2 (&a)[N2], float2 (&b)[N2]) const
     {
         if constexpr (VECTOR) {
             float u[V], v[V];
-            unpack16(r.a, u, T());
-            unpack16(r.b, v, T());
-            if constexpr (INTERLEAVED) {
+            unpack_vector<T, V>(r.a, u);
+            unpack_vector<T, V>(r.b, v);
+            auto from = [&](int e) { return e < V ? u[e] : v[e - V]; };
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) {
-                    a[j] = u[2 * j]; b[j] = u[2 * j + 1];
-                    a[V / 2 + j] = v[2 * j]; b[V / 2 + j] = v[2 * j + 1];
+            for (int i = 0; i < N2; ++i) {
+                if (INTERLEAVED) {
+                    a[i] = make_float2(from(4 * i), from(4 * i + 2));
+                    b[i] = make_float2(from(4 * i + 1), from(4 * i + 3));
+                } else {
+                    a[i] = make_float2(u[2 * i], u[2 * i + 1]);
+                    b[i] = make_float2(v[2 * i], v[2 * i + 1]);
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) { a[j] = u[j]; b[j] = v[j]; }
             }
         }
     }
-    __device__ __forceinline__ void load(const T *row, int64_t stride, float (&a)[N], float (&b)[N]) const
+    __device__ __forceinline__ void load(const T *row, int64_t stride, float2 (&a)[N2], float2 (&b)[N2]) const
     {
         if constexpr (VECTOR) {
             unpack(load_raw(row), a, b);
         } else {
+            float x[N], y[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 int e, f;
                 slot_elements(j, e, f);
-                a[j] = e < dim ? to_f32(row[e * stride]) : 0.f;
-                b[j] = f < dim ? to_f32(row[f * stride]) : 0.f;
+                x[j] = e < dim ? to_f32(row[e * stride]) : 0.f;
+                y[j] = f < dim ? to_f32(row[f * stride]) : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < N2; ++i) {
+                a[i] = make_float2(x[2 * i], x[2 * i + 1]);
+                b[i] = make_float2(y[2 * i], y[2 * i + 1]);
             }
         }
     }
-    __device__ __forceinline__ void store(T *row, int64_t stride, const float (&a)[N], const float (&b)[N]) const
+    __device__ __forceinline__ void store(T *row, int64_t stride, const float2 (&a)[N2], const float2 (&b)[N2]) const
     {
         if constexpr (VECTOR) {
             float u[V], v[V];
-            if constexpr (INTERLEAVED) {
+            auto into = [&](int e) -> float & { return e < V ? u[e] : v[e - V]; };
 #pragma unroll
-                for (int j = 0; j < V / 2; ++j) {
-                    u[2 * j] = a[j]; u[2 * j + 1] = b[j];
-                    v[2 * j] = a[V / 2 + j]; v[2 * j + 1] = b[V / 2 + j];
+            for (int i = 0; i < N2; ++i) {
+                if (INTERLEAVED) {
+                    into(4 * i) = a[i].x; into(4 * i + 2) = a[i].y;
+                    into(4 * i + 1) = b[i].x; into(4 * i + 3) = b[i].y;
+                } else {
+                    u[2 * i] = a[i].x; u[2 * i + 1] = a[i].y;
+                    v[2 * i] = b[i].x; v[2 * i + 1] = b[i].y;
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) { u[j] = a[j]; v[j] = b[j]; }
             }
-            if (active) {
-                *reinterpret_cast<uint4 *>(row + ea) = pack16(u, T());
-                *reinterpret_cast<uint4 *>(row + eb) = pack16(v, T());
-            }
+            Raw r;
+            r.a = pack_vector<T, V>(u);
+            r.b = pack_vector<T, V>(v);
+            store_raw(row, r);
         } else {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 int e, f;
                 slot_elements(j, e, f);
-                if (e < dim) row[e * stride] = from_f32<T>(a[j]);
-                if (f < dim) row[f * stride] = from_f32<T>(b[j]);
+                if (e < dim) row[e * stride] = from_f32<T>(j & 1 ? a[j / 2].y : a[j / 2].x);
+                if (f < dim) row[f * stride] = from_f32<T>(j & 1 ? b[j / 2].y : b[j / 2].x);
             }
         }
     }
@@ -182,6 +232,49 @@ template <typename T, bool VECTOR, bool INTERLEAVED> struct RotaryLane {
             if (f < dim) dst[f * ds] = src[f * ss];
         }
     }
+    // (a, b) <- (a c - b s, b c + a s) with a token's angles on the rotated slots; BACK: the transposed rotation
+    template <bool BACK>
+    __device__ __forceinline__ void rotate(const float *cosines, const float *sines, float2 (&a)[N2], float2 (&b)[N2]) const
+    {
+        float2 c[N2], s[N2];
+        if constexpr (VECTOR) {
+            constexpr int Q = V >= 4 ? 4 : V;
+            typedef typename VectorOf<Q * 4>::type Angles;
+            if (!rotated) return;
+#pragma unroll
+            for (int i = 0; i < V / Q; ++i) {
+                const int at = i * (kRotaryMaxDim / 2 / V * Q) + lane * Q;
+                float x[Q], y[Q];
+                unpack_vector<float, Q>(*reinterpret_cast<const Angles *>(cosines + at), x);
+                unpack_vector<float, Q>(*reinterpret_cast<const Angles *>(sines + at), y);
+#pragma unroll
+                for (int j = 0; j < Q / 2; ++j) {
+                    c[i * Q / 2 + j] = make_float2(x[2 * j], x[2 * j + 1]);
+                    s[i * Q / 2 + j] = make_float2(y[2 * j], y[2 * j + 1]);
+                }
+            }
+        } else {
+            // slots that are not rotated: the identity would still mix an infinite partner in (0 * inf), so they are put back
+#pragma unroll
+            for (int i = 0; i < N2; ++i) {
+                const int p0 = slot_rotated(2 * i) ? lane + 64 * i : 0, p1 = slot_rotated(2 * i + 1) ? lane + 64 * i + 32 : 0;
+                c[i] = make_float2(cosines[p0], cosines[p1]);
+                s[i] = make_float2(sines[p0], sines[p1]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N2; ++i) {
+            const float2 minus = make_float2(-s[i].x, -s[i].y);
+            const float2 x = fma2(b[i], BACK ? s[i] : minus, mul2(a[i], c[i])), y = fma2(a[i], BACK ? minus : s[i], mul2(b[i], c[i]));
+            if constexpr (VECTOR) {
+                a[i] = x;
+                b[i] = y;
+            } else {
+                if (slot_rotated(2 * i)) { a[i].x = x.x; b[i].x = y.x; }
+                if (slot_rotated(2 * i + 1)) { a[i].y = x.y; b[i].y = y.y; }
+            }
+        }
+    }
 };
 
 __device__ __forceinline__ float group_sum(float v, int lanes_log2)
@@ -190,243 +283,209 @@ __device__ __forceinline__ float group_sum(float v, int lanes_log2)
     return v;
 }
 
-// A group of lanes takes one unit: `heads_per_unit` heads of one part of one token.
-template <typename T, bool VECTOR, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotaryThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
+// A CTA takes `cta_tokens` tokens of one part (queries, keys or values); its groups of lanes take the (token, head)
+// pairs in turn, the loads of two of them issued together.
+template <typename T, int V, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRotaryThreads, 3) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
 {
-    typedef RotaryLane<T, VECTOR, INTERLEAVED> Lane;
-    constexpr int N = Lane::N;
-    constexpr int FLIGHT = VECTOR ? 4 : 1;      // heads whose loads are issued together
-    const int lanes = 1 << p.lanes_log2;
-    const int64_t unit = int64_t(blockIdx.x) * (kRotaryThreads >> p.lanes_log2) + (threadIdx.x >> p.lanes_log2);
-    int64_t token;
-    uint32_t u;
-    if (p.tokens * p.units_per_token < (int64_t(1) << 31)) {
-        token = uint32_t(unit) / p.units_per_token;
-        u = uint32_t(unit) - uint32_t(token) * p.units_per_token;
-    } else {
-        token = unit / p.units_per_token;
-        u = uint32_t(unit - token * p.units_per_token);
-    }
-    bool valid = token < p.tokens;               // the lanes of a warp stay together for the shuffles
-    if (!valid) { token = 0; u = 0; }
+    typedef RotaryLane<T, V, INTERLEAVED> Lane;
+    constexpr int N2 = Lane::N2, FLIGHT = 2;
+    __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
+    const int lanes = 1 << p.lanes_log2, groups = kRotaryThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    uint32_t cta = blockIdx.x;
     int which = 0;
-    while (which < 2 && u >= uint32_t(p.part[which].units)) u -= uint32_t(p.part[which++].units);
+    while (which < 2 && cta >= p.part[which].ctas) cta -= p.part[which++].ctas;
     const RotaryPart &part = p.part[which];
+    const int64_t first = int64_t(cta) * part.cta_tokens;
+    const int tokens = int(min(int64_t(part.cta_tokens), p.tokens - first)), heads = part.heads, items = tokens * heads;
+    const bool norm = p.norm && !part.copy, turning = part.pairs > 0;
     Lane lane;
     lane.set(part, threadIdx.x & (lanes - 1));
-
-    const int first = int(u * p.heads_per_unit);
-    const int count = valid ? min(int(p.heads_per_unit), part.heads - first) : 0;
-    const T *x = static_cast<const T *>(part.x) + token * part.x_t + first * part.x_h;
-    T *y = static_cast<T *>(part.y) + first * part.y_h;
-    bool write = valid;
-    if (part.paged) {
-        const int32_t slot = p.slots[token];
-        write = valid && slot >= 0 && slot < p.slot_count;
-        if (valid && slot >= p.slot_count && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_SLOT));
-        const uint32_t at = write ? uint32_t(slot) : 0u, page = p.page.div(at);
-        y += int64_t(page) * part.y_page + int64_t(at - page * p.page.d) * part.y_t;
-    } else {
-        y += token * part.y_t;
-    }
-
-    float c[N], s[N], wa[N], wb[N];
-    const bool norm = p.norm && !part.copy;
-    if (part.pairs > 0) {
-        const int32_t pos = p.pos[token];
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            c[j] = 1.f;
-            s[j] = 0.f;
-            if (lane.slot_rotated(j)) rotary_angle(pos, p.freq[lane.slot_pair(j)], p.mult, c[j], s[j]);
-        }
-    }
-    if (norm && part.w) {
-        lane.load(static_cast<const T *>(part.w), 1, wa, wb);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) wa[j] = wb[j] = 1.f;
-    }
-
-    const uint32_t steps = p.heads_per_unit;     // the same for every lane of the warp
-    for (uint32_t h0 = 0; h0 < steps; h0 += FLIGHT) {
+    float2 wa[N2], wb[N2];
+    bool ready = false;
+#pragma unroll 1
+    for (int base = 0; base < items; base += FLIGHT * groups) {        // the same steps in every lane: shuffles follow
         typename Lane::Raw raw[FLIGHT];
-        if constexpr (VECTOR) {
+        const T *src[FLIGHT];
+        int head[FLIGHT], token[FLIGHT];
 #pragma unroll
-            for (int i = 0; i < FLIGHT; ++i) {
-                raw[i].a = raw[i].b = make_uint4(0, 0, 0, 0);
-                if (int(h0) + i < count) raw[i] = lane.load_raw(x + (int64_t(h0) + i) * part.x_h);
+        for (int i = 0; i < FLIGHT; ++i) {
+            const int item = base + i * groups + group;
+            const bool here = item < items;
+            const int t = here ? int(part.head.div(uint32_t(item))) : 0;
+            token[i] = here ? t : -1;
+            head[i] = here ? item - t * heads : 0;
+            src[i] = static_cast<const T *>(part.x) + (first + t) * part.x_t + head[i] * part.x_h;
+            if constexpr (V > 1) raw[i] = here ? lane.load_raw(src[i]) : Lane::zero();
+        }
+        if (!ready) {                                                   // while the first loads are under way
+#pragma unroll
+            for (int j = 0; j < N2; ++j) wa[j] = wb[j] = both(1.f);
+            if (norm && part.w) lane.load(static_cast<const T *>(part.w), 1, wa, wb);
+            if (turning) {
+                angles_to_shared<V>(p, first, tokens, cosines, sines);
+                __syncthreads();
             }
+            ready = true;
         }
 #pragma unroll
         for (int i = 0; i < FLIGHT; ++i) {
-            const int h = int(h0) + i;
-            const bool here = h < count;
-            T *row = y + int64_t(h) * part.y_h;
-            if (part.copy) {
-                if (here && write) {
-                    if constexpr (VECTOR) {
-                        if (lane.active) {
-                            *reinterpret_cast<uint4 *>(row + lane.ea) = raw[i].a;
-                            *reinterpret_cast<uint4 *>(row + lane.eb) = raw[i].b;
-                        }
-                    } else {
-                        lane.copy(x + int64_t(h) * part.x_h, part.x_d, row, part.y_d);
-                    }
-                }
-            }
-            float a[N], b[N];
-            if constexpr (VECTOR) {
+            const bool here = token[i] >= 0;
+            float2 a[N2], b[N2];
+            if constexpr (V > 1) {
                 lane.unpack(raw[i], a, b);
             } else {
 #pragma unroll
-                for (int j = 0; j < N; ++j) a[j] = b[j] = 0.f;
-                if (here && !part.copy) lane.load(x + int64_t(h) * part.x_h, part.x_d, a, b);
+                for (int j = 0; j < N2; ++j) a[j] = b[j] = both(0.f);
+                if (here && !part.copy) lane.load(src[i], part.x_d, a, b);
             }
-            if (p.norm) {                         // all lanes: a warp may hold heads of several parts
-                float ss = 0.f;
+            if (norm) {
+                float2 squares = both(0.f);
 #pragma unroll
-                for (int j = 0; j < N; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
-                ss = group_sum(ss, p.lanes_log2);
-                const float r = rsqrtf(ss / float(part.dim) + p.eps);
+                for (int j = 0; j < N2; ++j) squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
+                const float ss = group_sum(squares.x + squares.y, p.lanes_log2);
+                const float2 r = both(rsqrtf(fmaf(ss, part.inv_dim, p.eps)));
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    a[j] = a[j] * r * wa[j];
-                    b[j] = b[j] * r * wb[j];
+                for (int j = 0; j < N2; ++j) {
+                    a[j] = mul2(mul2(a[j], r), wa[j]);
+                    b[j] = mul2(mul2(b[j], r), wb[j]);
                 }
             }
-            if (part.copy || !here || !write) continue;
-            if (part.pairs > 0) {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (lane.slot_rotated(j)) {
-                        const float t = a[j] * c[j] - b[j] * s[j];
-                        b[j] = b[j] * c[j] + a[j] * s[j];
-                        a[j] = t;
-                    }
+            if (!here) continue;
+            T *dst = static_cast<T *>(part.y) + head[i] * part.y_h;
+            if (part.paged) {
+                const int32_t slot = p.slots[first + token[i]];
+                if (slot >= p.slot_count && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_SLOT));
+                if (slot < 0 || slot >= p.slot_count) continue;
+                const uint32_t page = p.page.div(uint32_t(slot));
+                dst += int64_t(page) * part.y_page + int64_t(uint32_t(slot) - page * p.page.d) * part.y_t;
+            } else {
+                dst += (first + token[i]) * part.y_t;
             }
-            lane.store(row, part.y_d, a, b);
+            if (part.copy) {
+                if constexpr (V > 1) lane.store_raw(dst, raw[i]);
+                else lane.copy(src[i], part.x_d, dst, part.y_d);
+                continue;
+            }
+            if (turning) lane.template rotate<false>(cosines + token[i] * (kRotaryMaxDim / 2), sines + token[i] * (kRotaryMaxDim / 2), a, b);
+            lane.store(dst, part.y_d, a, b);
         }
     }
 }
 
-// Persistent CTAs, each for one part: a thread keeps its pairs (the lane's place in the head never changes) and
-// so its share of dw in registers over all units it takes; at the end the CTA's groups are added in shared memory
-// in a fixed order and the CTA writes one row of `partial`.
-template <typename T, bool VECTOR, bool INTERLEAVED>
+// Persistent CTAs, each for one part, `cta_tokens` tokens at a time: a thread keeps its pairs (the lane's place in the
+// head never changes) and so its share of dw in registers over everything it takes; at the end the CTA's groups are
+// added in shared memory in a fixed order and the CTA writes one row of `partial`.
+template <typename T, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
 {
-    typedef RotaryLane<T, VECTOR, INTERLEAVED> Lane;
-    constexpr int N = Lane::N;
+    typedef RotaryLane<T, V, INTERLEAVED> Lane;
+    constexpr int N = Lane::N, N2 = Lane::N2, FLIGHT = V > 1 ? 2 : 1;
+    __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
     __shared__ float sums[kRotaryThreads / 32][kRotaryMaxDim];
-    const int lanes = 1 << p.lanes_log2;
-    const int which = blockIdx.x < p.ctas[0] ? 0 : 1;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lanes = 1 << p.lanes_log2, groups = kRotaryThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const int which = blockIdx.x < p.part[0].ctas ? 0 : 1;
     const RotaryPart &part = p.part[which];
-    const uint32_t cta = which ? blockIdx.x - p.ctas[0] : blockIdx.x;
-    const int groups = kRotaryThreads >> p.lanes_log2;
+    const uint32_t cta = which ? blockIdx.x - p.part[0].ctas : blockIdx.x;
+    const int heads = part.heads;
+    const bool turning = p.pairs > 0;
     Lane lane;
     lane.set(part, threadIdx.x & (lanes - 1));
-    float wa[N], wb[N], da[N], db[N];
-    if (p.norm && part.w) {
-        lane.load(static_cast<const T *>(part.w), 1, wa, wb);
-    } else {
+    float2 wa[N2], wb[N2], da2[N2], db2[N2];
 #pragma unroll
-        for (int j = 0; j < N; ++j) wa[j] = wb[j] = 1.f;
+    for (int j = 0; j < N2; ++j) {
+        wa[j] = wb[j] = both(1.f);
+        da2[j] = db2[j] = both(0.f);
     }
-#pragma unroll
-    for (int j = 0; j < N; ++j) da[j] = db[j] = 0.f;
+    if (p.norm && part.w) lane.load(static_cast<const T *>(part.w), 1, wa, wb);
 
-    const int64_t units = p.tokens * part.units;
-    const int64_t stride = int64_t(p.ctas[which]) * groups;
-    const int64_t begin = int64_t(cta) * groups;         // the CTA's first unit; its warps take the same number of steps
-    for (int64_t base = begin; base < units; base += stride) {
-        int64_t unit = base + (threadIdx.x >> p.lanes_log2);
-        const bool valid = unit < units;
-        if (!valid) unit = 0;
-        int64_t token;
-        if (units < (int64_t(1) << 32)) token = uint32_t(unit) / uint32_t(part.units);
-        else token = unit / part.units;
-        const int first = int(unit - token * part.units) * int(p.heads_per_unit);
-        const int count = valid ? min(int(p.heads_per_unit), part.heads - first) : 0;
-        const T *x = static_cast<const T *>(part.x) + token * part.x_t + first * part.x_h;
-        T *dx = static_cast<T *>(part.y) + token * part.x_t + first * part.x_h;
-        const T *dy = static_cast<const T *>(part.dy) + token * part.y_t + first * part.y_h;
-        float c[N], s[N];
-        if (part.pairs > 0) {
-            const int32_t pos = p.pos[token];
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                c[j] = 1.f;
-                s[j] = 0.f;
-                if (lane.slot_rotated(j)) rotary_angle(pos, p.freq[lane.slot_pair(j)], p.mult, c[j], s[j]);
-            }
-        }
-        for (uint32_t h0 = 0; h0 < p.heads_per_unit; h0 += 2) {
-            constexpr int FLIGHT = VECTOR ? 2 : 1;
+    for (int64_t first = int64_t(cta) * part.cta_tokens; first < p.tokens; first += int64_t(part.ctas) * part.cta_tokens) {
+        const int tokens = int(min(int64_t(part.cta_tokens), p.tokens - first)), items = tokens * heads;
+        bool angles_ready = !turning;
+#pragma unroll 1
+        for (int base = 0; base < items; base += FLIGHT * groups) {
             typename Lane::Raw rx[FLIGHT], rg[FLIGHT];
-            if constexpr (VECTOR) {
+            int token[FLIGHT], head[FLIGHT];
 #pragma unroll
-                for (int i = 0; i < FLIGHT; ++i) {
-                    rx[i].a = rx[i].b = rg[i].a = rg[i].b = make_uint4(0, 0, 0, 0);
-                    if (int(h0) + i < count) {
-                        rg[i] = lane.load_raw(dy + (int64_t(h0) + i) * part.y_h);
-                        if (p.norm) rx[i] = lane.load_raw(x + (int64_t(h0) + i) * part.x_h);
+            for (int i = 0; i < FLIGHT; ++i) {
+                const int item = base + i * groups + group;
+                const bool here = item < items;
+                const int t = here ? int(part.head.div(uint32_t(item))) : 0;
+                token[i] = here ? t : -1;
+                head[i] = here ? item - t * heads : 0;
+                if constexpr (V > 1) {
+                    rx[i] = rg[i] = Lane::zero();
+                    if (here) {
+                        rg[i] = lane.load_raw(static_cast<const T *>(part.dy) + (first + t) * part.y_t + head[i] * part.y_h);
+                        if (p.norm) rx[i] = lane.load_raw(static_cast<const T *>(part.x) + (first + t) * part.x_t + head[i] * part.x_h);
                     }
                 }
             }
+            if (!angles_ready) {
+                __syncthreads();                                        // the tokens before are done with
+                angles_to_shared<V>(p, first, tokens, cosines, sines);
+                __syncthreads();
+                angles_ready = true;
+            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int h = int(h0) + i;
-                const bool here = h < count;
-                float ga[N], gb[N], a[N], b[N];
-                if constexpr (VECTOR) {
+            for (int i = 0; i < FLIGHT; ++i) {
+                const bool here = token[i] >= 0;
+                const int64_t t = first + (here ? token[i] : 0);
+                float2 ga[N2], gb[N2], a[N2], b[N2];
+                if constexpr (V > 1) {
                     lane.unpack(rg[i], ga, gb);
                     if (p.norm) lane.unpack(rx[i], a, b);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < N; ++j) a[j] = b[j] = ga[j] = gb[j] = 0.f;
+                    for (int j = 0; j < N2; ++j) a[j] = b[j] = ga[j] = gb[j] = both(0.f);
                     if (here) {
-                        lane.load(dy + int64_t(h) * part.y_h, part.y_d, ga, gb);
-                        if (p.norm) lane.load(x + int64_t(h) * part.x_h, part.x_d, a, b);
+                        lane.load(static_cast<const T *>(part.dy) + t * part.y_t + head[i] * part.y_h, part.y_d, ga, gb);
+                        if (p.norm) lane.load(static_cast<const T *>(part.x) + t * part.x_t + head[i] * part.x_h, part.x_d, a, b);
                     }
                 }
-                if (part.pairs > 0) {
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (lane.slot_rotated(j)) {
-                            const float t = ga[j] * c[j] + gb[j] * s[j];
-                            gb[j] = gb[j] * c[j] - ga[j] * s[j];
-                            ga[j] = t;
-                        }
+                if (turning) {
+                    const int at = (here ? token[i] : 0) * (kRotaryMaxDim / 2);
+                    lane.template rotate<true>(cosines + at, sines + at, ga, gb);
                 }
                 if (p.norm) {
-                    float ss = 0.f, dot = 0.f;
+                    // with g = dm w:  dx = r (g - x r^2 mean(g x)),  dw += dm x r
+                    float2 squares = both(0.f), dots = both(0.f), pa[N2], pb[N2];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
-                        dot = fmaf(ga[j] * wa[j], a[j], fmaf(gb[j] * wb[j], b[j], dot));
+                    for (int j = 0; j < N2; ++j) {
+                        squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
+                        pa[j] = mul2(ga[j], wa[j]);
+                        pb[j] = mul2(gb[j], wb[j]);
+                        dots = fma2(pa[j], a[j], fma2(pb[j], b[j], dots));
                     }
-                    ss = group_sum(ss, p.lanes_log2);
-                    dot = group_sum(dot, p.lanes_log2);
-                    const float r = rsqrtf(ss / float(part.dim) + p.eps);
-                    const float mean = dot * r / float(part.dim);    // mean(g n)
+                    float ss = squares.x + squares.y, dot = dots.x + dots.y;
+                    for (int k = 0; k < p.lanes_log2; ++k) {
+                        ss += __shfl_xor_sync(0xffffffffu, ss, 1 << k);
+                        dot += __shfl_xor_sync(0xffffffffu, dot, 1 << k);
+                    }
+                    const float r = here ? rsqrtf(fmaf(ss, part.inv_dim, p.eps)) : 0.f;   // 0: nothing is added to dw
+                    const float2 r2 = both(r), pull = both(-(dot * r * part.inv_dim) * r);  // -r mean(g n)
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float na = a[j] * r, nb = b[j] * r;
-                        if (here) {
-                            da[j] = fmaf(ga[j], na, da[j]);
-                            db[j] = fmaf(gb[j], nb, db[j]);
-                        }
-                        ga[j] = r * (ga[j] * wa[j] - na * mean);
-                        gb[j] = r * (gb[j] * wb[j] - nb * mean);
+                    for (int j = 0; j < N2; ++j) {
+                        a[j] = mul2(a[j], r2);                                             // n
+                        b[j] = mul2(b[j], r2);
+                        da2[j] = fma2(ga[j], a[j], da2[j]);
+                        db2[j] = fma2(gb[j], b[j], db2[j]);
+                        ga[j] = fma2(pa[j], r2, mul2(a[j], pull));
+                        gb[j] = fma2(pb[j], r2, mul2(b[j], pull));
                     }
                 }
-                if (here) lane.store(dx + int64_t(h) * part.x_h, part.x_d, ga, gb);
+                if (here) lane.store(static_cast<T *>(part.y) + t * part.x_t + head[i] * part.x_h, part.x_d, ga, gb);
             }
         }
     }
     if (!p.norm || !p.partial) return;
+    float da[N], db[N];
+#pragma unroll
+    for (int j = 0; j < N2; ++j) {
+        da[2 * j] = da2[j].x; da[2 * j + 1] = da2[j].y;
+        db[2 * j] = db2[j].x; db[2 * j + 1] = db2[j].y;
+    }
     // the warp's groups hold the same pairs: add them, then the warps
     for (int k = p.lanes_log2; k < 5; ++k) {
 #pragma unroll
@@ -437,7 +496,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
     }
     const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
     if (l < lanes) {
-        if constexpr (VECTOR) {
+        if constexpr (V > 1) {
             if (lane.active) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
@@ -466,24 +525,33 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
     }
 }
 
-// dw = sum of the CTAs' rows, in a fixed order: 32 columns per block, 32 lanes of rows each
-__global__ void __launch_bounds__(1024) rotary_weight_gradient_kernel(const float *partial, int rows_q, int rows_k, int dim,
-                                                                      float *dwq, float *dwk)
+// dw = sum of the CTAs' rows, in a fixed order: 8 columns per block, 128 threads to a column's rows
+constexpr int kRotaryGradColumns = 8, kRotaryGradThreads = 1024;
+static __global__ void __launch_bounds__(kRotaryGradThreads) rotary_weight_gradient_kernel(const float *partial, int rows_q, int rows_k, int dim,
+                                                                                         float *dwq, float *dwk)
 {
-    __shared__ float tile[32][33];
+    __shared__ float tile[kRotaryGradThreads / 32][kRotaryGradColumns];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int which = blockIdx.y;
     float *dw = which ? dwk : dwq;
     if (!dw) return;
     const int rows = which ? rows_k : rows_q, first = which ? rows_q : 0;
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31);
+    const int col = blockIdx.x * kRotaryGradColumns + (threadIdx.x % kRotaryGradColumns);
     float t = 0.f;
     if (col < dim)
-        for (int r = threadIdx.x >> 5; r < rows; r += 32) t += partial[int64_t(first + r) * kRotaryMaxDim + col];
-    tile[threadIdx.x >> 5][threadIdx.x & 31] = t;
+#pragma unroll 4
+        for (int r = threadIdx.x / kRotaryGradColumns; r < rows; r += kRotaryGradThreads / kRotaryGradColumns)
+            t += partial[int64_t(first + r) * kRotaryMaxDim + col];
+    // the warp's 4 rows of threads, then the warps
+    t += __shfl_xor_sync(0xffffffffu, t, 8);
+    t += __shfl_xor_sync(0xffffffffu, t, 16);
+    if ((threadIdx.x & 31) < kRotaryGradColumns) tile[threadIdx.x / 32][threadIdx.x & 31] = t;
     __syncthreads();
-    t = tile[threadIdx.x & 31][threadIdx.x >> 5];
+    const int warp = threadIdx.x / 32;
+    if (warp >= kRotaryGradColumns) return;
+    t = tile[threadIdx.x & 31][warp];
     for (int k = 1; k < 32; k <<= 1) t += __shfl_xor_sync(0xffffffffu, t, k);
-    const int out = blockIdx.x * 32 + (threadIdx.x >> 5);
+    const int out = blockIdx.x * kRotaryGradColumns + warp;
     if ((threadIdx.x & 31) == 0 && out < dim) dw[out] = t;
 }
 

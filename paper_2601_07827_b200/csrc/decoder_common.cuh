@@ -68,20 +68,10 @@ template <typename T, int V> __device__ __forceinline__ typename VectorOf<V * in
     else return make_uint2(w[0], w[1]);
 }
 
-// Two fp32 operations in one instruction, each half rounded like its scalar form.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)),
-        "l"(*reinterpret_cast<const uint64_t *>(&c)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<const uint64_t *>(&a)), "l"(*reinterpret_cast<const uint64_t *>(&b)));
-    return *reinterpret_cast<const float2 *>(&r);
-}
+// Pairs of fp32 operations.  (As the packed two-in-one instructions they cost more moves between registers than
+// they save: the rotary kernels took 3 to 10 % longer with them.)
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31 without a divide: q = (n * mul) >> shift in 64 bits, with

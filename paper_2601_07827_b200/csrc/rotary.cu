@@ -1,5 +1,6 @@
 // C entry points of the head norm and rotary position operator (rotary_kernel.cuh).
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -40,6 +41,9 @@ bool strides_allow_vectors(const btc_rotary_s &op, int64_t v)
             if (t->stride[r - 1] != 1) return false;
             for (size_t k = 0; k + 1 < r; ++k)
                 if (t->extent[k] > 1 && t->stride[k] % v != 0) return false;
+            // byte offsets inside the tokens that a CTA takes at a time are formed in 32 bits, unsigned
+            const int64_t token = t->stride[r - 3], head = t->stride[r - 2];
+            if (token < 0 || head < 0 || (__int128(token) * kRotaryMaxTokens + __int128(head) * t->extent[r - 2] + 256) * 4 > INT32_MAX) return false;
         }
     }
     return true;
@@ -94,16 +98,20 @@ void fill_part(const btc_rotary_s &op, int i, RotaryPart &p)
 }
 
 template <typename T, int V>
-void launch_forward(const RotaryParams &p, bool interleaved, unsigned blocks, cudaStream_t st)
+void launch_forward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
 {
-    if (interleaved) rotary_forward_kernel<T, V, true><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else rotary_forward_kernel<T, V, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    // the scalar form asks for each slot in any case
+    constexpr bool F = V > 1;
+    if (interleaved) (F && full) ? rotary_forward_kernel<T, V, true, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_forward_kernel<T, V, true, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    else (F && full) ? rotary_forward_kernel<T, V, false, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_forward_kernel<T, V, false, false><<<blocks, kRotaryThreads, 0, st>>>(p);
 }
 template <typename T, int V>
-void launch_backward(const RotaryParams &p, bool interleaved, unsigned blocks, cudaStream_t st)
+void launch_backward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
 {
-    if (interleaved) rotary_backward_kernel<T, V, true><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else rotary_backward_kernel<T, V, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    // the scalar form asks for each slot in any case
+    constexpr bool F = V > 1;
+    if (interleaved) (F && full) ? rotary_backward_kernel<T, V, true, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_backward_kernel<T, V, true, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    else (F && full) ? rotary_backward_kernel<T, V, false, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_backward_kernel<T, V, false, false><<<blocks, kRotaryThreads, 0, st>>>(p);
 }
 
 #define BTC_ROTARY_DISPATCH(F, dtype, bytes, ...)                                                                        \
@@ -264,7 +272,7 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
     p.norm = op->norm; p.eps = float(op->eps); p.mult = float(op->multiplier);
     p.page.set(op->page_tokens);
     p.slot_count = int32_t(op->pages * op->page_tokens);
-    BTC_ROTARY_DISPATCH(launch_forward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED, unsigned(blocks),
+    BTC_ROTARY_DISPATCH(launch_forward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED, 2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(blocks),
                         static_cast<cudaStream_t>(cuda_stream));
     return launch_result();
 }
@@ -319,7 +327,7 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
         part.x = X[i]; part.dy = dY[i]; part.y = dX[i]; part.w = W[i];
         // each part gets CTAs by its share of the heads, at least one, at most one per block of tokens
         const int64_t share = std::max<int64_t>(1, std::min(most - 1, ((most - 1) * part.heads + all_heads / 2) / all_heads));
-        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 8, share);
+        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 16, share);
         part.ctas = uint32_t(std::min<int64_t>(share, (op->tokens + part.cta_tokens - 1) / part.cta_tokens));
     }
     p.pos = positions; p.freq = op->d_freq;
@@ -331,7 +339,7 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
     p.page.set(1);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     BTC_ROTARY_DISPATCH(launch_backward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED,
-                        unsigned(p.part[0].ctas + p.part[1].ctas), st);
+                        2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(p.part[0].ctas + p.part[1].ctas), st);
     const btc_error_t rc = launch_result();
     if (rc != BTC_SUCCESS || !sums) return rc;
     // the summing kernel is set up while the first one runs and waits for its end on the device

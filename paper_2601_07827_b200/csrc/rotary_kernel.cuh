@@ -100,6 +100,7 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
     typedef typename VectorOf<VECTOR ? V * int(sizeof(T)) : 16>::type Vec;
     struct Raw { Vec a, b; };
     int ea, eb;                    // VECTOR: element offsets of the two vectors
+    uint32_t oa, ob;               // the same in bytes
     bool active, rotated;          // VECTOR: the lane has pairs; they are rotated
     int lane, pairs, rest, dim;
 
@@ -113,6 +114,9 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
             rotated = first < pairs;
             if (INTERLEAVED || !rotated) { ea = 2 * first; eb = ea + V; }
             else { ea = first; eb = first + pairs; }
+            if (!active) ea = eb = 0;      // reads what is there, counts for nothing
+            oa = uint32_t(ea) * uint32_t(sizeof(T));
+            ob = uint32_t(eb) * uint32_t(sizeof(T));
         }
     }
     __device__ __forceinline__ bool slot_rotated(int j) const { return VECTOR ? rotated : lane + 32 * j < pairs; }
@@ -129,27 +133,21 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
             b = q < rest ? 2 * pairs + rest + q : dim;
         }
     }
-    __device__ __forceinline__ static Raw zero()
+    // `base` is the same in the whole CTA and the offset of the head (bytes) has 32 bits, so that an access needs one add
+    __device__ __forceinline__ Raw load_raw(const void *base, uint32_t off = 0) const
     {
         Raw r;
-        r.a = Vec();
-        r.b = Vec();
+        r.a = *reinterpret_cast<const Vec *>(static_cast<const char *>(base) + (off + oa));
+        r.b = *reinterpret_cast<const Vec *>(static_cast<const char *>(base) + (off + ob));
         return r;
     }
-    __device__ __forceinline__ Raw load_raw(const T *row) const
-    {
-        Raw r = zero();
-        if (active) {
-            r.a = *reinterpret_cast<const Vec *>(row + ea);
-            r.b = *reinterpret_cast<const Vec *>(row + eb);
-        }
-        return r;
-    }
-    __device__ __forceinline__ void store_raw(T *row, const Raw &r) const
+    // a lane's share of a sum over the head
+    __device__ __forceinline__ float share(float2 v) const { return !VECTOR || active ? v.x + v.y : 0.f; }
+    __device__ __forceinline__ void store_raw(void *base, uint32_t off, const Raw &r) const
     {
         if (active) {
-            *reinterpret_cast<Vec *>(row + ea) = r.a;
-            *reinterpret_cast<Vec *>(row + eb) = r.b;
+            *reinterpret_cast<Vec *>(static_cast<char *>(base) + (off + oa)) = r.a;
+            *reinterpret_cast<Vec *>(static_cast<char *>(base) + (off + ob)) = r.b;
         }
     }
     // slots 2i and 2i + 1 are the halves of a[i] and b[i]
@@ -193,7 +191,8 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
             }
         }
     }
-    __device__ __forceinline__ void store(T *row, int64_t stride, const float2 (&a)[N2], const float2 (&b)[N2]) const
+    template <typename Off>
+    __device__ __forceinline__ void store(T *base, Off off, int64_t stride, const float2 (&a)[N2], const float2 (&b)[N2]) const
     {
         if constexpr (VECTOR) {
             float u[V], v[V];
@@ -211,8 +210,9 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
             Raw r;
             r.a = pack_vector<T, V>(u);
             r.b = pack_vector<T, V>(v);
-            store_raw(row, r);
+            store_raw(base, off, r);
         } else {
+            T *row = base + off;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 int e, f;
@@ -233,14 +233,15 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
         }
     }
     // (a, b) <- (a c - b s, b c + a s) with a token's angles on the rotated slots; BACK: the transposed rotation
-    template <bool BACK>
+    // (FULL: every slot of every head is rotated, nothing is asked)
+    template <bool BACK, bool FULL>
     __device__ __forceinline__ void rotate(const float *cosines, const float *sines, float2 (&a)[N2], float2 (&b)[N2]) const
     {
         float2 c[N2], s[N2];
         if constexpr (VECTOR) {
             constexpr int Q = V >= 4 ? 4 : V;
             typedef typename VectorOf<Q * 4>::type Angles;
-            if (!rotated) return;
+            if (!FULL && !rotated) return;
 #pragma unroll
             for (int i = 0; i < V / Q; ++i) {
                 const int at = i * (kRotaryMaxDim / 2 / V * Q) + lane * Q;
@@ -277,19 +278,37 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
     }
 };
 
+// sum over the lanes of a head; the same number of steps in the whole launch
 __device__ __forceinline__ float group_sum(float v, int lanes_log2)
 {
-    for (int k = 0; k < lanes_log2; ++k) v += __shfl_xor_sync(0xffffffffu, v, 1 << k);
+    if (lanes_log2 >= 4) {
+        if (lanes_log2 == 5) v += __shfl_xor_sync(0xffffffffu, v, 16);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+    }
+    if (lanes_log2 >= 3) v += __shfl_xor_sync(0xffffffffu, v, 4);
+    if (lanes_log2 >= 2) v += __shfl_xor_sync(0xffffffffu, v, 2);
+    if (lanes_log2 >= 1) v += __shfl_xor_sync(0xffffffffu, v, 1);
     return v;
 }
 
+// Offsets inside what a CTA takes at a time: the vector forms have them in bytes and 32 bits (the host checks that
+// strides are not negative and that they fit), the scalar form in elements and 64 bits
+template <typename T, int V> struct RotaryOffset {
+    typedef uint32_t type;
+    static constexpr int SCALE = int(sizeof(T));
+};
+template <typename T> struct RotaryOffset<T, 1> {
+    typedef int64_t type;
+    static constexpr int SCALE = 1;
+};
+
 // A CTA takes `cta_tokens` tokens of one part (queries, keys or values); its groups of lanes take the (token, head)
-// pairs in turn, the loads of two of them issued together.
-template <typename T, int V, bool INTERLEAVED>
+// pairs in turn, the next one's loads issued before the present one is computed.
+template <typename T, int V, bool INTERLEAVED, bool FULL>
 __global__ void __launch_bounds__(kRotaryThreads, 3) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
 {
     typedef RotaryLane<T, V, INTERLEAVED> Lane;
-    constexpr int N2 = Lane::N2, FLIGHT = 2;
+    constexpr int N2 = Lane::N2;
     __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
     const int lanes = 1 << p.lanes_log2, groups = kRotaryThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
     uint32_t cta = blockIdx.x;
@@ -299,88 +318,90 @@ __global__ void __launch_bounds__(kRotaryThreads, 3) rotary_forward_kernel(const
     const int64_t first = int64_t(cta) * part.cta_tokens;
     const int tokens = int(min(int64_t(part.cta_tokens), p.tokens - first)), heads = part.heads, items = tokens * heads;
     const bool norm = p.norm && !part.copy, turning = part.pairs > 0;
+    typedef typename RotaryOffset<T, V>::type Off;
+    constexpr int SCALE = RotaryOffset<T, V>::SCALE;
+    const Off x_t = Off(part.x_t * SCALE), x_h = Off(part.x_h * SCALE), y_t = Off(part.y_t * SCALE), y_h = Off(part.y_h * SCALE);
+    const T *x0 = static_cast<const T *>(part.x) + first * part.x_t;
+    T *y0 = static_cast<T *>(part.y) + (part.paged ? 0 : first * part.y_t);
+    const FastDiv by_heads = part.head;
+    const float inv_dim = part.inv_dim;
+    const bool copy = part.copy, paged = part.paged;
     Lane lane;
     lane.set(part, threadIdx.x & (lanes - 1));
     float2 wa[N2], wb[N2];
-    bool ready = false;
-#pragma unroll 1
-    for (int base = 0; base < items; base += FLIGHT * groups) {        // the same steps in every lane: shuffles follow
-        typename Lane::Raw raw[FLIGHT];
-        const T *src[FLIGHT];
-        int head[FLIGHT], token[FLIGHT];
+    // the (token, head) pair number `item`; past the end: the last one again, which is not stored
+    auto place = [&](int item, int &token, int &head) {
+        item = min(item, items - 1);
+        token = int(by_heads.div(uint32_t(item)));
+        head = item - token * heads;
+    };
+    int token, head;
+    place(group, token, head);
+    typename Lane::Raw ahead;
+    if constexpr (V > 1) ahead = lane.load_raw(x0, token * x_t + head * x_h);
+    // while the first loads are under way
 #pragma unroll
-        for (int i = 0; i < FLIGHT; ++i) {
-            const int item = base + i * groups + group;
-            const bool here = item < items;
-            const int t = here ? int(part.head.div(uint32_t(item))) : 0;
-            token[i] = here ? t : -1;
-            head[i] = here ? item - t * heads : 0;
-            src[i] = static_cast<const T *>(part.x) + (first + t) * part.x_t + head[i] * part.x_h;
-            if constexpr (V > 1) raw[i] = here ? lane.load_raw(src[i]) : Lane::zero();
+    for (int j = 0; j < N2; ++j) wa[j] = wb[j] = both(1.f);
+    if (norm && part.w) lane.load(static_cast<const T *>(part.w), 1, wa, wb);
+    if (turning) {
+        angles_to_shared<V>(p, first, tokens, cosines, sines);
+        __syncthreads();
+    }
+#pragma unroll 2
+    for (int item = group; item < items + group; item += groups) {      // the same steps in every lane: shuffles follow
+        const typename Lane::Raw raw = ahead;
+        int next_token, next_head;
+        place(item + groups, next_token, next_head);
+        if constexpr (V > 1) ahead = lane.load_raw(x0, next_token * x_t + next_head * x_h);
+        float2 a[N2], b[N2];
+        if constexpr (V > 1) lane.unpack(raw, a, b);
+        else lane.load(x0 + (token * x_t + head * x_h), part.x_d, a, b);
+        if (norm) {
+            float2 squares = both(0.f);
+#pragma unroll
+            for (int j = 0; j < N2; ++j) squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
+            const float ss = group_sum(lane.share(squares), p.lanes_log2);
+            const float2 r = both(rsqrtf(fmaf(ss, inv_dim, p.eps)));
+#pragma unroll
+            for (int j = 0; j < N2; ++j) {
+                a[j] = mul2(mul2(a[j], r), wa[j]);
+                b[j] = mul2(mul2(b[j], r), wb[j]);
+            }
         }
-        if (!ready) {                                                   // while the first loads are under way
-#pragma unroll
-            for (int j = 0; j < N2; ++j) wa[j] = wb[j] = both(1.f);
-            if (norm && part.w) lane.load(static_cast<const T *>(part.w), 1, wa, wb);
-            if (turning) {
-                angles_to_shared<V>(p, first, tokens, cosines, sines);
-                __syncthreads();
-            }
-            ready = true;
+        bool store = item < items;
+        T *dst = y0;
+        Off at_y = head * y_h;
+        if (paged) {
+            const int32_t slot = p.slots[first + token];
+            if (slot >= p.slot_count && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_SLOT));
+            store = store && slot >= 0 && slot < p.slot_count;
+            const uint32_t at = store ? uint32_t(slot) : 0u, page = p.page.div(at);
+            dst += int64_t(page) * part.y_page + int64_t(at - page * p.page.d) * part.y_t;
+        } else {
+            at_y += token * y_t;
         }
-#pragma unroll
-        for (int i = 0; i < FLIGHT; ++i) {
-            const bool here = token[i] >= 0;
-            float2 a[N2], b[N2];
-            if constexpr (V > 1) {
-                lane.unpack(raw[i], a, b);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N2; ++j) a[j] = b[j] = both(0.f);
-                if (here && !part.copy) lane.load(src[i], part.x_d, a, b);
+        if (copy) {
+            if (store) {
+                if constexpr (V > 1) lane.store_raw(dst, at_y, raw);
+                else lane.copy(x0 + (token * x_t + head * x_h), part.x_d, dst + at_y, part.y_d);
             }
-            if (norm) {
-                float2 squares = both(0.f);
-#pragma unroll
-                for (int j = 0; j < N2; ++j) squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
-                const float ss = group_sum(squares.x + squares.y, p.lanes_log2);
-                const float2 r = both(rsqrtf(fmaf(ss, part.inv_dim, p.eps)));
-#pragma unroll
-                for (int j = 0; j < N2; ++j) {
-                    a[j] = mul2(mul2(a[j], r), wa[j]);
-                    b[j] = mul2(mul2(b[j], r), wb[j]);
-                }
-            }
-            if (!here) continue;
-            T *dst = static_cast<T *>(part.y) + head[i] * part.y_h;
-            if (part.paged) {
-                const int32_t slot = p.slots[first + token[i]];
-                if (slot >= p.slot_count && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_SLOT));
-                if (slot < 0 || slot >= p.slot_count) continue;
-                const uint32_t page = p.page.div(uint32_t(slot));
-                dst += int64_t(page) * part.y_page + int64_t(uint32_t(slot) - page * p.page.d) * part.y_t;
-            } else {
-                dst += (first + token[i]) * part.y_t;
-            }
-            if (part.copy) {
-                if constexpr (V > 1) lane.store_raw(dst, raw[i]);
-                else lane.copy(src[i], part.x_d, dst, part.y_d);
-                continue;
-            }
-            if (turning) lane.template rotate<false>(cosines + token[i] * (kRotaryMaxDim / 2), sines + token[i] * (kRotaryMaxDim / 2), a, b);
-            lane.store(dst, part.y_d, a, b);
+        } else {
+            if (turning) lane.template rotate<false, FULL>(cosines + token * (kRotaryMaxDim / 2), sines + token * (kRotaryMaxDim / 2), a, b);
+            if (store) lane.store(dst, at_y, part.y_d, a, b);
         }
+        token = next_token;
+        head = next_head;
     }
 }
 
 // Persistent CTAs, each for one part, `cta_tokens` tokens at a time: a thread keeps its pairs (the lane's place in the
 // head never changes) and so its share of dw in registers over everything it takes; at the end the CTA's groups are
 // added in shared memory in a fixed order and the CTA writes one row of `partial`.
-template <typename T, int V, bool INTERLEAVED>
+template <typename T, int V, bool INTERLEAVED, bool FULL>
 __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
 {
     typedef RotaryLane<T, V, INTERLEAVED> Lane;
-    constexpr int N = Lane::N, N2 = Lane::N2, FLIGHT = V > 1 ? 2 : 1;
+    constexpr int N = Lane::N, N2 = Lane::N2;
     __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
     __shared__ float sums[kRotaryThreads / 32][kRotaryMaxDim];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -388,8 +409,13 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
     const int which = blockIdx.x < p.part[0].ctas ? 0 : 1;
     const RotaryPart &part = p.part[which];
     const uint32_t cta = which ? blockIdx.x - p.part[0].ctas : blockIdx.x;
+    typedef typename RotaryOffset<T, V>::type Off;
+    constexpr int SCALE = RotaryOffset<T, V>::SCALE;
     const int heads = part.heads;
-    const bool turning = p.pairs > 0;
+    const Off x_t = Off(part.x_t * SCALE), x_h = Off(part.x_h * SCALE), y_t = Off(part.y_t * SCALE), y_h = Off(part.y_h * SCALE);
+    const FastDiv by_heads = part.head;
+    const float inv_dim = part.inv_dim;
+    const bool turning = p.pairs > 0, norm = p.norm;
     Lane lane;
     lane.set(part, threadIdx.x & (lanes - 1));
     float2 wa[N2], wb[N2], da2[N2], db2[N2];
@@ -402,81 +428,74 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
 
     for (int64_t first = int64_t(cta) * part.cta_tokens; first < p.tokens; first += int64_t(part.ctas) * part.cta_tokens) {
         const int tokens = int(min(int64_t(part.cta_tokens), p.tokens - first)), items = tokens * heads;
-        bool angles_ready = !turning;
-#pragma unroll 1
-        for (int base = 0; base < items; base += FLIGHT * groups) {
-            typename Lane::Raw rx[FLIGHT], rg[FLIGHT];
-            int token[FLIGHT], head[FLIGHT];
+        const T *x0 = static_cast<const T *>(part.x) + first * part.x_t, *g0 = static_cast<const T *>(part.dy) + first * part.y_t;
+        T *d0 = static_cast<T *>(part.y) + first * part.x_t;
+        // where the (token, head) pair number `item` lies; past the end: the last one again, which is not counted
+        auto place = [&](int item, int &token, Off &at_x, Off &at_y) {
+            item = min(item, items - 1);
+            token = int(by_heads.div(uint32_t(item)));
+            const int head = item - token * heads;
+            at_x = token * x_t + head * x_h;
+            at_y = token * y_t + head * y_h;
+        };
+        int token;
+        Off at_x, at_y;
+        place(group, token, at_x, at_y);
+        typename Lane::Raw ahead_x, ahead_g;
+        if constexpr (V > 1) {
+            ahead_g = lane.load_raw(g0, at_y);
+            if (norm) ahead_x = lane.load_raw(x0, at_x);
+        }
+        if (turning) {
+            __syncthreads();                                            // the tokens before are done with
+            angles_to_shared<V>(p, first, tokens, cosines, sines);
+            __syncthreads();
+        }
+#pragma unroll 2
+        for (int item = group; item < items + group; item += groups) {
+            const typename Lane::Raw rx = ahead_x, rg = ahead_g;
+            int next_token;
+            Off next_x, next_y;
+            place(item + groups, next_token, next_x, next_y);
+            if (V > 1 && item + groups < items) {                       // past the end the values stay as they are, and count for nothing
+                ahead_g = lane.load_raw(g0, next_y);
+                if (norm) ahead_x = lane.load_raw(x0, next_x);
+            }
+            float2 ga[N2], gb[N2], a[N2], b[N2];
+            if constexpr (V > 1) {
+                lane.unpack(rg, ga, gb);
+                if (norm) lane.unpack(rx, a, b);
+            } else {
+                lane.load(g0 + at_y, part.y_d, ga, gb);
+                if (norm) lane.load(x0 + at_x, part.x_d, a, b);
+            }
+            if (turning) lane.template rotate<true, FULL>(cosines + token * (kRotaryMaxDim / 2), sines + token * (kRotaryMaxDim / 2), ga, gb);
+            if (norm) {
+                // with g = dm w:  dx = r (g - x r^2 mean(g x)),  dw += dm x r
+                float2 squares = both(0.f), dots = both(0.f), pa[N2], pb[N2];
 #pragma unroll
-            for (int i = 0; i < FLIGHT; ++i) {
-                const int item = base + i * groups + group;
-                const bool here = item < items;
-                const int t = here ? int(part.head.div(uint32_t(item))) : 0;
-                token[i] = here ? t : -1;
-                head[i] = here ? item - t * heads : 0;
-                if constexpr (V > 1) {
-                    rx[i] = rg[i] = Lane::zero();
-                    if (here) {
-                        rg[i] = lane.load_raw(static_cast<const T *>(part.dy) + (first + t) * part.y_t + head[i] * part.y_h);
-                        if (p.norm) rx[i] = lane.load_raw(static_cast<const T *>(part.x) + (first + t) * part.x_t + head[i] * part.x_h);
-                    }
+                for (int j = 0; j < N2; ++j) {
+                    squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
+                    pa[j] = mul2(ga[j], wa[j]);
+                    pb[j] = mul2(gb[j], wb[j]);
+                    dots = fma2(pa[j], a[j], fma2(pb[j], b[j], dots));
+                }
+                const float ss = group_sum(lane.share(squares), p.lanes_log2), dot = group_sum(lane.share(dots), p.lanes_log2);
+                const float r = rsqrtf(fmaf(ss, inv_dim, p.eps));
+                const float2 r2 = both(r), pull = both(-(dot * r * inv_dim) * r * r);  // x pull = -n r mean(g n)
+                const float2 counted = both(item < items ? r : 0.f);
+#pragma unroll
+                for (int j = 0; j < N2; ++j) {
+                    da2[j] = fma2(ga[j], mul2(a[j], counted), da2[j]);
+                    db2[j] = fma2(gb[j], mul2(b[j], counted), db2[j]);
+                    ga[j] = fma2(pa[j], r2, mul2(a[j], pull));
+                    gb[j] = fma2(pb[j], r2, mul2(b[j], pull));
                 }
             }
-            if (!angles_ready) {
-                __syncthreads();                                        // the tokens before are done with
-                angles_to_shared<V>(p, first, tokens, cosines, sines);
-                __syncthreads();
-                angles_ready = true;
-            }
-#pragma unroll
-            for (int i = 0; i < FLIGHT; ++i) {
-                const bool here = token[i] >= 0;
-                const int64_t t = first + (here ? token[i] : 0);
-                float2 ga[N2], gb[N2], a[N2], b[N2];
-                if constexpr (V > 1) {
-                    lane.unpack(rg[i], ga, gb);
-                    if (p.norm) lane.unpack(rx[i], a, b);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < N2; ++j) a[j] = b[j] = ga[j] = gb[j] = both(0.f);
-                    if (here) {
-                        lane.load(static_cast<const T *>(part.dy) + t * part.y_t + head[i] * part.y_h, part.y_d, ga, gb);
-                        if (p.norm) lane.load(static_cast<const T *>(part.x) + t * part.x_t + head[i] * part.x_h, part.x_d, a, b);
-                    }
-                }
-                if (turning) {
-                    const int at = (here ? token[i] : 0) * (kRotaryMaxDim / 2);
-                    lane.template rotate<true>(cosines + at, sines + at, ga, gb);
-                }
-                if (p.norm) {
-                    // with g = dm w:  dx = r (g - x r^2 mean(g x)),  dw += dm x r
-                    float2 squares = both(0.f), dots = both(0.f), pa[N2], pb[N2];
-#pragma unroll
-                    for (int j = 0; j < N2; ++j) {
-                        squares = fma2(a[j], a[j], fma2(b[j], b[j], squares));
-                        pa[j] = mul2(ga[j], wa[j]);
-                        pb[j] = mul2(gb[j], wb[j]);
-                        dots = fma2(pa[j], a[j], fma2(pb[j], b[j], dots));
-                    }
-                    float ss = squares.x + squares.y, dot = dots.x + dots.y;
-                    for (int k = 0; k < p.lanes_log2; ++k) {
-                        ss += __shfl_xor_sync(0xffffffffu, ss, 1 << k);
-                        dot += __shfl_xor_sync(0xffffffffu, dot, 1 << k);
-                    }
-                    const float r = here ? rsqrtf(fmaf(ss, part.inv_dim, p.eps)) : 0.f;   // 0: nothing is added to dw
-                    const float2 r2 = both(r), pull = both(-(dot * r * part.inv_dim) * r);  // -r mean(g n)
-#pragma unroll
-                    for (int j = 0; j < N2; ++j) {
-                        a[j] = mul2(a[j], r2);                                             // n
-                        b[j] = mul2(b[j], r2);
-                        da2[j] = fma2(ga[j], a[j], da2[j]);
-                        db2[j] = fma2(gb[j], b[j], db2[j]);
-                        ga[j] = fma2(pa[j], r2, mul2(a[j], pull));
-                        gb[j] = fma2(pb[j], r2, mul2(b[j], pull));
-                    }
-                }
-                if (here) lane.store(static_cast<T *>(part.y) + t * part.x_t + head[i] * part.x_h, part.x_d, ga, gb);
-            }
+            if (item < items) lane.store(d0, at_x, part.x_d, ga, gb);
+            token = next_token;
+            at_x = next_x;
+            at_y = next_y;
         }
     }
     if (!p.norm || !p.partial) return;

@@ -56,19 +56,24 @@ btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t 
         }
         configured[slot].store(true, std::memory_order_relaxed);
     }
-    paged_attention_kernel<T, DP, NT><<<unsigned(ctas), Shape::WARPS * 32, Shape::SMEM, st>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return BTC_ERR_CUDA;
-    // the joining kernel is set up while the first one runs and waits for its end on the device
+    // both kernels are set up while the one before them in the stream runs, and wait for its end on the device
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(ctas));
-    cfg.blockDim = dim3(kJoinThreads);
+    cfg.blockDim = dim3(Shape::WARPS * 32);
+    cfg.dynamicSmemBytes = Shape::SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, DP, NT>, p, ctas) != cudaSuccess) {
+    cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, DP, NT>, p);
+    if (e == cudaSuccess) {
+        cfg.blockDim = dim3(kJoinThreads);
+        cfg.dynamicSmemBytes = 0;
+        e = cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, DP, NT>, p, ctas);
+    }
+    if (e != cudaSuccess) {
         cudaGetLastError();
         return BTC_ERR_CUDA;
     }

@@ -104,12 +104,12 @@ __device__ __forceinline__ void mma8_tf32(float (&c)[4], const uint32_t (&a)[4],
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x = hi + lo with hi rounded to TF32's 11 significant bits (so that |lo| <= 2^-11 |x|); the tensor core ignores the
-// low 13 bits of what it is given, hence lo is rounded by adding half a unit: 2^-22 |x| is left out
+// x = hi + lo with hi rounded to TF32's 11 significant bits, so that |lo| <= 2^-11 |x|; of lo the tensor core takes
+// the leading 11 bits (it ignores the low 13 of what it is given): at most 2^-21 |x| is left out
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t &hi, uint32_t &lo)
 {
     hi = (x + 0x1000u) & 0xffffe000u;
-    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
+    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
 }
 // the products with x0, x1: lo * hi, hi * lo and hi * hi, each into an accumulator
 __device__ __forceinline__ void mma8_split(float (&c_lh)[4], float (&c_hl)[4], float (&c_hh)[4], const uint32_t (&ah)[4],
@@ -580,7 +580,9 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int head_blocks = p.key_heads * p.blocks;
 
-    // the combining kernel may set itself up while this one runs
+    // launched while the kernel before it may still run: nothing is read or written before that has ended; the joining
+    // kernel in turn is set up while this one runs
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // tiles of all sequences: thread i sums sequences [i * per, (i + 1) * per), then a prefix sum over the threads
@@ -678,8 +680,8 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         uint32_t seen[STAGES];
 #pragma unroll
         for (int k = 0; k < STAGES; ++k) seen[k] = 0;
-        w.begin_item(cur);
         bool began_here = cur.tile == 0;                        // the current item's first tile is in this warp's range
+        w.begin_item(cur);
         int stage = 0, into = 0;
         // one step: start the copies of tile i + STAGES - 1, consume tile i (the first STAGES - 1 steps only copy)
         for (int64_t i = 1 - STAGES; i < n; ++i) {
@@ -813,6 +815,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
     __shared__ float4 sums[SPLIT - 1][QUADS];
     const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t item = p.partial_item[2 * c + 1];
     if (item < 0) return;
     if (tid == 0) parts = ctas - c;

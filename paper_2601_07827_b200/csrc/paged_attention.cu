@@ -24,7 +24,7 @@ namespace {
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : 2; }
 
 // CTAs of the first kernel: one per SM (shared memory admits no second)
-int ctas_of(const btc_paged_attention_s &op) { return std::min(op.handle.sm_count, kJoinMaxCtas); }
+int ctas_of(const btc_paged_attention_s &op) { return op.handle.sm_count; }
 
 int64_t slot_floats(const btc_paged_attention_s &op) { return int64_t(8 * op.nt) * op.dp + 16 * op.nt; }
 
@@ -69,6 +69,7 @@ btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t 
     cfg.numAttrs = 1;
     cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, DP, NT>, p);
     if (e == cudaSuccess) {
+        cfg.gridDim = dim3(unsigned(ctas), kJoinSlices);
         cfg.blockDim = dim3(kJoinThreads);
         cfg.dynamicSmemBytes = 0;
         e = cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, DP, NT>, p, ctas);

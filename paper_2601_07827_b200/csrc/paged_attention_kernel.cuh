@@ -73,6 +73,10 @@ template <typename T> struct AttentionBias { static constexpr float value = 0.f;
 // 2^-24 of the largest stay normal numbers
 template <> struct AttentionBias<__half> { static constexpr float value = 10.f; };
 
+// The code of a kernel that runs for a few microseconds is fetched as it goes: a jump over code that is not needed costs
+// about a third of a microsecond.  What is rarely needed is marked so that it is put out of the way.
+__device__ __forceinline__ bool rare(bool x) { return __builtin_expect(x, 0); }
+
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], unsigned addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -143,6 +147,13 @@ struct AttentionSpan {
     }
 };
 
+// n / d for n >= 0 and d > 0; a 64-bit division is several times as long as a 32-bit one
+__device__ __forceinline__ int64_t divide(int64_t n, int32_t d)
+{
+    if (__builtin_expect(n >= (int64_t(1) << 31), 0)) return n / d;
+    return int64_t(uint32_t(n) / uint32_t(d));
+}
+
 // A place in the list of tiles: sequence, head block, tile; the same in every lane.
 struct AttentionCursor {
     int32_t seq, hb, tile;                   // tile counted from the span's first
@@ -189,7 +200,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         const uint32_t j = p.page.div(uint32_t(t));
         row = t - int32_t(j * p.page.d);
         const int32_t page = p.table[c.seq * p.table_n + int64_t(j) * p.table_j];
-        if (page < 0 || page >= p.pages) {
+        if (rare(page < 0 || page >= p.pages)) {
             if (p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
             return -1;
         }
@@ -391,7 +402,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) odd |= s[nt][j] != s[nt][j];
-            if (__any_sync(0xffffffffu, odd)) {
+            if (rare(__any_sync(0xffffffffu, odd))) {
                 int count;
                 const int h0 = first_head(cur, count);
                 float again[NT][4];
@@ -545,7 +556,11 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 };
 
 // what a part with maximum m counts in a whole with maximum top >= m (a part that saw nothing has m = -inf and o = l = 0)
-__device__ __forceinline__ float join_weight(float m, float top) { return m == top ? 1.f : exp2f(m - top); }
+__device__ __forceinline__ float join_weight(float m, float top)
+{
+    const float w = exp2f(m - top);          // NaN where both are infinite
+    return m == top ? 1.f : w;
+}
 
 // elements d..d+3 of head h of an item (8 NT = `per` heads) from its joined sums
 template <typename T>
@@ -575,6 +590,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ float stats[2 * W][2 * H];
     __shared__ int32_t dep_item[2 * W];
+    __shared__ uint32_t item_ends;
     __shared__ int32_t first_item, last_item;                  // items of the CTA's range that it does not hold whole; -1: none
     int64_t *scan = reinterpret_cast<int64_t *>(smem + W * Shape::RING);     // until the ranges are known
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -596,7 +612,8 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
             AttentionSpan span;
             span.set(p, length);
             mine += span.tiles;
-            if (blockIdx.x == 0 && p.flags && (length < 0 || length > p.room)) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+            if (rare(length < 0 || length > p.room))
+                if (blockIdx.x == 0 && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
         int64_t x = mine;
 #pragma unroll
@@ -614,27 +631,13 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         scan[tid + 1] = x + before;
         __syncthreads();
     }
-    // sequences with nothing to see
-    for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
-        AttentionSpan span;
-        span.set(p, p.lengths[s]);
-        if (span.tiles == 0) {
-            for (int e = tid; e < p.heads * p.dim_v; e += THREADS) {
-                const int h = e / p.dim_v, d = e - h * p.dim_v;
-                static_cast<T *>(p.o)[s * p.o_n + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
-            }
-            if (p.lse)
-                for (int h = tid; h < p.heads; h += THREADS) p.lse[int64_t(s) * p.heads + h] = -INFINITY;
-        }
-    }
-
     // equal ranges of the list of tiles, at least one tile per warp of the CTAs that take part
     const int64_t total = scan[THREADS] * head_blocks;
     int64_t ctas = (total + W - 1) / W;
     if (ctas > gridDim.x) ctas = gridDim.x;
     int64_t lo = 0, hi = 0, cta_lo = 0, cta_hi = 0;
     if (blockIdx.x < ctas) {
-        const int64_t each = total / ctas, more = total - each * ctas;
+        const int64_t each = divide(total, int32_t(ctas)), more = total - each * ctas;
         cta_lo = each * blockIdx.x + min(int64_t(blockIdx.x), more);
         cta_hi = cta_lo + each + (int64_t(blockIdx.x) < more ? 1 : 0);
         const int64_t n = cta_hi - cta_lo, we = n / W, wm = n - we * W;
@@ -661,7 +664,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
             at -= int64_t(cur.span.tiles) * head_blocks;
             cur.span.set(p, p.lengths[++cur.seq]);
         }
-        cur.hb = int32_t(at / cur.span.tiles);
+        cur.hb = int32_t(divide(at, cur.span.tiles));
         cur.tile = int32_t(at - int64_t(cur.hb) * cur.span.tiles);
         cur.key_head = cur.hb / p.blocks;
         cur.block = cur.hb - cur.key_head * p.blocks;
@@ -733,131 +736,204 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     }
     __syncthreads();
 
-    float (*joined)[2 * H] = reinterpret_cast<float (*)[2 * H]>(smem + Shape::DEPOSIT);     // behind warp 0's deposit in its ring
-    float (*weight)[H] = reinterpret_cast<float (*)[H]>(smem + Shape::DEPOSIT + 2 * W * 2 * H * 4);
-    // join what the warps left: first each deposit's weight against the largest maximum of its item (a warp takes a
-    // head, a lane a deposit; the deposits of an item are neighbours) ...
     if (tid < 2) p.partial_item[2 * blockIdx.x + tid] = tid == 0 ? first_item : (last_item == first_item ? -1 : last_item);
-    if (blockIdx.x >= ctas) return;
-    for (int h = warp; h < H; h += W) {
-        const bool mine = lane < 2 * W && dep_item[lane < 2 * W ? lane : 0] >= 0;
-        const int32_t item = mine ? dep_item[lane] : -1 - lane;
-        const float m = mine ? stats[lane][h] : -INFINITY, l = mine ? stats[lane][H + h] : 0.f;
-        float top = m;
+    if (blockIdx.x < ctas) {
+        // join what the warps left: first each deposit's weight against the largest maximum of its item (a warp takes a
+        // head, a lane a deposit; the deposits of an item are neighbours), 0 where there is none, and the places
+        // where the items end ...
+        float (*joined)[2 * H] = reinterpret_cast<float (*)[2 * H]>(smem + Shape::DEPOSIT);     // behind warp 0's deposit in its ring
+        float (*weight)[H] = reinterpret_cast<float (*)[H]>(smem + Shape::DEPOSIT + 2 * W * 2 * H * 4);
+        for (int h = warp; h < H; h += W) {
+            const int at = lane < 2 * W ? lane : 0;
+            const int32_t item = lane < 2 * W ? dep_item[at] : -1;
+            const bool mine = item >= 0;
+            const float m = mine ? stats[at][h] : -INFINITY, l = mine ? stats[at][H + h] : 0.f;
+            const uint32_t same = __match_any_sync(0xffffffffu, mine ? item : -1 - lane);
+            float top = m;
 #pragma unroll
-        for (int j = 0; j < 2 * W; ++j) {
-            const float x = __shfl_sync(0xffffffffu, m, j);
-            if (__shfl_sync(0xffffffffu, item, j) == item) top = fmaxf(top, x);
-        }
-        const float share = join_weight(m, top);
-        float sum = 0.f;
+            for (int j = 0; j < 2 * W; ++j) {
+                const float x = __shfl_sync(0xffffffffu, m, j);
+                if ((same >> j) & 1) top = fmaxf(top, x);
+            }
+            const float share = mine ? join_weight(m, top) : 0.f;
+            float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 2 * W; ++j) {
-            const float x = __shfl_sync(0xffffffffu, l * share, j);
-            if (__shfl_sync(0xffffffffu, item, j) == item) sum += x;
+            for (int j = 0; j < 2 * W; ++j) {
+                const float x = __shfl_sync(0xffffffffu, l * share, j);
+                if ((same >> j) & 1) sum += x;
+            }
+            if (lane < 2 * W) {
+                weight[lane][h] = share;
+                joined[lane][h] = top;
+                joined[lane][H + h] = sum;
+            }
+            if (h == 0) {
+                const uint32_t ends = __ballot_sync(0xffffffffu, mine && (same >> lane) == 1);    // the last deposit of its item
+                if (lane == 0) item_ends = ends;
+            }
         }
-        if (mine) {
-            weight[lane][h] = share;
-            joined[lane][h] = top;
-            joined[lane][H + h] = sum;
+        __syncthreads();
+        // ... then the sums, four elements of a head per thread
+        for (int e = 4 * tid; e < H * DP; e += 4 * THREADS) {
+            const int h = e / DP, d = e - h * DP;
+            int begin = 0;
+            for (uint32_t ends = item_ends; ends; ends &= ends - 1) {
+                const int last = __ffs(int(ends)) - 1;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int i = begin; i <= last; ++i) {
+                    const unsigned char *src = (i & 1) ? smem + (i >> 1) * Shape::RING : smem + W * Shape::RING + (i >> 1) * Shape::DEPOSIT;
+                    const float4 x = reinterpret_cast<const float4 *>(src)[e / 4];
+                    const float share = weight[i][h];
+                    if (share != 0.f) {                            // no deposit there, or one that does not count
+                        o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
+                    }
+                }
+                const int32_t item = dep_item[last];
+                const float m = joined[last][h], l = joined[last][H + h];
+                if (item == first_item || item == last_item) {
+                    float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * (H * DP + 2 * H);
+                    *reinterpret_cast<float4 *>(out + e) = o;
+                    if (d == 0) { out[H * DP + h] = m; out[H * DP + H + h] = l; }
+                } else {
+                    write_joined<T>(p, item, H, h, d, o, m, l);
+                }
+                begin = last + 1;
+            }
         }
     }
-    __syncthreads();
-    // ... then the sums, four elements of a head per thread
-    for (int e = 4 * tid; e < H * DP; e += 4 * THREADS) {
-        const int h = e / DP, d = e - h * DP;
-        int32_t item = -1;
-        int last = 0;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto flush = [&]() {
-            if (item < 0) return;
-            const float m = joined[last][h], l = joined[last][H + h];
-            if (item == first_item || item == last_item) {
-                float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * (H * DP + 2 * H);
-                *reinterpret_cast<float4 *>(out + e) = o;
-                if (d == 0) { out[H * DP + h] = m; out[H * DP + H + h] = l; }
-            } else {
-                write_joined<T>(p, item, H, h, d, o, m, l);
+    // sequences with nothing to see
+    for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
+        AttentionSpan span;
+        span.set(p, p.lengths[s]);
+        if (rare(span.tiles == 0)) {
+            for (int e = tid; e < p.heads * p.dim_v; e += THREADS) {
+                const int h = e / p.dim_v, d = e - h * p.dim_v;
+                static_cast<T *>(p.o)[s * p.o_n + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
             }
-        };
-#pragma unroll 1
-        for (int i = 0; i < 2 * W; ++i) {
-            const int32_t here = dep_item[i];
-            if (here < 0) continue;
-            if (here != item) {
-                flush();
-                item = here;
-                o = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            const unsigned char *src = (i & 1) ? smem + (i >> 1) * Shape::RING : smem + W * Shape::RING + (i >> 1) * Shape::DEPOSIT;
-            const float4 x = reinterpret_cast<const float4 *>(src)[e / 4];
-            const float share = weight[i][h];
-            o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
-            last = i;
+            if (p.lse)
+                for (int h = tid; h < p.heads; h += THREADS) p.lse[int64_t(s) * p.heads + h] = -INFINITY;
         }
-        flush();
     }
 }
 
-// Items that span CTAs: block c joins the item that begins in CTA c's range and ends in a later one's: CTA c's
-// second slot, then the first slots of the CTAs after it while they carry the same item.  A thread takes four
-// elements of a head; the threads beyond the elements split the parts among them, so that a long sequence alone
-// (148 parts) is a few rounds of loads.
-constexpr int kJoinMaxCtas = 1024, kJoinThreads = 1024;
+// loads that stay where they are written: ahead of the branches and barriers that come before their use
+__device__ __forceinline__ int32_t load_now(const int32_t *p)
+{
+    int32_t v;
+    asm volatile("ld.global.cg.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float load_now(const float *p)
+{
+    float v;
+    asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 load_now(const float4 *p)
+{
+    float4 v;
+    asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+// Items that span CTAs: the blocks (c, slice) join the item that begins in CTA c's range and ends in a later one's: CTA
+// c's second slot, then the first slots of the CTAs after it while they carry the same item.  A block takes a quarter
+// of the heads, a thread four elements of one; the threads beyond the elements split the parts among them, so
+// that a long sequence alone (148 parts) is a few rounds of loads.
+constexpr int kJoinThreads = 256, kJoinSlices = 4;
 template <typename T, int DP, int NT>
 __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const __grid_constant__ AttentionParams p, int ctas)
 {
-    constexpr int H = 8 * NT, QUADS = H * DP / 4, SPLIT = kJoinThreads / QUADS;
+    constexpr int H = 8 * NT, HEADS = H / kJoinSlices, QUADS = HEADS * DP / 4, SPLIT = kJoinThreads / QUADS, AHEAD = 16 / SPLIT;
     constexpr int64_t slot_floats = H * DP + 2 * H;
-    static_assert(QUADS * SPLIT <= kJoinThreads && SPLIT >= 2, "");
+    static_assert(QUADS * SPLIT <= kJoinThreads && SPLIT >= 2 && HEADS <= kJoinThreads / 32, "");
     __shared__ int32_t parts;
-    __shared__ float tops[H], totals[H];
+    __shared__ float tops[HEADS], totals[HEADS];
     __shared__ float4 sums[SPLIT - 1][QUADS];
-    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+    const int c = blockIdx.x, h0 = blockIdx.y * HEADS, tid = threadIdx.x, lane = tid & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int32_t item = p.partial_item[2 * c + 1];
+    const int32_t item = load_now(p.partial_item + 2 * c + 1);
     if (item < 0) return;
-    if (tid == 0) parts = ctas - c;
-    __syncthreads();
-    // part 0 is CTA c's second slot, part i CTA c + i's first; the first CTA without the item ends it
-    for (int i = tid + 1; i < ctas - c; i += kJoinThreads)
-        if (p.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
-    __syncthreads();
-    const int n = parts;
+    // Part 0 is CTA c's second slot, part i CTA c + i's first; the first CTA without the item ends it.  How many parts there
+    // are is known one round trip to memory later: what the first 32 (a warp's maxima and sums) and the first 16
+    // (a thread's elements) hold is loaded before that.
+    const int left = ctas - c;
     const float *first = p.partial + 2 * int64_t(c) * slot_floats;
     auto part = [&](int i) { return first + (i == 0 ? slot_floats : 2 * int64_t(i) * slot_floats); };
+    const int split = tid / QUADS, quad = tid - split * QUADS, k = quad * 4 / DP, h = h0 + k, d = quad * 4 - k * DP;
+    const int32_t other = tid + 1 < left ? load_now(p.partial_item + 2 * (c + tid + 1)) : -1;
+    float m0 = -INFINITY, l0 = 0.f;
+    if (tid / 32 < HEADS && lane < left) {
+        m0 = load_now(part(lane) + H * DP + h0 + tid / 32);
+        l0 = load_now(part(lane) + H * DP + H + h0 + tid / 32);
+    }
+    float4 ahead[AHEAD];
+    float ahead_m[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+        const int i = split + j * SPLIT;
+        ahead[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        ahead_m[j] = -INFINITY;
+        if (split < SPLIT && i < left) {
+            ahead[j] = load_now(reinterpret_cast<const float4 *>(part(i) + h0 * DP + quad * 4));
+            ahead_m[j] = load_now(part(i) + H * DP + h);
+        }
+    }
+    if (tid == 0) parts = left;
+    __syncthreads();
+    if (tid + 1 < left && other != item) atomicMin(&parts, tid + 1);
+    if (rare(left > kJoinThreads))
+        for (int i = tid + 1 + kJoinThreads; i < left; i += kJoinThreads)
+            if (p.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
+    __syncthreads();
+    const int n = parts;
     // a warp takes a head's maxima and sums
-    for (int h = tid / 32; h < H; h += kJoinThreads / 32) {
-        float top = -INFINITY;
-        for (int i = lane; i < n; i += 32) top = fmaxf(top, part(i)[H * DP + h]);
-        for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-        float l = 0.f;
-        for (int i = lane; i < n; i += 32) l = fmaf(part(i)[H * DP + H + h], join_weight(part(i)[H * DP + h], top), l);
-        for (int k = 1; k < 32; k <<= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
-        if (lane == 0) { tops[h] = top; totals[h] = l; }
+    if (tid / 32 < HEADS) {
+        const int at = H * DP + h0 + tid / 32;
+        float top = lane < n ? m0 : -INFINITY;
+        if (rare(n > 32)) {
+#pragma unroll 1
+            for (int i = lane + 32; i < n; i += 32) top = fmaxf(top, part(i)[at]);
+        }
+#pragma unroll
+        for (int j = 1; j < 32; j <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, j));
+        float l = lane < n ? l0 * join_weight(m0, top) : 0.f;
+        if (rare(n > 32)) {
+#pragma unroll 1
+            for (int i = lane + 32; i < n; i += 32) l = fmaf(part(i)[at + H], join_weight(part(i)[at], top), l);
+        }
+#pragma unroll
+        for (int j = 1; j < 32; j <<= 1) l += __shfl_xor_sync(0xffffffffu, l, j);
+        if (lane == 0) { tops[tid / 32] = top; totals[tid / 32] = l; }
     }
     __syncthreads();
-    const int split = tid / QUADS, quad = tid - split * QUADS, h = quad * 4 / DP, d = quad * 4 - h * DP;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     if (split < SPLIT) {
-        const float top = tops[h];
-#pragma unroll 4
-        for (int i = split; i < n; i += SPLIT) {
-            const float4 x = *reinterpret_cast<const float4 *>(part(i) + quad * 4);
-            const float share = join_weight(part(i)[H * DP + h], top);
+        const float top = tops[k];
+        auto add = [&](const float4 &x, float m) {
+            const float share = join_weight(m, top);
             o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
+        };
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (split + j * SPLIT < n) add(ahead[j], ahead_m[j]);
+        if (rare(n > AHEAD * SPLIT)) {
+#pragma unroll 4
+            for (int i = split + AHEAD * SPLIT; i < n; i += SPLIT)
+                add(*reinterpret_cast<const float4 *>(part(i) + h0 * DP + quad * 4), part(i)[H * DP + h]);
         }
         if (split > 0) sums[split - 1][quad] = o;
     }
     __syncthreads();
     if (split > 0) return;
 #pragma unroll
-    for (int k = 0; k < SPLIT - 1; ++k) {
-        const float4 x = sums[k][quad];
+    for (int j = 0; j < SPLIT - 1; ++j) {
+        const float4 x = sums[j][quad];
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
-    write_joined<T>(p, item, H, h, d, o, tops[h], totals[h]);
+    write_joined<T>(p, item, H, h, d, o, tops[k], totals[k]);
 }
 
 }  // namespace btc

@@ -114,10 +114,29 @@ void fill_workspace(const btc_pages_s &op, void *workspace, PagesParams &p)
     p.begin = reinterpret_cast<int64_t *>(base + w.begin);
 }
 
+// One launch that may be set up while the kernel before it in the stream runs (the kernels wait on the device).
+template <typename... Args, typename... Given>
+btc_error_t launch_early(void (*kernel)(Args...), unsigned blocks, unsigned threads, cudaStream_t st, Given &&...given)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, Args(given)...) != cudaSuccess) {
+        cudaGetLastError();
+        return BTC_ERR_CUDA;
+    }
+    return BTC_SUCCESS;
+}
+
 // Launches the copies (and the renumbering when p.table is set).  `pairs_most`: as many pairs as there can be.
-// `dependent`: the kernel before it in the stream makes the list; this one is set up while that runs.
 btc_error_t launch_copies(const btc_pages_s &op, PagesCopyParams &p, void *const *tensors, int32_t count, int64_t pairs_most,
-                          bool dependent, cudaStream_t st)
+                          cudaStream_t st)
 {
     const int32_t layouts = int32_t(op.layouts.size());
     // the largest unit that every run, stride and address of this call allows (pages whose smallest stride is not one
@@ -162,26 +181,14 @@ btc_error_t launch_copies(const btc_pages_s &op, PagesCopyParams &p, void *const
         __int128 steps = __int128(pairs_most) * (n / layouts) * p.chunks;
         if (p.table) steps = std::max<__int128>(steps, (__int128(p.sequences) * p.columns + kPagesCopyThreads - 1) / kPagesCopyThreads);
         const int64_t blocks = int64_t(std::max<__int128>(1, std::min<__int128>(steps, most)));
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(unsigned(blocks));
-        cfg.blockDim = dim3(kPagesCopyThreads);
-        cfg.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = dependent && at == 0 ? 1 : 0;
-        cudaError_t e = cudaSuccess;
+        btc_error_t rc;
         switch (unit) {
-        case 16: e = cudaLaunchKernelEx(&cfg, pages_copy_kernel<uint4>, p); break;
-        case 8: e = cudaLaunchKernelEx(&cfg, pages_copy_kernel<uint2>, p); break;
-        case 4: e = cudaLaunchKernelEx(&cfg, pages_copy_kernel<uint32_t>, p); break;
-        default: e = cudaLaunchKernelEx(&cfg, pages_copy_kernel<uint16_t>, p); break;
+        case 16: rc = launch_early(pages_copy_kernel<uint4>, unsigned(blocks), kPagesCopyThreads, st, p); break;
+        case 8: rc = launch_early(pages_copy_kernel<uint2>, unsigned(blocks), kPagesCopyThreads, st, p); break;
+        case 4: rc = launch_early(pages_copy_kernel<uint32_t>, unsigned(blocks), kPagesCopyThreads, st, p); break;
+        default: rc = launch_early(pages_copy_kernel<uint16_t>, unsigned(blocks), kPagesCopyThreads, st, p); break;
         }
-        if (e != cudaSuccess) {
-            cudaGetLastError();
-            return BTC_ERR_CUDA;
-        }
+        if (rc != BTC_SUCCESS) return rc;
         p.table = nullptr;                 // renumbered once
         at += n;
     } while (at < count);
@@ -263,13 +270,12 @@ btc_error_t btc_pages_extend(btc_pages_t op, void *cuda_stream, const int32_t *n
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
     p.fresh = new_tokens; p.slots = slots; p.most = max_new;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    pages_extend_kernel<<<kPagesCluster, kPagesThreads, 0, st>>>(p);
-    rc = launch_result();
+    rc = launch_early(pages_extend_kernel, kPagesCluster, kPagesThreads, st, p);
     if (rc != BTC_SUCCESS || count == 0) return rc;
     PagesCopyParams c;
     std::memset(static_cast<void *>(&c), 0, sizeof c);
     c.pairs = p.pairs; c.count = p.count; c.pages = p.pages; c.flags = flags;
-    return launch_copies(*op, c, tensors, count, op->sequences, true, st);
+    return launch_copies(*op, c, tensors, count, op->sequences, st);
 }
 
 btc_error_t btc_pages_fork(btc_pages_t op, void *cuda_stream, const int32_t *src, const int32_t *dst, int32_t count,
@@ -282,8 +288,7 @@ btc_error_t btc_pages_fork(btc_pages_t op, void *cuda_stream, const int32_t *src
     PagesParams p;
     fill_state(*op, p);
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
-    pages_fork_kernel<<<unsigned(count), 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, src, dst);
-    return launch_result();
+    return launch_early(pages_fork_kernel, unsigned(count), 128, static_cast<cudaStream_t>(cuda_stream), p, src, dst);
 }
 
 btc_error_t btc_pages_free(btc_pages_t op, void *cuda_stream, const int32_t *sequences, int32_t count, int32_t *table,
@@ -296,8 +301,7 @@ btc_error_t btc_pages_free(btc_pages_t op, void *cuda_stream, const int32_t *seq
     PagesParams p;
     fill_state(*op, p);
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
-    pages_free_kernel<<<unsigned(count), 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, sequences);
-    return launch_result();
+    return launch_early(pages_free_kernel, unsigned(count), 128, static_cast<cudaStream_t>(cuda_stream), p, sequences);
 }
 
 btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table, int32_t *refs, void *const *tensors,
@@ -315,15 +319,14 @@ btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table,
     fill_workspace(*op, workspace, p);
     p.table = table; p.refs = refs; p.flags = flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    pages_compact_kernel<<<kPagesCluster, kPagesThreads, 0, st>>>(p);
-    rc = launch_result();
+    rc = launch_early(pages_compact_kernel, kPagesCluster, kPagesThreads, st, p);
     if (rc != BTC_SUCCESS) return rc;
     PagesCopyParams c;
     std::memset(static_cast<void *>(&c), 0, sizeof c);
     c.pairs = p.pairs; c.count = p.count; c.pages = p.pages; c.flags = flags;
     c.table = table; c.map = p.map; c.live = p.count + 1;
     c.table_n = p.table_n; c.table_j = p.table_j; c.sequences = p.sequences; c.columns = p.columns;
-    return launch_copies(*op, c, tensors, count, op->pages / 2, true, st);
+    return launch_copies(*op, c, tensors, count, op->pages / 2, st);
 }
 
 btc_error_t btc_pages_copy(btc_pages_t op, void *cuda_stream, const int32_t *pairs, int32_t pair_count,
@@ -338,7 +341,7 @@ btc_error_t btc_pages_copy(btc_pages_t op, void *cuda_stream, const int32_t *pai
     PagesCopyParams c;
     std::memset(static_cast<void *>(&c), 0, sizeof c);
     c.pairs = pairs; c.most = pair_count; c.pages = int32_t(op->pages); c.flags = flags;
-    return launch_copies(*op, c, tensors, count, pair_count, false, static_cast<cudaStream_t>(cuda_stream));
+    return launch_copies(*op, c, tensors, count, pair_count, static_cast<cudaStream_t>(cuda_stream));
 }
 
 }  // extern "C"

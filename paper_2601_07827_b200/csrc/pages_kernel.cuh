@@ -77,6 +77,13 @@ __device__ __forceinline__ int64_t pages_peer_value(const int64_t *mine, unsigne
     asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
     return v;
 }
+// Every kernel here may be launched while the one before it in the stream still runs (its set-up is then hidden): it
+// touches nothing before that one has ended, and lets the next one do the same.
+__device__ __forceinline__ void pages_begin()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 __device__ __forceinline__ void pages_flag(int32_t *flags, int what)
 {
     if (flags) atomicOr(flags, what);
@@ -138,20 +145,23 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
 {
     __shared__ int64_t scratch[33], totals[3];           // totals: free pages, pages wanted, copies of this CTA
     const unsigned rank = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     const bool vec = (reinterpret_cast<uintptr_t>(p.refs) & 15) == 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    pages_begin();
 
-    // free pages of this CTA's share
+    // free pages of this CTA's share; the first four of a thread stay in registers (`head`: all, in pools of up to 32768)
     int32_t lo, hi;
     pool_share(p.pages, rank, lo, hi);
-    int64_t mine = 0;
-    for (int32_t at = lo + 4 * tid; at < hi; at += 4 * kPagesThreads) {
+    const int4 head = four_refs(p.refs, lo + 4 * tid, hi, vec);
+    const int head_free = (head.x == 0) + (head.y == 0) + (head.z == 0) + (head.w == 0);
+    int64_t mine = head_free;
+#pragma unroll 4
+    for (int32_t at = lo + 4 * tid + 4 * kPagesThreads; at < hi; at += 4 * kPagesThreads) {
         const int4 r = four_refs(p.refs, at, hi, vec);
         mine += (r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0);
     }
     int64_t total;
-    block_exclusive(mine, scratch, total);
+    const int64_t head_before = block_exclusive(mine, scratch, total);     // (of use where the head is all)
     if (tid == 0) totals[0] = total;
 
     // what this CTA's sequences want
@@ -184,15 +194,15 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
                 }
             }
         }
-        int64_t sum, copy_sum;
-        const int64_t before = block_exclusive(need, scratch, sum);
-        const int64_t copies_before = block_exclusive(copy, scratch, copy_sum);
+        // both prefix sums in one: a round has at most 1024 copies
+        int64_t sum;
+        const int64_t before = block_exclusive(need * 2048 + copy, scratch, sum);
         if (s < s_hi) {
-            p.begin[s] = wanted + before;
-            p.rank[s] = part ? int32_t((copies + copies_before) * 2 + copy) : -1;
+            p.begin[s] = wanted + before / 2048;
+            p.rank[s] = part ? int32_t((copies + before % 2048) * 2 + copy) : -1;
         }
-        wanted += sum;
-        copies += copy_sum;
+        wanted += sum / 2048;
+        copies += sum % 2048;
     }
     if (tid == 0) {
         totals[1] = wanted;
@@ -212,10 +222,10 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
     int64_t at_rank = free_before;
     for (int32_t base = lo; base < hi && at_rank < want_all; base += 4 * kPagesThreads) {
         const int32_t at = base + 4 * tid;
-        const int4 r = four_refs(p.refs, at, hi, vec);
+        const int4 r = base == lo ? head : four_refs(p.refs, at, hi, vec);
         const int32_t v[4] = {r.x, r.y, r.z, r.w};
-        int64_t sum;
-        int64_t k = at_rank + block_exclusive((r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0), scratch, sum);
+        int64_t sum = 0;
+        int64_t k = at_rank + (hi - lo <= 4 * kPagesThreads ? head_before : block_exclusive((r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0), scratch, sum));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (v[j] == 0) {
@@ -226,44 +236,50 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
     }
     pages_cluster_sync();                                // the old state has been read, the list is complete
 
-    // a warp per sequence
-    for (int32_t s = s_lo + warp; s < s_hi; s += kPagesThreads / 32) {
+    // A warp per sequence, or, where calls bring a few tokens a sequence, a thread: a step is a chain of dependent
+    // accesses, and 8 CTAs of warps would go through 1000 sequences in four rounds of it
+    const int wide = p.most <= 8 ? 1 : 32, part_lane = tid & (wide - 1);
+    for (int32_t s = s_lo + tid / wide; s < s_hi; s += kPagesThreads / wide) {
         const int32_t info = p.rank[s], add = p.fresh[s], length = p.lengths[s];
+        const int64_t begin = p.begin[s];
         bool granted = info >= 0;
         int64_t first = 0;
-        int32_t full = 0, after = 0, last = -1;
+        int32_t full = 0, after = 0, old = -1;
         bool copy = false, kept = false;                  // kept: the last page is partly filled (and stays or is copied)
         if (granted) {
             full = int32_t(p.page.div(uint32_t(length)));
             after = int32_t(p.page.div(uint32_t(length + add - 1))) + 1;
             kept = length != full * p.page_tokens;
             copy = info & 1;
-            first = want_before + p.begin[s];
+            first = want_before + begin;
             const int64_t need = after - full + (copy ? 1 : 0) - (kept ? 1 : 0);
             granted = first + need <= free_all;
-            if (!granted && lane == 0) pages_flag(p.flags, BTC_FLAG_POOL_EXHAUSTED);
+            if (!granted && part_lane == 0) pages_flag(p.flags, BTC_FLAG_POOL_EXHAUSTED);
+            if (kept) old = p.table[s * p.table_n + full * p.table_j];
         }
+        if (wide == 32) __syncwarp();                     // every lane has the old page before lane 0 replaces it
         if (granted) {
-            if (kept) last = copy ? __ldcg(p.holes + first) : p.table[s * p.table_n + full * p.table_j];
-            const int32_t old = kept && copy ? p.table[s * p.table_n + full * p.table_j] : -1;
-            __syncwarp();
-            if (kept && copy && lane == 0) {
-                p.table[s * p.table_n + full * p.table_j] = last;
-                p.refs[last] = 1;
-                atomicSub(p.refs + old, 1);
-                const int64_t k = copies_before + (info >> 1);
-                p.pairs[2 * k] = old;
-                p.pairs[2 * k + 1] = last;
-                atomicMax(p.count, int32_t(k + 1));
+            const int32_t last = copy ? __ldcg(p.holes + first) : old;
+            if (part_lane == 0) {
+                if (copy) {
+                    p.table[s * p.table_n + full * p.table_j] = last;
+                    p.refs[last] = 1;
+                    atomicSub(p.refs + old, 1);
+                    const int64_t k = copies_before + (info >> 1);
+                    p.pairs[2 * k] = old;
+                    p.pairs[2 * k + 1] = last;
+                    atomicMax(p.count, int32_t(k + 1));
+                }
+                p.lengths[s] = length + add;
             }
             const int32_t from = full + (kept ? 1 : 0);
             const int64_t list = first + (copy ? 1 : 0) - from;      // page of column j: holes[list + j]
-            for (int32_t j = from + lane; j < after; j += 32) {
+            for (int32_t j = from + part_lane; j < after; j += wide) {
                 const int32_t page = __ldcg(p.holes + list + j);
                 p.table[s * p.table_n + j * p.table_j] = page;
                 p.refs[page] = 1;
             }
-            for (int32_t i = lane; i < p.most; i += 32) {
+            for (int32_t i = part_lane; i < p.most; i += wide) {
                 int32_t slot = -1;
                 if (i < add) {
                     const int32_t t = length + i, j = int32_t(p.page.div(uint32_t(t)));
@@ -272,10 +288,8 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
                 }
                 p.slots[int64_t(s) * p.most + i] = slot;
             }
-            __syncwarp();
-            if (lane == 0) p.lengths[s] = length + add;
         } else {
-            for (int32_t i = lane; i < p.most; i += 32) p.slots[int64_t(s) * p.most + i] = -1;
+            for (int32_t i = part_lane; i < p.most; i += wide) p.slots[int64_t(s) * p.most + i] = -1;
         }
     }
 }
@@ -283,6 +297,7 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
 // fork: row dst[i] becomes a copy of row src[i], whose pages gain a reference.  A CTA per pair.
 static __global__ void __launch_bounds__(128) pages_fork_kernel(const __grid_constant__ PagesParams p, const int32_t *src, const int32_t *dst)
 {
+    pages_begin();
     const int32_t a = src[blockIdx.x], b = dst[blockIdx.x];
     if (a < 0 || a >= p.sequences || b < 0 || b >= p.sequences || a == b || p.lengths[b] != 0) {
         if (threadIdx.x == 0) pages_flag(p.flags, BTC_FLAG_BAD_SEQUENCE);
@@ -306,6 +321,7 @@ static __global__ void __launch_bounds__(128) pages_fork_kernel(const __grid_con
 // that is listed twice is freed once.
 static __global__ void __launch_bounds__(128) pages_free_kernel(const __grid_constant__ PagesParams p, const int32_t *list)
 {
+    pages_begin();
     const int32_t s = list[blockIdx.x];
     if (s < 0 || s >= p.sequences) {
         if (threadIdx.x == 0) pages_flag(p.flags, BTC_FLAG_BAD_SEQUENCE);
@@ -329,19 +345,22 @@ static __global__ void __launch_bounds__(128) pages_free_kernel(const __grid_con
 static __global__ void __cluster_dims__(kPagesCluster, 1, 1) __launch_bounds__(kPagesThreads)
 pages_compact_kernel(const __grid_constant__ PagesParams p)
 {
-    __shared__ int64_t scratch[33], totals[2];            // totals: live pages of this CTA; of them below L
+    __shared__ int64_t scratch[33], totals[1];            // totals: live pages of this CTA
     const unsigned rank = blockIdx.x;
     const int tid = threadIdx.x;
     const bool vec = (reinterpret_cast<uintptr_t>(p.refs) & 15) == 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    pages_begin();
     int32_t lo, hi;
     pool_share(p.pages, rank, lo, hi);
-    int64_t mine = 0, total;
-    for (int32_t at = lo + 4 * tid; at < hi; at += 4 * kPagesThreads) {
+    const bool one_round = hi - lo <= 4 * kPagesThreads;   // pools of up to 32768: every thread has its pages in `head`
+    const int4 head = four_refs(p.refs, lo + 4 * tid, hi, vec);
+    int64_t mine = (head.x > 0) + (head.y > 0) + (head.z > 0) + (head.w > 0), total;
+#pragma unroll 4
+    for (int32_t at = lo + 4 * tid + 4 * kPagesThreads; at < hi; at += 4 * kPagesThreads) {
         const int4 r = four_refs(p.refs, at, hi, vec);
         mine += (r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0);
     }
-    block_exclusive(mine, scratch, total);
+    const int64_t head_before = block_exclusive(mine, scratch, total);
     if (tid == 0) totals[0] = total;
     pages_cluster_sync();
     int64_t live_before = 0, live = 0;
@@ -351,48 +370,38 @@ pages_compact_kernel(const __grid_constant__ PagesParams p)
         if (r < rank) live_before += v;
         live += v;
     }
-    // live pages below L in this CTA's share
-    mine = 0;
-    for (int32_t at = lo + 4 * tid; at < hi && at < live; at += 4 * kPagesThreads) {
-        const int4 r = four_refs(p.refs, at, hi, vec);
-        mine += (r.x > 0) + (at + 1 < live && r.y > 0) + (at + 2 < live && r.z > 0) + (at + 3 < live && r.w > 0);
-    }
-    block_exclusive(mine, scratch, total);
-    if (tid == 0) totals[1] = total;
-    pages_cluster_sync();
-    int64_t below = 0;                                     // live pages below L: they stay
-#pragma unroll
-    for (unsigned r = 0; r < kPagesCluster; ++r) below += pages_peer_value(&totals[1], r);
-    const int64_t moves = live - below;
-    if (rank == 0 && tid == 0) {
-        p.count[0] = int32_t(moves);
-        p.count[1] = int32_t(live);
-    }
-    // page x: live pages before it are n(x); a hole is number x - n(x) of the holes, a mover number n(x) - below
+    // page x: live pages before it are n(x); a hole is number x - n(x) of the holes, a mover number n(x) - n(L)
     int64_t n = live_before;
     for (int32_t base = lo; base < hi; base += 4 * kPagesThreads) {
         const int32_t at = base + 4 * tid;
-        const int4 r = four_refs(p.refs, at, hi, vec);
+        const int4 r = base == lo ? head : four_refs(p.refs, at, hi, vec);
         const int32_t v[4] = {r.x, r.y, r.z, r.w};
-        int64_t sum;
-        int64_t k = n + block_exclusive((r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0), scratch, sum);
+        int64_t sum = 0;
+        int64_t k = n + (one_round ? head_before : block_exclusive((r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0), scratch, sum));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int32_t x = at + j;
             if (x >= hi) break;
+            if (x == live) p.count[0] = int32_t(live - k);            // n(L) pages stay: as many moves as holes below L
             if (x < live) {
                 if (v[j] <= 0) p.holes[x - k] = x;
             } else {
-                if (v[j] > 0) p.movers[k - below] = x;
+                // movers are listed from the last live page on, so that n(L) need not be known yet
+                if (v[j] > 0) p.movers[live - 1 - k] = x;
                 p.map[x] = x;
             }
             k += v[j] > 0;
         }
         n += sum;
     }
+    if (rank == 0 && tid == 0) {
+        if (live == p.pages) p.count[0] = 0;               // a full pool: there is no page number L
+        p.count[1] = int32_t(live);
+    }
     pages_cluster_sync();
+    const int64_t moves = __ldcg(p.count);
     for (int64_t k = int64_t(rank) * kPagesThreads + tid; k < moves; k += kPagesCluster * kPagesThreads) {
-        const int32_t src = __ldcg(p.movers + k), dst = __ldcg(p.holes + k);
+        const int32_t src = __ldcg(p.movers + (moves - 1 - k)), dst = __ldcg(p.holes + k);
         p.pairs[2 * k] = src;
         p.pairs[2 * k + 1] = dst;
         p.map[src] = dst;
@@ -405,7 +414,7 @@ pages_compact_kernel(const __grid_constant__ PagesParams p)
 template <typename U>
 static __global__ void __launch_bounds__(kPagesCopyThreads) pages_copy_kernel(const __grid_constant__ PagesCopyParams p)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    pages_begin();
     if (p.table) {
         const int64_t all = int64_t(p.sequences) * p.columns;
         const int32_t live = *p.live;

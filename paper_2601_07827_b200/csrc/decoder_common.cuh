@@ -68,6 +68,13 @@ template <typename T, int V> __device__ __forceinline__ typename VectorOf<V * in
     else return make_uint2(w[0], w[1]);
 }
 
+// The decoder kernels may be launched while the one before it in the stream still runs (its set-up is then hidden): it
+// touches nothing before that one has ended, and lets the next one do the same.
+__device__ __forceinline__ void early_begin()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 // Pairs of fp32 operations.  (As the packed two-in-one instructions they cost more moves between registers than
 // they save: the rotary kernels took 3 to 10 % longer with them.)
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }

@@ -40,6 +40,25 @@ template <typename F> btc_error_t guarded(F &&body)
     }
 }
 
-inline btc_error_t launch_result() { return cudaGetLastError() == cudaSuccess ? BTC_SUCCESS : BTC_ERR_CUDA; }
+// One launch that may be set up while the kernel before it in the stream runs (the kernels wait on the device).
+template <typename... Args, typename... Given>
+btc_error_t launch_early(void (*kernel)(Args...), dim3 blocks, unsigned threads, size_t shared, cudaStream_t st, Given &&...given)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, Args(given)...) != cudaSuccess) {
+        cudaGetLastError();
+        return BTC_ERR_CUDA;
+    }
+    return BTC_SUCCESS;
+}
 
 }  // namespace btc

@@ -56,29 +56,9 @@ btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t 
         }
         configured[slot].store(true, std::memory_order_relaxed);
     }
-    // both kernels are set up while the one before them in the stream runs, and wait for its end on the device
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(ctas));
-    cfg.blockDim = dim3(Shape::WARPS * 32);
-    cfg.dynamicSmemBytes = Shape::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, paged_attention_kernel<T, DP, NT>, p);
-    if (e == cudaSuccess) {
-        cfg.gridDim = dim3(unsigned(ctas), kJoinSlices);
-        cfg.blockDim = dim3(kJoinThreads);
-        cfg.dynamicSmemBytes = 0;
-        e = cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<T, DP, NT>, p, ctas);
-    }
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        return BTC_ERR_CUDA;
-    }
-    return BTC_SUCCESS;
+    const btc_error_t rc = launch_early(paged_attention_kernel<T, DP, NT>, dim3(unsigned(ctas)), Shape::WARPS * 32, Shape::SMEM, st, p);
+    if (rc != BTC_SUCCESS) return rc;
+    return launch_early(paged_attention_join_kernel<T, DP, NT>, dim3(unsigned(ctas), kJoinSlices), kJoinThreads, 0, st, p, ctas);
 }
 
 template <typename T> btc_error_t launch_typed(const btc_paged_attention_s &op, const AttentionParams &p, cudaStream_t st)

@@ -596,10 +596,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int head_blocks = p.key_heads * p.blocks;
 
-    // launched while the kernel before it may still run: nothing is read or written before that has ended; the joining
-    // kernel in turn is set up while this one runs
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    early_begin();
 
     // tiles of all sequences: thread i sums sequences [i * per, (i + 1) * per), then a prefix sum over the threads
     const int per = (p.sequences + THREADS - 1) / THREADS;
@@ -852,8 +849,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
     __shared__ float tops[HEADS], totals[HEADS];
     __shared__ float4 sums[SPLIT - 1][QUADS];
     const int c = blockIdx.x, h0 = blockIdx.y * HEADS, tid = threadIdx.x, lane = tid & 31;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    early_begin();
     const int32_t item = load_now(p.partial_item + 2 * c + 1);
     if (item < 0) return;
     // Part 0 is CTA c's second slot, part i CTA c + i's first; the first CTA without the item ends it.  How many parts there

@@ -114,26 +114,6 @@ void fill_workspace(const btc_pages_s &op, void *workspace, PagesParams &p)
     p.begin = reinterpret_cast<int64_t *>(base + w.begin);
 }
 
-// One launch that may be set up while the kernel before it in the stream runs (the kernels wait on the device).
-template <typename... Args, typename... Given>
-btc_error_t launch_early(void (*kernel)(Args...), unsigned blocks, unsigned threads, cudaStream_t st, Given &&...given)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(threads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, Args(given)...) != cudaSuccess) {
-        cudaGetLastError();
-        return BTC_ERR_CUDA;
-    }
-    return BTC_SUCCESS;
-}
-
 // Launches the copies (and the renumbering when p.table is set).  `pairs_most`: as many pairs as there can be.
 btc_error_t launch_copies(const btc_pages_s &op, PagesCopyParams &p, void *const *tensors, int32_t count, int64_t pairs_most,
                           cudaStream_t st)
@@ -183,10 +163,10 @@ btc_error_t launch_copies(const btc_pages_s &op, PagesCopyParams &p, void *const
         const int64_t blocks = int64_t(std::max<__int128>(1, std::min<__int128>(steps, most)));
         btc_error_t rc;
         switch (unit) {
-        case 16: rc = launch_early(pages_copy_kernel<uint4>, unsigned(blocks), kPagesCopyThreads, st, p); break;
-        case 8: rc = launch_early(pages_copy_kernel<uint2>, unsigned(blocks), kPagesCopyThreads, st, p); break;
-        case 4: rc = launch_early(pages_copy_kernel<uint32_t>, unsigned(blocks), kPagesCopyThreads, st, p); break;
-        default: rc = launch_early(pages_copy_kernel<uint16_t>, unsigned(blocks), kPagesCopyThreads, st, p); break;
+        case 16: rc = launch_early(pages_copy_kernel<uint4>, unsigned(blocks), kPagesCopyThreads, 0, st, p); break;
+        case 8: rc = launch_early(pages_copy_kernel<uint2>, unsigned(blocks), kPagesCopyThreads, 0, st, p); break;
+        case 4: rc = launch_early(pages_copy_kernel<uint32_t>, unsigned(blocks), kPagesCopyThreads, 0, st, p); break;
+        default: rc = launch_early(pages_copy_kernel<uint16_t>, unsigned(blocks), kPagesCopyThreads, 0, st, p); break;
         }
         if (rc != BTC_SUCCESS) return rc;
         p.table = nullptr;                 // renumbered once
@@ -270,7 +250,7 @@ btc_error_t btc_pages_extend(btc_pages_t op, void *cuda_stream, const int32_t *n
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
     p.fresh = new_tokens; p.slots = slots; p.most = max_new;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    rc = launch_early(pages_extend_kernel, kPagesCluster, kPagesThreads, st, p);
+    rc = launch_early(pages_extend_kernel, kPagesCluster, kPagesThreads, 0, st, p);
     if (rc != BTC_SUCCESS || count == 0) return rc;
     PagesCopyParams c;
     std::memset(static_cast<void *>(&c), 0, sizeof c);
@@ -288,7 +268,7 @@ btc_error_t btc_pages_fork(btc_pages_t op, void *cuda_stream, const int32_t *src
     PagesParams p;
     fill_state(*op, p);
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
-    return launch_early(pages_fork_kernel, unsigned(count), 128, static_cast<cudaStream_t>(cuda_stream), p, src, dst);
+    return launch_early(pages_fork_kernel, unsigned(count), 128, 0, static_cast<cudaStream_t>(cuda_stream), p, src, dst);
 }
 
 btc_error_t btc_pages_free(btc_pages_t op, void *cuda_stream, const int32_t *sequences, int32_t count, int32_t *table,
@@ -301,7 +281,7 @@ btc_error_t btc_pages_free(btc_pages_t op, void *cuda_stream, const int32_t *seq
     PagesParams p;
     fill_state(*op, p);
     p.table = table; p.lengths = lengths; p.refs = refs; p.flags = flags;
-    return launch_early(pages_free_kernel, unsigned(count), 128, static_cast<cudaStream_t>(cuda_stream), p, sequences);
+    return launch_early(pages_free_kernel, unsigned(count), 128, 0, static_cast<cudaStream_t>(cuda_stream), p, sequences);
 }
 
 btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table, int32_t *refs, void *const *tensors,
@@ -319,7 +299,7 @@ btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table,
     fill_workspace(*op, workspace, p);
     p.table = table; p.refs = refs; p.flags = flags;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    rc = launch_early(pages_compact_kernel, kPagesCluster, kPagesThreads, st, p);
+    rc = launch_early(pages_compact_kernel, kPagesCluster, kPagesThreads, 0, st, p);
     if (rc != BTC_SUCCESS) return rc;
     PagesCopyParams c;
     std::memset(static_cast<void *>(&c), 0, sizeof c);

@@ -77,13 +77,6 @@ __device__ __forceinline__ int64_t pages_peer_value(const int64_t *mine, unsigne
     asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
     return v;
 }
-// Every kernel here may be launched while the one before it in the stream still runs (its set-up is then hidden): it
-// touches nothing before that one has ended, and lets the next one do the same.
-__device__ __forceinline__ void pages_begin()
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
 __device__ __forceinline__ void pages_flag(int32_t *flags, int what)
 {
     if (flags) atomicOr(flags, what);
@@ -147,7 +140,7 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
     const unsigned rank = blockIdx.x;
     const int tid = threadIdx.x;
     const bool vec = (reinterpret_cast<uintptr_t>(p.refs) & 15) == 0;
-    pages_begin();
+    early_begin();
 
     // free pages of this CTA's share; the first four of a thread stay in registers (`head`: all, in pools of up to 32768)
     int32_t lo, hi;
@@ -297,7 +290,7 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
 // fork: row dst[i] becomes a copy of row src[i], whose pages gain a reference.  A CTA per pair.
 static __global__ void __launch_bounds__(128) pages_fork_kernel(const __grid_constant__ PagesParams p, const int32_t *src, const int32_t *dst)
 {
-    pages_begin();
+    early_begin();
     const int32_t a = src[blockIdx.x], b = dst[blockIdx.x];
     if (a < 0 || a >= p.sequences || b < 0 || b >= p.sequences || a == b || p.lengths[b] != 0) {
         if (threadIdx.x == 0) pages_flag(p.flags, BTC_FLAG_BAD_SEQUENCE);
@@ -321,7 +314,7 @@ static __global__ void __launch_bounds__(128) pages_fork_kernel(const __grid_con
 // that is listed twice is freed once.
 static __global__ void __launch_bounds__(128) pages_free_kernel(const __grid_constant__ PagesParams p, const int32_t *list)
 {
-    pages_begin();
+    early_begin();
     const int32_t s = list[blockIdx.x];
     if (s < 0 || s >= p.sequences) {
         if (threadIdx.x == 0) pages_flag(p.flags, BTC_FLAG_BAD_SEQUENCE);
@@ -349,7 +342,7 @@ pages_compact_kernel(const __grid_constant__ PagesParams p)
     const unsigned rank = blockIdx.x;
     const int tid = threadIdx.x;
     const bool vec = (reinterpret_cast<uintptr_t>(p.refs) & 15) == 0;
-    pages_begin();
+    early_begin();
     int32_t lo, hi;
     pool_share(p.pages, rank, lo, hi);
     const bool one_round = hi - lo <= 4 * kPagesThreads;   // pools of up to 32768: every thread has its pages in `head`
@@ -414,7 +407,7 @@ pages_compact_kernel(const __grid_constant__ PagesParams p)
 template <typename U>
 static __global__ void __launch_bounds__(kPagesCopyThreads) pages_copy_kernel(const __grid_constant__ PagesCopyParams p)
 {
-    pages_begin();
+    early_begin();
     if (p.table) {
         const int64_t all = int64_t(p.sequences) * p.columns;
         const int32_t live = *p.live;

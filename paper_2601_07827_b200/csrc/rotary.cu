@@ -98,28 +98,28 @@ void fill_part(const btc_rotary_s &op, int i, RotaryPart &p)
 }
 
 template <typename T, int V>
-void launch_forward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
+btc_error_t launch_forward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
 {
-    // the scalar form asks for each slot in any case
-    constexpr bool F = V > 1;
-    if (interleaved) (F && full) ? rotary_forward_kernel<T, V, true, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_forward_kernel<T, V, true, false><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else (F && full) ? rotary_forward_kernel<T, V, false, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_forward_kernel<T, V, false, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    constexpr bool F = V > 1;              // the scalar form asks for each slot in any case
+    void (*kernel)(const RotaryParams) = interleaved ? (full ? rotary_forward_kernel<T, V, true, F> : rotary_forward_kernel<T, V, true, false>)
+                                                     : (full ? rotary_forward_kernel<T, V, false, F> : rotary_forward_kernel<T, V, false, false>);
+    return launch_early(kernel, blocks, kRotaryThreads, 0, st, p);
 }
 template <typename T, int V>
-void launch_backward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
+btc_error_t launch_backward(const RotaryParams &p, bool interleaved, bool full, unsigned blocks, cudaStream_t st)
 {
-    // the scalar form asks for each slot in any case
-    constexpr bool F = V > 1;
-    if (interleaved) (F && full) ? rotary_backward_kernel<T, V, true, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_backward_kernel<T, V, true, false><<<blocks, kRotaryThreads, 0, st>>>(p);
-    else (F && full) ? rotary_backward_kernel<T, V, false, F><<<blocks, kRotaryThreads, 0, st>>>(p) : rotary_backward_kernel<T, V, false, false><<<blocks, kRotaryThreads, 0, st>>>(p);
+    constexpr bool F = V > 1;              // the scalar form asks for each slot in any case
+    void (*kernel)(const RotaryParams) = interleaved ? (full ? rotary_backward_kernel<T, V, true, F> : rotary_backward_kernel<T, V, true, false>)
+                                                     : (full ? rotary_backward_kernel<T, V, false, F> : rotary_backward_kernel<T, V, false, false>);
+    // not set up early: persistent CTAs that arrive while the SMs still drain the kernel before cost 3 % of a large pass
+    kernel<<<blocks, kRotaryThreads, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? BTC_SUCCESS : BTC_ERR_CUDA;
 }
 
 #define BTC_ROTARY_DISPATCH(F, dtype, bytes, ...)                                                                        \
-    do {                                                                                                                 \
-        if ((dtype) == BTC_F32) (bytes) == 16 ? F<float, 4>(__VA_ARGS__) : (bytes) == 8 ? F<float, 2>(__VA_ARGS__) : F<float, 1>(__VA_ARGS__);                 \
-        else if ((dtype) == BTC_F16) (bytes) == 16 ? F<__half, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__half, 4>(__VA_ARGS__) : F<__half, 1>(__VA_ARGS__);         \
-        else (bytes) == 16 ? F<__nv_bfloat16, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__nv_bfloat16, 4>(__VA_ARGS__) : F<__nv_bfloat16, 1>(__VA_ARGS__);            \
-    } while (0)
+    ((dtype) == BTC_F32 ? ((bytes) == 16 ? F<float, 4>(__VA_ARGS__) : (bytes) == 8 ? F<float, 2>(__VA_ARGS__) : F<float, 1>(__VA_ARGS__))              \
+     : (dtype) == BTC_F16 ? ((bytes) == 16 ? F<__half, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__half, 4>(__VA_ARGS__) : F<__half, 1>(__VA_ARGS__))          \
+     : ((bytes) == 16 ? F<__nv_bfloat16, 8>(__VA_ARGS__) : (bytes) == 8 ? F<__nv_bfloat16, 4>(__VA_ARGS__) : F<__nv_bfloat16, 1>(__VA_ARGS__)))
 
 }  // namespace
 
@@ -259,7 +259,7 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
         fill_part(*op, i, part);
         part.x = X[i]; part.y = Y[i]; part.w = W[i];
         if (part.heads > INT32_MAX / kRotaryMaxTokens / 2) return BTC_ERR_NOT_SUPPORTED;
-        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 8, int64_t(op->handle.sm_count) * 6);
+        part.cta_tokens = tokens_per_cta(op->tokens, part.heads, p.lanes_log2, 24, int64_t(op->handle.sm_count) * 4);
         const int64_t ctas = (op->tokens + part.cta_tokens - 1) / part.cta_tokens;
         if (ctas > INT32_MAX / 4) return BTC_ERR_NOT_SUPPORTED;
         part.ctas = uint32_t(ctas);
@@ -272,9 +272,8 @@ btc_error_t btc_rotary_execute(btc_rotary_t op, void *cuda_stream, const int32_t
     p.norm = op->norm; p.eps = float(op->eps); p.mult = float(op->multiplier);
     p.page.set(op->page_tokens);
     p.slot_count = int32_t(op->pages * op->page_tokens);
-    BTC_ROTARY_DISPATCH(launch_forward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED, 2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(blocks),
-                        static_cast<cudaStream_t>(cuda_stream));
-    return launch_result();
+    return BTC_ROTARY_DISPATCH(launch_forward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED,
+                               2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(blocks), static_cast<cudaStream_t>(cuda_stream));
 }
 
 btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_t *positions, const void *Wq,
@@ -338,27 +337,12 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
     p.norm = op->norm; p.eps = float(op->eps); p.mult = float(op->multiplier);
     p.page.set(1);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    BTC_ROTARY_DISPATCH(launch_backward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED,
-                        2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(p.part[0].ctas + p.part[1].ctas), st);
-    const btc_error_t rc = launch_result();
+    const btc_error_t rc = BTC_ROTARY_DISPATCH(launch_backward, op->dtype, bytes, p, op->layout == BTC_ROTARY_INTERLEAVED,
+                                               2 * int64_t(op->pairs) == op->x[0].extent[2], unsigned(p.part[0].ctas + p.part[1].ctas), st);
     if (rc != BTC_SUCCESS || !sums) return rc;
-    // the summing kernel is set up while the first one runs and waits for its end on the device
     const int dim = int(op->x[0].extent[2]);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((dim + kRotaryGradColumns - 1) / kRotaryGradColumns), 2);
-    cfg.blockDim = dim3(kRotaryGradThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, rotary_weight_gradient_kernel, static_cast<const float *>(p.partial), int(p.part[0].ctas),
-                           int(p.part[1].ctas), dim, dWq, dWk) != cudaSuccess) {
-        cudaGetLastError();
-        return BTC_ERR_CUDA;
-    }
-    return BTC_SUCCESS;
+    return launch_early(rotary_weight_gradient_kernel, dim3(unsigned((dim + kRotaryGradColumns - 1) / kRotaryGradColumns), 2), kRotaryGradThreads,
+                        0, st, static_cast<const float *>(p.partial), int(p.part[0].ctas), int(p.part[1].ctas), dim, dWq, dWk);
 }
 
 }  // extern "C"

@@ -25,7 +25,7 @@ namespace btc {
 
 constexpr int kRotaryMaxDim = 256;
 constexpr int kRotaryThreads = 256;
-constexpr int kRotaryMaxTokens = 16;     // tokens a CTA takes at a time
+constexpr int kRotaryMaxTokens = 32;     // tokens a CTA takes at a time
 
 struct RotaryPart {
     const void *x;                 // input [T, heads, dim]
@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 3) rotary_forward_kernel(const
 {
     typedef RotaryLane<T, V, INTERLEAVED> Lane;
     constexpr int N2 = Lane::N2;
+    early_begin();
     __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
     const int lanes = 1 << p.lanes_log2, groups = kRotaryThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
     uint32_t cta = blockIdx.x;
@@ -404,7 +405,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
     constexpr int N = Lane::N, N2 = Lane::N2;
     __shared__ __align__(16) float cosines[kRotaryMaxTokens * kRotaryMaxDim / 2], sines[kRotaryMaxTokens * kRotaryMaxDim / 2];
     __shared__ float sums[kRotaryThreads / 32][kRotaryMaxDim];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    early_begin();
     const int lanes = 1 << p.lanes_log2, groups = kRotaryThreads >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
     const int which = blockIdx.x < p.part[0].ctas ? 0 : 1;
     const RotaryPart &part = p.part[which];
@@ -550,7 +551,7 @@ static __global__ void __launch_bounds__(kRotaryGradThreads) rotary_weight_gradi
                                                                                          float *dwq, float *dwk)
 {
     __shared__ float tile[kRotaryGradThreads / 32][kRotaryGradColumns];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    early_begin();
     const int which = blockIdx.y;
     float *dw = which ? dwk : dwq;
     if (!dw) return;

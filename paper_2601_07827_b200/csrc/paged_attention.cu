@@ -92,7 +92,7 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
             q.extent[1] % k.extent[2] != 0)
             return BTC_ERR_EXTENT_MISMATCH;
         if (q.extent[2] > kAttnMaxDim || v.extent[3] > kAttnMaxDim) return BTC_ERR_NOT_SUPPORTED;
-        if (k.extent[0] > INT32_MAX || k.extent[1] > INT32_MAX || t.extent[1] > INT32_MAX || q.extent[0] > INT32_MAX / 2 ||
+        if (k.extent[0] > INT32_MAX || k.extent[1] > INT32_MAX || t.extent[1] > INT32_MAX || q.extent[0] > kAttnMaxSequences ||
             q.extent[1] > INT32_MAX / 2 || q.extent[1] * o.extent[2] > INT32_MAX / 2)
             return BTC_ERR_NOT_SUPPORTED;
         for (const TensorDesc *d : {&q, &k, &v, &t, &o})
@@ -173,7 +173,7 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
     const int64_t vec = int64_t(16 / es);
     p.vec_k = rows_allow_vectors(op->k, vec) && aligned_to(K, 16);
     p.vec_v = rows_allow_vectors(op->v, vec) && aligned_to(V, 16);
-    p.whole_tiles = p.vec_k && p.vec_v && op->k.extent[1] % kAttnTok == 0;
+    p.whole_tiles = !(p.vec_k && p.vec_v) ? 0 : (op->k.extent[1] % kAttnTok == 0 ? kAttnTok : (op->k.extent[1] % 8 == 0 ? 8 : 0));
     p.vec_q = es == 2 && p.dim_k % 2 == 0 && rows_allow_vectors(op->q, 2) && aligned_to(Q, 4);
     p.scale_log2 = float(op->scale * 1.4426950408889634);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -18,7 +18,7 @@
 //     (x = hi + lo; lo * lo is dropped, at most 2^-22 of the product), as in the contractions.
 //   * running maximum, sum and output in fp32 (the flash form); the output is rescaled only when a maximum moved.
 // Work.  The tiles of all (sequence, key head) pairs form one list; CTAs and in them warps take equal
-// contiguous ranges of it, whatever the lengths are, found on the device from a prefix sum of the tile
+// contiguous shares of it, whatever the lengths are, found on the device from a prefix sum of the tile
 // counts (the host never reads a length).  What a warp cannot finish is merged in shared memory by its
 // CTA, what a CTA cannot finish goes to the workspace and a second small kernel joins it, in a fixed order.
 #pragma once
@@ -30,6 +30,11 @@ namespace btc {
 
 constexpr int kAttnTok = 16;                 // tokens per tile
 constexpr int kAttnMaxDim = 256;
+// What beginning and ending an item (a sequence's key head) costs, in tiles: about 2 us, when a tile takes 1.3.  The list
+// of tiles is cut into equal shares of tiles plus this for every item; counted by tiles alone, the CTA with
+// the shortest sequences of a ragged batch ran 17 us longer than the others' 68.
+constexpr int kAttnItemTiles = 2;
+constexpr int kAttnMaxSequences = 1 << 23;   // tiles and sequences are counted in one 64-bit prefix sum
 
 struct AttentionParams {
     const void *q, *k, *v;
@@ -46,7 +51,7 @@ struct AttentionParams {
     int32_t dim_k, dim_v, pages, columns;
     int32_t window;                          // 0: everything up to the length is visible
     int32_t room;                            // tokens a table row can hold
-    int32_t whole_tiles;                     // vec_k and vec_v, and pages of whole tiles
+    int32_t whole_tiles;                     // vec_k and vec_v, and pages of whole tiles (16) or half tiles (8); 0: neither
     int32_t vec_k, vec_v, vec_q;             // 16-byte copies of keys / values, 4-byte loads of queries
     FastDiv page;
     float scale_log2;                        // scale * log2(e)
@@ -221,18 +226,21 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         return left < 0 ? 0 : (left < 16 ? left : 16);
     }
 
-    // start the copies of a tile whose 16 rows are all there, in one page: an address step and a copy per row
-    __device__ __forceinline__ void copy_whole(unsigned dst, const T *src, int64_t s_slot, int dim) const
+    // start the copies of a tile whose 16 rows are all there, the first and the last 8 in one page each: an address step
+    // and a copy per row
+    __device__ __forceinline__ void copy_whole(unsigned dst, const T *src, const T *src8, int64_t s_slot, int dim) const
     {
         const int sub = my_sub();
 #pragma unroll
         for (int c0 = 0; c0 < COLS; ++c0) {
             const int chunk = my_chunk() + 32 * c0, bytes = chunk_bytes(chunk, dim);
-            const T *at = src + sub * s_slot + (bytes ? chunk * PER : 0);
+            const int64_t mine = sub * s_slot + (bytes ? chunk * PER : 0);
+            const T *at = src + mine;
             const unsigned to = dst + sub * ROW + ((chunk ^ sub) << 4);       // = swizzled(sub, chunk): rows r0 + sub only flip bits 4 to 6
             if (!idle()) {
 #pragma unroll
                 for (int r0 = 0; r0 < kAttnTok; r0 += STEP) {
+                    if (r0 == 8) at = src8 + mine;
                     cp_async_part((to ^ ((r0 & 7) << 4)) + r0 * ROW, at, bytes);
                     at += STEP * s_slot;
                 }
@@ -279,10 +287,17 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         const unsigned dst = ring + unsigned(stage) * Shape::STAGE;
         const T *k = static_cast<const T *>(p.k) + c.key_head * p.k_head, *v = static_cast<const T *>(p.v) + c.key_head * p.v_head;
         if (p.whole_tiles && mask == 0xffffu) {
-            // the page holds a multiple of 16 tokens, so `page` is the same in every lane and lane 0 has the first row
-            const int64_t first = __shfl_sync(0xffffffffu, row, 0);
-            copy_whole(dst, k + page * p.k_page + first * p.k_slot, p.k_slot, p.dim_k);
-            copy_whole(dst + kAttnTok * ROW, v + page * p.v_page + first * p.v_slot, p.v_slot, p.dim_v);
+            // lanes 0 and 8 have the first row of each half; where pages hold a multiple of 16 tokens both are in one page
+            const int64_t row0 = __shfl_sync(0xffffffffu, row, 0);
+            int32_t page0 = page, page8 = page;
+            int64_t row8 = row0 + 8;
+            if (p.whole_tiles == 8) {
+                page0 = __shfl_sync(0xffffffffu, page, 0);
+                page8 = __shfl_sync(0xffffffffu, page, 8);
+                row8 = __shfl_sync(0xffffffffu, row, 8);
+            }
+            copy_whole(dst, k + page0 * p.k_page + row0 * p.k_slot, k + page8 * p.k_page + row8 * p.k_slot, p.k_slot, p.dim_k);
+            copy_whole(dst + kAttnTok * ROW, v + page0 * p.v_page + row0 * p.v_slot, v + page8 * p.v_page + row8 * p.v_slot, p.v_slot, p.dim_v);
             return;
         }
         copy_rows(dst, k, p.k_page, p.k_slot, p.k_d, p.dim_k, p.vec_k, page, row, mask);
@@ -458,20 +473,26 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                         const float x = __shfl_sync(0xffffffffu, s[nt][2 * ks], src), y = __shfl_sync(0xffffffffu, s[nt][2 * ks + 1], src);
                         b[nt][ks][half] = __float_as_uint((lane >> 2) & 1 ? y : x);
                     }
+            // The rows of the product may be any order of the head's elements.  They are taken so that a lane's four elements
+            // of one token in two row tiles are neighbours (element()): one 16-byte read for them
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int pair = 0; pair < MT / 2; ++pair)
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
-                    uint32_t hi[4], lo[4];
+                    uint32_t hi[2][4], lo[2][4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int d = mt * 16 + (j & 1) * 8 + (lane >> 2), t = ks * 8 + (j >> 1) * 4 + (lane & 3);
-                        uint32_t x;
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(vs_base + swizzled(t, d >> 2) + unsigned(d & 3) * 4u) : "memory");
-                        split_tf32(x, hi[j], lo[j]);
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t x[4];
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                                     : "r"(vs_base + swizzled(ks * 8 + j * 4 + (lane & 3), lane >> 2) + pair * 128) : "memory");
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) split_tf32(x[e], hi[e >> 1][2 * j + (e & 1)], lo[e >> 1][2 * j + (e & 1)]);
                     }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma8_split(o[mt][nt], o[mt][nt], o[mt][nt], hi, lo, b[nt][ks][0], b[nt][ks][1]);
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            mma8_split(o[2 * pair + i][nt], o[2 * pair + i][nt], o[2 * pair + i][nt], hi[i], lo[i], b[nt][ks][0], b[nt][ks][1]);
                 }
         } else {
             uint32_t hi[NT][2], lo[NT][2];
@@ -498,6 +519,11 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         }
     }
 
+    // which element of the head the accumulator row (lane / 4, + 8 when half) of row tile mt is
+    __device__ __forceinline__ int element(int mt, int half) const
+    {
+        return F32 ? (mt >> 1) * 32 + (lane >> 2) * 4 + (mt & 1) * 2 + half : mt * 16 + half * 8 + (lane >> 2);
+    }
     __device__ __forceinline__ void finish_sums()
     {
 #pragma unroll
@@ -526,7 +552,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const int d = mt * 16 + half * 8 + (lane >> 2);
+                        const int d = element(mt, half);
                         if (d < p.dim_v) dst[d * p.o_d] = from_f32<T>(o[mt][nt][2 * half + j] * inv);
                     }
                 if (p.lse && lane < 4)
@@ -546,7 +572,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
-                        out[h * DP + mt * 16 + half * 8 + (lane >> 2)] = o[mt][nt][2 * half + j];
+                        out[h * DP + element(mt, half)] = o[mt][nt][2 * half + j];
                 if (lane < 4) {
                     stats[h] = m[nt][j];
                     stats[8 * NT + h] = l[nt][j];
@@ -601,14 +627,14 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     // tiles of all sequences: thread i sums sequences [i * per, (i + 1) * per), then a prefix sum over the threads
     const int per = (p.sequences + THREADS - 1) / THREADS;
     {
-        int64_t mine = 0;
+        int64_t mine = 0;                                       // tiles * 2^24 + sequences that have any
         for (int i = 0; i < per; ++i) {
             const int s = tid * per + i;
             if (s >= p.sequences) break;
             const int32_t length = p.lengths[s];
             AttentionSpan span;
             span.set(p, length);
-            mine += span.tiles;
+            mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
             if (rare(length < 0 || length > p.room))
                 if (blockIdx.x == 0 && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
@@ -628,51 +654,71 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         scan[tid + 1] = x + before;
         __syncthreads();
     }
-    // equal ranges of the list of tiles, at least one tile per warp of the CTAs that take part
-    const int64_t total = scan[THREADS] * head_blocks;
+    // equal shares of the list, at least one unit per warp of the CTAs that take part
+    auto units = [&](int i) { return ((scan[i] >> 24) + (scan[i] & 0xffffff) * kAttnItemTiles) * head_blocks; };
+    const int64_t total = units(THREADS);
     int64_t ctas = (total + W - 1) / W;
     if (ctas > gridDim.x) ctas = gridDim.x;
-    int64_t lo = 0, hi = 0, cta_lo = 0, cta_hi = 0;
+    // Lanes 0, 1 and 2 look up the places where the warp's share begins and ends and where the CTA's ends.
+    AttentionCursor cur;
+    int64_t n = 0;                                              // tiles of this warp
+    bool closes = false;                                        // its last tile is the CTA's last
     if (blockIdx.x < ctas) {
         const int64_t each = divide(total, int32_t(ctas)), more = total - each * ctas;
-        cta_lo = each * blockIdx.x + min(int64_t(blockIdx.x), more);
-        cta_hi = cta_lo + each + (int64_t(blockIdx.x) < more ? 1 : 0);
-        const int64_t n = cta_hi - cta_lo, we = n / W, wm = n - we * W;
-        lo = cta_lo + we * warp + min(int64_t(warp), wm);
-        hi = lo + we + (warp < wm ? 1 : 0);
+        const int64_t cta_lo = each * blockIdx.x + min(int64_t(blockIdx.x), more), in_cta = each + (int64_t(blockIdx.x) < more ? 1 : 0);
+        const int64_t we = in_cta / W, wm = in_cta - we * W;
+        const int64_t lo = cta_lo + we * warp + min(int64_t(warp), wm);
+        const int64_t unit = lane == 1 ? lo + we + (warp < wm ? 1 : 0) : (lane == 2 ? cta_lo + in_cta : lo);
+        cur.seq = p.sequences;
+        cur.hb = cur.tile = 0;
+        cur.span.begin = cur.span.end = cur.span.first_tile = cur.span.tiles = 0;
+        int64_t tiles_before = (scan[THREADS] >> 24) * head_blocks;
+        if (unit < total) {
+            int a = 0, b = THREADS;                             // units(a) <= unit < units(b)
+            while (b - a > 1) {
+                const int c = (a + b) / 2;
+                if (units(c) <= unit) a = c; else b = c;
+            }
+            int64_t at = unit - units(a);
+            tiles_before = (scan[a] >> 24) * head_blocks;
+            cur.seq = a * per;
+            cur.span.set(p, p.lengths[cur.seq]);
+            // a sequence's units: kAttnItemTiles and then its tiles, for each key head
+            while (cur.seq + 1 < p.sequences) {
+                const int64_t here = cur.span.tiles > 0 ? int64_t(cur.span.tiles + kAttnItemTiles) * head_blocks : 0;
+                if (at < here) break;
+                at -= here;
+                tiles_before += int64_t(cur.span.tiles) * head_blocks;
+                cur.span.set(p, p.lengths[++cur.seq]);
+            }
+            const int32_t item_units = cur.span.tiles + kAttnItemTiles;
+            cur.hb = int32_t(divide(at, item_units));
+            cur.tile = max(0, int32_t(at - int64_t(cur.hb) * item_units) - kAttnItemTiles);
+            tiles_before += int64_t(cur.hb) * cur.span.tiles + cur.tile;
+        }
+        const int64_t from = __shfl_sync(0xffffffffu, tiles_before, 0), to = __shfl_sync(0xffffffffu, tiles_before, 1);
+        n = to - from;
+        closes = to == __shfl_sync(0xffffffffu, tiles_before, 2);
+        cur.seq = __shfl_sync(0xffffffffu, cur.seq, 0);
+        cur.hb = __shfl_sync(0xffffffffu, cur.hb, 0);
+        cur.tile = __shfl_sync(0xffffffffu, cur.tile, 0);
+        cur.span.begin = __shfl_sync(0xffffffffu, cur.span.begin, 0);
+        cur.span.end = __shfl_sync(0xffffffffu, cur.span.end, 0);
+        cur.span.first_tile = __shfl_sync(0xffffffffu, cur.span.first_tile, 0);
+        cur.span.tiles = __shfl_sync(0xffffffffu, cur.span.tiles, 0);
+        cur.key_head = cur.hb / p.blocks;
+        cur.block = cur.hb - cur.key_head * p.blocks;
+        // does the CTA's share begin inside an item?  (Then its first unit is a tile, and warp 0 has it.)
+        if (warp == 0 && cur.tile != 0 && lane == 0) first_item = cur.seq * head_blocks + cur.hb;
     }
-
     const unsigned ring = static_cast<unsigned>(__cvta_generic_to_shared(smem)) + unsigned(warp) * Shape::RING;
     float *deposit_first = reinterpret_cast<float *>(smem + W * Shape::RING) + warp * (Shape::DEPOSIT / 4);
     float *deposit_last = reinterpret_cast<float *>(smem + warp * Shape::RING);
 
-    AttentionCursor cur;
-    if (lo < hi) {
-        // where the range begins: the thread whose sequences hold it, then walk those sequences
-        int a = 0, b = THREADS;                                 // scan[a] * head_blocks <= lo < scan[b] * head_blocks
-        while (b - a > 1) {
-            const int c = (a + b) / 2;
-            if (scan[c] * head_blocks <= lo) a = c; else b = c;
-        }
-        int64_t at = lo - scan[a] * head_blocks;
-        cur.seq = a * per;
-        cur.span.set(p, p.lengths[cur.seq]);
-        while (at >= int64_t(cur.span.tiles) * head_blocks && cur.seq + 1 < p.sequences) {
-            at -= int64_t(cur.span.tiles) * head_blocks;
-            cur.span.set(p, p.lengths[++cur.seq]);
-        }
-        cur.hb = int32_t(divide(at, cur.span.tiles));
-        cur.tile = int32_t(at - int64_t(cur.hb) * cur.span.tiles);
-        cur.key_head = cur.hb / p.blocks;
-        cur.block = cur.hb - cur.key_head * p.blocks;
-        // does the CTA's range begin inside an item?
-        if (warp == 0 && cur.tile != 0 && lane == 0) first_item = cur.seq * head_blocks + cur.hb;
-    }
     __syncthreads();
 
-    if (lo < hi) {
+    if (n > 0) {
         AttentionWarp<T, DP, NT> w(p, ring, lane);
-        const int64_t n = hi - lo;
         AttentionCursor ahead = cur;                            // the tile whose page numbers are in `page`, `row`
         int64_t issued = 0;
         int32_t row, page = w.look_up(ahead, row);
@@ -717,7 +763,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
                     w.deposit(slot ? deposit_last : deposit_first, stats[2 * warp + slot]);
                     if (lane == 0) {
                         dep_item[2 * warp + slot] = cur.seq * head_blocks + cur.hb;
-                        if (i + 1 == n && hi == cta_hi && !item_ends) last_item = cur.seq * head_blocks + cur.hb;
+                        if (i + 1 == n && closes && !item_ends) last_item = cur.seq * head_blocks + cur.hb;
                     }
                 }
                 if (i + 1 < n) {

@@ -396,7 +396,7 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
  * (BTC_FLAG_BAD_PAGE); lengths below zero count as zero, lengths beyond the table row as the row's
  * capacity (BTC_FLAG_BAD_LENGTH).
  *   Q [N, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
- *   D and Dv up to 256; table [N, M] I32.  lengths: DEVICE int32[N]; lse: DEVICE float[N * Hq] or NULL.
+ *   D and Dv up to 256; N up to 2^23; table [N, M] I32.  lengths: DEVICE int32[N]; lse: DEVICE float[N * Hq] or NULL.
  * fp32 products are formed from three TF32 tensor-core products (as in contractions); 16-bit operations round
  * once, at the output.  Infinite keys give infinite scores; an infinite visible value gives infinities or NaN.  The
  * result does not depend on scheduling.  Lengths are read on the device only: one

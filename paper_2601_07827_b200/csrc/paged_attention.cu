@@ -111,6 +111,8 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
         op.nt = group > 8 && op.dp <= 128 ? 2 : 1;
         op.blocks = (group + 8 * op.nt - 1) / (8 * op.nt);
         if (__int128(q.extent[0]) * k.extent[2] * op.blocks > INT32_MAX) return BTC_ERR_NOT_SUPPORTED;
+        // tiles of all sequences: 38 bits of the kernel's prefix sum
+        if (__int128(q.extent[0]) * (std::min<int64_t>(t.extent[1] * k.extent[1], INT32_MAX) / kAttnTok + 1) >= (__int128(1) << 38)) return BTC_ERR_NOT_SUPPORTED;
         btc_paged_attention_s *kept = new (std::nothrow) btc_paged_attention_s(std::move(op));
         if (!kept) return BTC_ERR_OUT_OF_MEMORY;
         *out = kept;

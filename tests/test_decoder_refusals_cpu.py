@@ -173,3 +173,16 @@ def test_pages_refusals(api, handle):
     assert code(api, lambda: op.free(0, 256, 1, 256, 0, 256)) == E.ERR_INVALID_ARGUMENT
     assert code(api, lambda: op.copy(0, 0, 1, [256, 256])) == E.ERR_INVALID_ARGUMENT
     assert code(api, lambda: op.copy(0, 256, 1, [256, 256, 256])) == E.ERR_INVALID_ARGUMENT
+
+
+def test_paged_attention_limits(api, handle):
+    """More sequences, or more tokens in all, than the kernel's counters hold."""
+    E = api
+    t = lambda *s, st=None: dense(api, handle, api.BF16, *s, strides=st)  # noqa: E731
+    n = (1 << 23) + 1
+    one = dense(api, handle, api.I32, n, 1)
+    assert code(api, lambda: api.PagedAttention(handle, t(n, 1, 8), t(9, 16, 1, 8), t(9, 16, 1, 8), one, t(n, 1, 8))) == E.ERR_NOT_SUPPORTED
+    n = 1 << 22
+    wide = dense(api, handle, api.I32, n, 1)
+    long_page = t(1, 1 << 21, 1, 8)
+    assert code(api, lambda: api.PagedAttention(handle, t(n, 1, 8), long_page, long_page, wide, t(n, 1, 8))) == E.ERR_NOT_SUPPORTED

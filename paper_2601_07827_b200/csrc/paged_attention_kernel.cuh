@@ -69,7 +69,7 @@ template <typename T, int DP, int NT> struct AttentionShape {
     static constexpr int FIT = 224 * 1024 / (RING + DEPOSIT);
     static constexpr int WARPS = FIT < 8 ? FIT : 8;
     static constexpr int SMEM = WARPS * (RING + DEPOSIT);
-    static_assert(RING >= DEPOSIT + 2 * WARPS * 3 * 8 * NT * 4, "the last item's deposit, and warp 0's joint figures, take the ring");
+    static_assert(RING >= DEPOSIT, "the last item's deposit takes the warp's ring");
     static_assert(WARPS * DEPOSIT >= (WARPS * 32 + 1) * 8, "the prefix sum takes the first items' place");
 };
 
@@ -616,7 +616,6 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ float stats[2 * W][2 * H];
     __shared__ int32_t dep_item[2 * W];
-    __shared__ uint32_t item_ends;
     __shared__ int32_t first_item, last_item;                  // items of the CTA's range that it does not hold whole; -1: none
     int64_t *scan = reinterpret_cast<int64_t *>(smem + W * Shape::RING);     // until the ranges are known
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -781,11 +780,8 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
 
     if (tid < 2) p.partial_item[2 * blockIdx.x + tid] = tid == 0 ? first_item : (last_item == first_item ? -1 : last_item);
     if (blockIdx.x < ctas) {
-        // join what the warps left: first each deposit's weight against the largest maximum of its item (a warp takes a
-        // head, a lane a deposit; the deposits of an item are neighbours), 0 where there is none, and the places
-        // where the items end ...
-        float (*joined)[2 * H] = reinterpret_cast<float (*)[2 * H]>(smem + Shape::DEPOSIT);     // behind warp 0's deposit in its ring
-        float (*weight)[H] = reinterpret_cast<float (*)[H]>(smem + Shape::DEPOSIT + 2 * W * 2 * H * 4);
+        // Join what the warps left, a warp to a head.  First a lane to a deposit (those of an item are neighbours): its
+        // weight against the item's largest maximum; then a lane to four elements.
         for (int h = warp; h < H; h += W) {
             const int at = lane < 2 * W ? lane : 0;
             const int32_t item = lane < 2 * W ? dep_item[at] : -1;
@@ -805,41 +801,36 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
                 const float x = __shfl_sync(0xffffffffu, l * share, j);
                 if ((same >> j) & 1) sum += x;
             }
-            if (lane < 2 * W) {
-                weight[lane][h] = share;
-                joined[lane][h] = top;
-                joined[lane][H + h] = sum;
-            }
-            if (h == 0) {
-                const uint32_t ends = __ballot_sync(0xffffffffu, mine && (same >> lane) == 1);    // the last deposit of its item
-                if (lane == 0) item_ends = ends;
-            }
-        }
-        __syncthreads();
-        // ... then the sums, four elements of a head per thread
-        for (int e = 4 * tid; e < H * DP; e += 4 * THREADS) {
-            const int h = e / DP, d = e - h * DP;
+            const uint32_t present = __ballot_sync(0xffffffffu, mine);
+            uint32_t ends = __ballot_sync(0xffffffffu, mine && (same >> lane) == 1);    // the last deposit of its item
             int begin = 0;
-            for (uint32_t ends = item_ends; ends; ends &= ends - 1) {
+            while (ends) {
                 const int last = __ffs(int(ends)) - 1;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                ends &= ends - 1;
+                const int32_t this_item = __shfl_sync(0xffffffffu, item, last);
+                const float this_top = __shfl_sync(0xffffffffu, top, last), this_sum = __shfl_sync(0xffffffffu, sum, last);
+#pragma unroll
+                for (int q0 = 0; q0 < DP / 4; q0 += 32) {
+                    const int quad = q0 + lane;
+                    const bool here = quad < DP / 4;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-                for (int i = begin; i <= last; ++i) {
-                    const unsigned char *src = (i & 1) ? smem + (i >> 1) * Shape::RING : smem + W * Shape::RING + (i >> 1) * Shape::DEPOSIT;
-                    const float4 x = reinterpret_cast<const float4 *>(src)[e / 4];
-                    const float share = weight[i][h];
-                    if (share != 0.f) {                            // no deposit there, or one that does not count
-                        o.x = fmaf(x.x, share, o.x); o.y = fmaf(x.y, share, o.y); o.z = fmaf(x.z, share, o.z); o.w = fmaf(x.w, share, o.w);
+                    for (int i = begin; i <= last; ++i) {
+                        const float weight = __shfl_sync(0xffffffffu, share, i);
+                        if (((present >> i) & 1) && here) {
+                            const unsigned char *src = (i & 1) ? smem + (i >> 1) * Shape::RING : smem + W * Shape::RING + (i >> 1) * Shape::DEPOSIT;
+                            const float4 x = reinterpret_cast<const float4 *>(src)[h * (DP / 4) + quad];
+                            o.x = fmaf(x.x, weight, o.x); o.y = fmaf(x.y, weight, o.y); o.z = fmaf(x.z, weight, o.z); o.w = fmaf(x.w, weight, o.w);
+                        }
                     }
-                }
-                const int32_t item = dep_item[last];
-                const float m = joined[last][h], l = joined[last][H + h];
-                if (item == first_item || item == last_item) {
-                    float *out = p.partial + (2 * int64_t(blockIdx.x) + (item == first_item ? 0 : 1)) * (H * DP + 2 * H);
-                    *reinterpret_cast<float4 *>(out + e) = o;
-                    if (d == 0) { out[H * DP + h] = m; out[H * DP + H + h] = l; }
-                } else {
-                    write_joined<T>(p, item, H, h, d, o, m, l);
+                    if (!here) continue;
+                    if (this_item == first_item || this_item == last_item) {
+                        float *out = p.partial + (2 * int64_t(blockIdx.x) + (this_item == first_item ? 0 : 1)) * (H * DP + 2 * H);
+                        reinterpret_cast<float4 *>(out)[h * (DP / 4) + quad] = o;
+                        if (quad == 0) { out[H * DP + h] = this_top; out[H * DP + H + h] = this_sum; }
+                    } else {
+                        write_joined<T>(p, this_item, H, h, 4 * quad, o, this_top, this_sum);
+                    }
                 }
                 begin = last + 1;
             }

@@ -9,6 +9,8 @@
 // results do not depend on scheduling (the only atomics are integer additions).
 // Page contents move with 16-byte accesses where sizes, strides and addresses allow, 16 KB per CTA and step: bound by
 // HBM (each byte is read once and written once).
+// Measured (replayed graphs): 8 sequences freed, 8 forked and 64 extended by a token 14.6 us, the same over 1000 sequences and
+// 200000 pages 21.5 us; a compaction that moves 235 MB of pages 87 us, of which the copy is 70 (6.7 TB/s).
 #pragma once
 
 #include "../../include/btc.h"
@@ -230,8 +232,9 @@ pages_extend_kernel(const __grid_constant__ PagesParams p)
     pages_cluster_sync();                                // the old state has been read, the list is complete
 
     // A warp per sequence, or, where calls bring a few tokens a sequence, a thread: a step is a chain of dependent
-    // accesses, and 8 CTAs of warps would go through 1000 sequences in four rounds of it
-    const int wide = p.most <= 8 ? 1 : 32, part_lane = tid & (wide - 1);
+    // accesses, and 8 CTAs of warps would go through 1000 sequences in four rounds of it.  1000 sequences, threads / warps:
+    // 21.6 / 24.5 us for 1 token each, 25.5 / 25.9 for 16, 31.0 / 25.9 for 32, 62 / 32 for 128
+    const int wide = p.most <= 16 ? 1 : 32, part_lane = tid & (wide - 1);
     for (int32_t s = s_lo + tid / wide; s < s_hi; s += kPagesThreads / wide) {
         const int32_t info = p.rank[s], add = p.fresh[s], length = p.lengths[s];
         const int64_t begin = p.begin[s];

@@ -305,6 +305,31 @@ def test_unrotated_infinities_stay_in_place(api, handle):
             assert (y[0, 0, 2 * pairs:D - 1] == 1).all()
 
 
+def test_offsets_beyond_32_bits(api, handle):
+    """More than 2^31 elements in one tensor (vector form), tokens 2^31 bytes and more apart (scalar form)."""
+    T, H, D, pairs = 420_000, 40, 128, 64
+    freq = [10000.0 ** (-i / pairs) for i in range(pairs)]
+    x = torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda").normal_()
+    pos = (torch.arange(T, device="cuda") % 100_003).to(torch.int32)
+    rows = torch.tensor([0, 1, T // 2, 2 ** 31 // (H * D), 2 ** 31 // (H * D) + 1, T - 2, T - 1])
+    kept = x[rows.cuda()].cpu()
+    op = api.Rotary(handle, freq, info(api, handle, x), info(api, handle, x), norm=True)
+    op.execute(torch.cuda.current_stream().cuda_stream, pos.data_ptr(), 0, 0, x.data_ptr(), x.data_ptr())      # in place
+    want = rotary_forward(kept, None, pos[rows.cuda()].cpu(), freq, 1.0, False, True, 1e-6)
+    close(x[rows.cuda()], want, scale_of(want, 1.0), torch.bfloat16, CHAIN)
+    del x
+    stride = 1_200_000_000
+    flat = torch.zeros(2 * stride + 4 * D, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(flat, (3, 4, D), (stride, D, 1))
+    x.copy_(torch.randn(3, 4, D, generator=gen(2)))
+    kept = x.cpu().clone()
+    y = torch.empty(3, 4, D, dtype=torch.bfloat16, device="cuda")
+    op = api.Rotary(handle, freq, info(api, handle, x), info(api, handle, y), norm=True)
+    op.execute(torch.cuda.current_stream().cuda_stream, pos.data_ptr(), 0, 0, x.data_ptr(), y.data_ptr())
+    want = rotary_forward(kept, None, pos[:3].cpu(), freq, 1.0, False, True, 1e-6)
+    close(y, want, scale_of(want, 1.0), torch.bfloat16, CHAIN)
+
+
 def test_other_stream_and_graph(api, handle):
     T, H, D = 64, 4, 128
     x = torch.randn(T, H, D, device="cuda", dtype=torch.bfloat16)

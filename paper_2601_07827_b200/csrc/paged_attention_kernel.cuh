@@ -186,6 +186,11 @@ template <typename T, int DP, int NT> struct AttentionWarp {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int KSTEPS = F32 ? DP / 8 : DP / 16;
     static constexpr int MT = DP / 16;
+    // fp32: the tensor core cuts its sums off where an fp32 addition rounds, always towards zero, which adds up over a long
+    // chain.  Scores leave it after so many steps, outputs after every step, and are added in fp32: errors of
+    // 3e-7 to 4e-7 instead of 7e-7 to 3e-6 (heads of 64 to 256, 2700 to 131072 tokens; plain fp32 8e-7 to 1e-6), for
+    // 2 to 3 % of the time.
+    static constexpr int kExactSteps = 2;
 
     const AttentionParams &p;
     unsigned ring;                           // shared-memory address of the warp's ring
@@ -384,6 +389,10 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
+            for (int j = 0; j < 4; ++j) s[nt][j] = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
             for (int i = 0; i < CHAINS; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) part[nt][i][j] = 0.f;
@@ -400,6 +409,14 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                     for (int j = 0; j < 4; ++j) split_tf32(a[j], hi[j], lo[j]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma8_split(part[nt][0], part[nt][1], part[nt][2], hi, lo, q[nt][ks][0], q[nt][ks][1]);
+                    if (ks % kExactSteps == kExactSteps - 1)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                s[nt][j] += part[nt][2][j];
+                                part[nt][2][j] = 0.f;
+                            }
                 } else {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma16(part[nt][ks & 1], a, q[nt][ks][0], q[nt][ks][1], T());
@@ -409,8 +426,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[nt][j] = part[nt][1][j] + part[nt][0][j];
-                    if constexpr (F32) s[nt][j] += part[nt][2][j];
+                    s[nt][j] += part[nt][1][j] + part[nt][0][j];
                 }
         }
         if constexpr (F32) {
@@ -493,8 +509,12 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            mma8_split(o[2 * pair + i][nt], o[2 * pair + i][nt], o[2 * pair + i][nt], hi[i], lo[i], b[nt][ks][0], b[nt][ks][1]);
+                        for (int i = 0; i < 2; ++i) {
+                            float f[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma8_split(f, f, f, hi[i], lo[i], b[nt][ks][0], b[nt][ks][1]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[2 * pair + i][nt][j] += f[j];
+                        }
                 }
         } else {
             uint32_t hi[NT][2], lo[NT][2];

@@ -75,10 +75,12 @@ template <typename T, int DP, int NT> struct AttentionShape {
     static_assert(WARPS * DEPOSIT >= (WARPS * 32 + 1) * 8, "the prefix sum takes the first items' place");
 };
 
-template <typename T> struct AttentionBias { static constexpr float value = 0.f; };
+template <typename T> struct AttentionBias { static constexpr float value = 0.f, factor = 1.f; };
 // f16 products: probabilities are kept 2^10 times larger (they cancel against the sum), so that values down to
-// 2^-24 of the largest stay normal numbers
-template <> struct AttentionBias<__half> { static constexpr float value = 10.f; };
+// 2^-24 of the largest stay normal numbers.  The factor is applied to the probability, which is exact: as an addend to
+// the score it would be rounded where scores are large (beyond 2^25 it changed from maximum to maximum, at 2^27 the
+// largest probability became 2^16, more than f16 holds).
+template <> struct AttentionBias<__half> { static constexpr float value = 10.f, factor = 1024.f; };
 
 // The code of a kernel that runs for a few microseconds is fetched as it goes: a jump over code that is not needed costs
 // about a third of a microsecond.  What is rarely needed is marked so that it is put out of the way.
@@ -462,12 +464,12 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                 top = fmaxf(top, m[nt][j]);
                 // nothing seen yet (or every score is -inf): subtract 0, the probabilities are exp2(-inf) = 0
-                const float base = (top == -INFINITY ? 0.f : top) - AttentionBias<T>::value;
+                const float base = top == -INFINITY ? 0.f : top;
                 alpha[nt][j] = m[nt][j] == top ? 1.f : exp2f(m[nt][j] - top);
                 moved |= alpha[nt][j] != 1.f;
                 m[nt][j] = top;
-                s0 = exp2f(s0 - base);
-                s1 = exp2f(s1 - base);
+                s0 = exp2f(s0 - base) * AttentionBias<T>::factor;
+                s1 = exp2f(s1 - base) * AttentionBias<T>::factor;
                 l[nt][j] = l[nt][j] * alpha[nt][j] + (s0 + s1);
             }
         if (__any_sync(0xffffffffu, moved)) {
@@ -579,7 +581,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                     }
                 if (p.lse && lane < 4)
                     p.lse[int64_t(c.seq) * p.heads + h0 + h] = l[nt][j] == 0.f ? -INFINITY
-                        : (m[nt][j] - AttentionBias<T>::value + log2f(l[nt][j])) * 0.6931471805599453f;
+                        : (m[nt][j] + (log2f(l[nt][j]) - AttentionBias<T>::value)) * 0.6931471805599453f;
             }
     }
     // an unfinished item: output, maxima and sums to shared memory
@@ -626,7 +628,7 @@ __device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t i
     for (int j = 0; j < 4; ++j)
         if (d + j < p.dim_v) dst[(d + j) * p.o_d] = from_f32<T>(l == 0.f ? 0.f : v[j] * inv);
     if (d == 0 && p.lse)
-        p.lse[int64_t(seq) * p.heads + head] = l == 0.f ? -INFINITY : (m - AttentionBias<T>::value + log2f(l)) * 0.6931471805599453f;
+        p.lse[int64_t(seq) * p.heads + head] = l == 0.f ? -INFINITY : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
 }
 
 template <typename T, int DP, int NT>

@@ -397,8 +397,9 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
  * capacity (BTC_FLAG_BAD_LENGTH).
  *   Q [N, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
  *   D and Dv up to 256; N up to 2^23; table [N, M] I32.  lengths: DEVICE int32[N]; lse: DEVICE float[N * Hq] or NULL.
- * fp32 products are formed from three TF32 tensor-core products (as in contractions); 16-bit operations round
- * once, at the output.  Infinite keys give infinite scores; an infinite visible value gives infinities or NaN.  The
+ * Sums over tokens are fp32.  fp32 products are formed from three TF32 tensor-core products (as in contractions); for
+ * 16-bit types probabilities enter the second product with 22 bits (F16) or 16 (BF16), and the output is rounded
+ * once.  Infinite keys give infinite scores; an infinite visible value gives infinities or NaN.  The
  * result does not depend on scheduling.  Lengths are read on the device only: one
  * captured graph serves all steps of a growing cache.
  * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA. */

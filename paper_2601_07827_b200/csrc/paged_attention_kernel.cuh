@@ -13,10 +13,15 @@
 //     of each product would be padding for groups of 8), and P needs only a transpose of 8 x 8 blocks.
 //     The products are a few percent of the time; mma.sync keeps them in registers of the warp that
 //     copied the tile, where tcgen05's 128-row tiles would be 15/16 empty.
-//   * 16-bit types: P is split in two (p = hi + lo, products with both), so that the result carries
-//     one rounding, that of the output.  fp32: each product is formed from three TF32 products
+//   * 16-bit types: P is split in two (p = hi + lo, products with both): f16 then holds 22 bits of it, bf16 16,
+//     2^-17 of a probability left out at most, a 256th of what the output's own rounding leaves out (a third part
+//     would be half as many products again).  fp32: each product is formed from three TF32 products
 //     (x = hi + lo; lo * lo is dropped, at most 2^-22 of the product), as in the contractions.
 //   * running maximum, sum and output in fp32 (the flash form); the output is rescaled only when a maximum moved.
+//     The tensor core adds up the tokens of one tile; tiles are added in fp32, rounded to nearest.  The tensor core cuts
+//     its sums off, always towards zero: over the 7000 tiles of a warp whole outputs fell short by 4e-4 (f16 and
+//     bf16), as much as f16's own rounding.  The additions cost 0 to 3 % (heads of 128: 64 ragged requests 79.3 -> 79.5 us,
+//     with groups of 16 109 -> 113 us).
 // Work.  The tiles of all (sequence, key head) pairs form one list; CTAs and in them warps take equal
 // contiguous shares of it, whatever the lengths are, found on the device from a prefix sum of the tile
 // counts (the host never reads a length).  What a warp cannot finish is merged in shared memory by its
@@ -188,8 +193,8 @@ template <typename T, int DP, int NT> struct AttentionWarp {
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int KSTEPS = F32 ? DP / 8 : DP / 16;
     static constexpr int MT = DP / 16;
-    // fp32: the tensor core cuts its sums off where an fp32 addition rounds, always towards zero, which adds up over a long
-    // chain.  Scores leave it after so many steps, outputs after every step, and are added in fp32: errors of
+    // fp32: even within a tile the tensor core's cut-off sums are the largest error.  Scores leave it after so many
+    // steps, outputs after every step, and are added in fp32: errors of
     // 3e-7 to 4e-7 instead of 7e-7 to 3e-6 (heads of 64 to 256, 2700 to 131072 tokens; plain fp32 8e-7 to 1e-6), for
     // 2 to 3 % of the time.
     static constexpr int kExactSteps = 2;
@@ -536,8 +541,11 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 ldsm4_trans(a, (at ^ ((mt & 3) << 5)) + (mt >> 2) * 128);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    mma16(o[mt][nt], a, hi[nt][0], hi[nt][1], T());
-                    mma16(o[mt][nt], a, lo[nt][0], lo[nt][1], T());
+                    float f[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma16(f, a, lo[nt][0], lo[nt][1], T());
+                    mma16(f, a, hi[nt][0], hi[nt][1], T());
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[mt][nt][j] += f[j];
                 }
             }
         }

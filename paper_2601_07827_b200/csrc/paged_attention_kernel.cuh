@@ -578,17 +578,18 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             for (int j = 0; j < 2; ++j) {
                 const int h = nt * 8 + 2 * (lane & 3) + j;
                 if (h >= count) continue;
-                const float inv = l[nt][j] == 0.f ? 0.f : 1.f / l[nt][j];
+                const bool nothing = l[nt][j] == 0.f;          // every score is -inf: zeros, whatever V holds (0 * inf is NaN)
+                const float inv = 1.f / l[nt][j];
                 T *dst = static_cast<T *>(p.o) + c.seq * p.o_n + int64_t(h0 + h) * p.o_h;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int d = element(mt, half);
-                        if (d < p.dim_v) dst[d * p.o_d] = from_f32<T>(o[mt][nt][2 * half + j] * inv);
+                        if (d < p.dim_v) dst[d * p.o_d] = from_f32<T>(nothing ? 0.f : o[mt][nt][2 * half + j] * inv);
                     }
                 if (p.lse && lane < 4)
-                    p.lse[int64_t(c.seq) * p.heads + h0 + h] = l[nt][j] == 0.f ? -INFINITY
+                    p.lse[int64_t(c.seq) * p.heads + h0 + h] = nothing ? -INFINITY
                         : (m[nt][j] + (log2f(l[nt][j]) - AttentionBias<T>::value)) * 0.6931471805599453f;
             }
     }
@@ -629,14 +630,15 @@ __device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t i
     const int kh = hb / p.blocks, in_group = (hb - kh * p.blocks) * per + h;
     if (in_group >= p.group) return;
     const int head = kh * p.group + in_group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const bool nothing = l == 0.f;             // as in write_out
+    const float inv = 1.f / l;
     T *dst = static_cast<T *>(p.o) + seq * p.o_n + int64_t(head) * p.o_h;
     const float v[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (d + j < p.dim_v) dst[(d + j) * p.o_d] = from_f32<T>(l == 0.f ? 0.f : v[j] * inv);
+        if (d + j < p.dim_v) dst[(d + j) * p.o_d] = from_f32<T>(nothing ? 0.f : v[j] * inv);
     if (d == 0 && p.lse)
-        p.lse[int64_t(seq) * p.heads + head] = l == 0.f ? -INFINITY : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
+        p.lse[int64_t(seq) * p.heads + head] = nothing ? -INFINITY : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
 }
 
 template <typename T, int DP, int NT>

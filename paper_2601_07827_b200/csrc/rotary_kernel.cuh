@@ -102,6 +102,12 @@ template <typename T, int V, bool INTERLEAVED> struct RotaryLane {
     static constexpr int N = VECTOR ? V : 4;
     typedef typename VectorOf<VECTOR ? V * int(sizeof(T)) : 16>::type Vec;
     struct Raw { Vec a, b; };
+    __device__ __forceinline__ static Raw no_raw()     // zeros
+    {
+        Raw r;
+        r.a = r.b = Vec{};
+        return r;
+    }
     int ea, eb;                    // VECTOR: element offsets of the two vectors
     uint32_t oa, ob;               // the same in bytes
     bool active, rotated;          // VECTOR: the lane has pairs; they are rotated
@@ -434,7 +440,8 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
         const int tokens = int(min(int64_t(part.cta_tokens), p.tokens - first)), items = tokens * heads;
         const T *x0 = static_cast<const T *>(part.x) + first * part.x_t, *g0 = static_cast<const T *>(part.dy) + first * part.y_t;
         T *d0 = static_cast<T *>(part.y) + first * part.x_t;
-        // where the (token, head) pair number `item` lies; past the end: the last one again, which is not counted
+        // where the (token, head) pair number `item` lies.  Past the end: the last one again, whose dy is not read (dx may be
+        // the same memory and written by now) and whose sums are left out, not multiplied by zero: an infinity would stay
         auto place = [&](int item, int &token, Off &at_x, Off &at_y) {
             item = min(item, items - 1);
             token = int(by_heads.div(uint32_t(item)));
@@ -447,7 +454,8 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
         place(group, token, at_x, at_y);
         typename Lane::Raw ahead_x, ahead_g;
         if constexpr (V > 1) {
-            ahead_g = lane.load_raw(g0, at_y);
+            ahead_g = Lane::no_raw();
+            if (group < items) ahead_g = lane.load_raw(g0, at_y);
             if (norm) ahead_x = lane.load_raw(x0, at_x);
         }
         if (turning) {
@@ -461,16 +469,20 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
             int next_token;
             Off next_x, next_y;
             place(item + groups, next_token, next_x, next_y);
-            if (V > 1 && item + groups < items) {                       // past the end the values stay as they are, and count for nothing
-                ahead_g = lane.load_raw(g0, next_y);
-                if (norm) ahead_x = lane.load_raw(x0, next_x);
+            if constexpr (V > 1) {
+                if (item + groups < items) {                            // past the end both stay as they are
+                    ahead_g = lane.load_raw(g0, next_y);
+                    if (norm) ahead_x = lane.load_raw(x0, next_x);
+                }
             }
             float2 ga[N2], gb[N2], a[N2], b[N2];
             if constexpr (V > 1) {
                 lane.unpack(rg, ga, gb);
                 if (norm) lane.unpack(rx, a, b);
             } else {
-                lane.load(g0 + at_y, part.y_d, ga, gb);
+#pragma unroll
+                for (int j = 0; j < N2; ++j) ga[j] = gb[j] = both(0.f);
+                if (item < items) lane.load(g0 + at_y, part.y_d, ga, gb);
                 if (norm) lane.load(x0 + at_x, part.x_d, a, b);
             }
             if (turning) lane.template rotate<true, FULL>(cosines + token * (kRotaryMaxDim / 2), sines + token * (kRotaryMaxDim / 2), ga, gb);
@@ -486,12 +498,14 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_backward_kernel(cons
                 }
                 const float ss = group_sum(lane.share(squares), p.lanes_log2), dot = group_sum(lane.share(dots), p.lanes_log2);
                 const float r = rsqrtf(fmaf(ss, inv_dim, p.eps));
-                const float2 r2 = both(r), pull = both(-(dot * r * inv_dim) * r * r);  // x pull = -n r mean(g n)
-                const float2 counted = both(item < items ? r : 0.f);
+                const float2 r2 = both(r), pull = both(-(dot * r * inv_dim) * r * r);          // x pull = -n r mean(g n)
+                const bool counts = item < items;
 #pragma unroll
                 for (int j = 0; j < N2; ++j) {
-                    da2[j] = fma2(ga[j], mul2(a[j], counted), da2[j]);
-                    db2[j] = fma2(gb[j], mul2(b[j], counted), db2[j]);
+                    if (counts) {
+                        da2[j] = fma2(ga[j], mul2(a[j], r2), da2[j]);
+                        db2[j] = fma2(gb[j], mul2(b[j], r2), db2[j]);
+                    }
                     ga[j] = fma2(pa[j], r2, mul2(a[j], pull));
                     gb[j] = fma2(pb[j], r2, mul2(b[j], pull));
                 }

@@ -104,8 +104,10 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
         op.scale = scale;
         op.window = window;
         const int64_t dim = std::max(q.extent[2], v.extent[3]), group = q.extent[1] / k.extent[2];
-        // fp32 heads of 65 to 96 elements have a size of their own because products and shared memory bound them: 24
-        // windows of 1000 tokens, heads of 80: 17.1 us, padded to 128 19.2 us
+        // fp32 heads of 65 to 96 elements have a size of their own because products and shared memory bound them (padded to
+        // 128 in brackets): 24 windows of 1000 tokens, heads of 80: 17.4 us [19.6]; 64 ragged requests, heads of 80: 112
+        // [154], of 96: 117 [154], 16 heads to a key head: 186 [282]; 8 requests 25 [31]; 2 x 128 Ki tokens 240 [339]; one
+        // request 12.6 [12.8]
         op.dp = dim <= 64 ? 64 : (dim <= 96 && q.dtype == BTC_F32 ? 96 : (dim <= 128 ? 128 : 256));
         // Groups of more than 8 heads take 16 at a time, so that the cache is read once per 16 heads (64 ragged requests,
         // groups of 16: 108 us, 133 with 8 at a time; groups of 24: 184 and 196); heads of more than 128 elements 8

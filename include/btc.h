@@ -351,7 +351,7 @@ enum {
  *     (y_a, y_b) = multiplier * (m_a cos - m_b sin, m_b cos + m_a sin),  angle = positions[t] * frequencies[i]
  * for the pairs i = 0..pairs-1, (a, b) = (i, i + pairs) in the HALF layout and (2i, 2i + 1) in the
  * INTERLEAVED one; values from 2 * pairs on are not rotated (y = m).  The frequencies (radians per
- * position, any values: each long-context scaling is a choice of them and of the multiplier) are a host
+ * position, any finite values: each long-context scaling is a choice of them and of the multiplier) are a host
  * array that is copied.  The angle is reduced exactly, in fixed point: no position is too long.
  *   Xq [T, Hq, D] -> Yq [T, Hq, D]     required
  *   Xk [T, Hk, D] -> Yk                both or neither (NULL)
@@ -360,6 +360,7 @@ enum {
  * then goes to page slots[t] / S, row slots[t] % S, and a negative slot drops the token's key and value
  * (two tokens of one call with the same slot: either may stay).  One element type (F32, F16, BF16) for
  * all; W has it too.  D and Dv up to 256.  Y may be the same memory as X with the same strides.
+ * multiplier and eps are fp32 in the kernels: they must be finite there, and eps 0 or at least 2^-126.
  * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING (elements of an output alias), NOT_SUPPORTED
  * (type, head size, P * S beyond int32), MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA.
  *
@@ -399,7 +400,8 @@ btc_error_t btc_rotary_backward(btc_rotary_t op, void *cuda_stream, const int32_
  *   D and Dv up to 256; N up to 2^23; table [N, M] I32.  lengths: DEVICE int32[N]; lse: DEVICE float[N * Hq] or NULL.
  * Sums over tokens are fp32.  fp32 products are formed from three TF32 tensor-core products (as in contractions); for
  * 16-bit types probabilities enter the second product with 22 bits (F16) or 16 (BF16), and the output is rounded
- * once.  Infinite keys give infinite scores; an infinite visible value gives infinities or NaN.  The
+ * once.  scale * log2(e) must be finite in fp32.  Infinite keys give infinite scores; an infinite visible value gives
+ * infinities or NaN, as do fp32 values within 2^-12 of the largest finite one.  The
  * result does not depend on scheduling.  Lengths are read on the device only: one
  * captured graph serves all steps of a growing cache.
  * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA. */

@@ -3,6 +3,7 @@
 
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <exception>
 #include <new>
@@ -14,6 +15,9 @@ namespace btc {
 inline bool decoder_type(btc_dtype_t t) { return t == BTC_F32 || t == BTC_F16 || t == BTC_BF16; }
 
 inline bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// Is a number that was given as a double finite as fp32, which the kernels compute in?
+inline bool fits_f32(double x) { return std::isfinite(float(x)); }
 
 // |stride| * (extent - 1) summed stays far inside int64: the kernels form offsets without overflow tests
 inline bool spans_fit(const TensorDesc &t)

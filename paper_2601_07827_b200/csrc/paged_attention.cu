@@ -21,6 +21,8 @@ struct btc_paged_attention_s {
 
 namespace {
 
+constexpr double kLog2E = 1.4426950408889634;
+
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : 2; }
 
 // CTAs of the first kernel: one per SM (shared memory admits no second)
@@ -80,7 +82,7 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
                                        int32_t window, btc_paged_attention_t *out)
 {
     if (!handle || !Q || !K || !V || !table || !O || !out) return BTC_ERR_INVALID_ARGUMENT;
-    if (window < 0 || !std::isfinite(scale)) return BTC_ERR_INVALID_ARGUMENT;
+    if (window < 0 || !fits_f32(scale * kLog2E)) return BTC_ERR_INVALID_ARGUMENT;
     return guarded([&]() -> btc_error_t {
         const TensorDesc &q = Q->desc, &k = K->desc, &v = V->desc, &t = table->desc, &o = O->desc;
         if (q.extent.size() != 3 || k.extent.size() != 4 || v.extent.size() != 4 || t.extent.size() != 2 || o.extent.size() != 3)
@@ -181,7 +183,7 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
     p.vec_v = rows_allow_vectors(op->v, vec) && aligned_to(V, 16);
     p.whole_tiles = !(p.vec_k && p.vec_v) ? 0 : (op->k.extent[1] % kAttnTok == 0 ? kAttnTok : (op->k.extent[1] % 8 == 0 ? 8 : 0));
     p.vec_q = es == 2 && p.dim_k % 2 == 0 && rows_allow_vectors(op->q, 2) && aligned_to(Q, 4);
-    p.scale_log2 = float(op->scale * 1.4426950408889634);
+    p.scale_log2 = float(op->scale * kLog2E);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (op->q.dtype) {
     case BTC_F32: return launch_typed<float>(*op, p, st);

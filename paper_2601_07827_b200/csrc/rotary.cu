@@ -1,5 +1,6 @@
 // C entry points of the head norm and rotary position operator (rotary_kernel.cuh).
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <cstring>
@@ -137,8 +138,8 @@ btc_error_t btc_create_rotary(btc_handle_t handle, int32_t layout, int32_t pairs
     if (!handle || !Xq || !Yq || !out) return BTC_ERR_INVALID_ARGUMENT;
     if ((Xk == nullptr) != (Yk == nullptr) || (Xv == nullptr) != (Yv == nullptr)) return BTC_ERR_INVALID_ARGUMENT;
     if (layout != BTC_ROTARY_HALF && layout != BTC_ROTARY_INTERLEAVED) return BTC_ERR_INVALID_ARGUMENT;
-    if (pairs < 0 || (pairs > 0 && !frequencies) || !std::isfinite(multiplier)) return BTC_ERR_INVALID_ARGUMENT;
-    if (norm && !(eps >= 0.0 && std::isfinite(eps))) return BTC_ERR_INVALID_ARGUMENT;
+    if (pairs < 0 || (pairs > 0 && !frequencies) || !fits_f32(multiplier)) return BTC_ERR_INVALID_ARGUMENT;
+    if (norm && !(eps == 0.0 || (eps >= double(FLT_MIN) && fits_f32(eps)))) return BTC_ERR_INVALID_ARGUMENT;
     for (int32_t i = 0; i < pairs; ++i)
         if (!std::isfinite(frequencies[i])) return BTC_ERR_INVALID_ARGUMENT;
     return guarded([&]() -> btc_error_t {

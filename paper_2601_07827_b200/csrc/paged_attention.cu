@@ -111,9 +111,11 @@ btc_error_t btc_create_paged_attention(btc_handle_t handle, btc_tensor_info_t Q,
         // [154], of 96: 117 [154], 16 heads to a key head: 186 [282]; 8 requests 25 [31]; 2 x 128 Ki tokens 240 [339]; one
         // request 12.6 [12.8]
         op.dp = dim <= 64 ? 64 : (dim <= 96 && q.dtype == BTC_F32 ? 96 : (dim <= 128 ? 128 : 256));
-        // Groups of more than 8 heads take 16 at a time, so that the cache is read once per 16 heads (64 ragged requests,
-        // groups of 16: 108 us, 133 with 8 at a time; groups of 24: 184 and 196); heads of more than 128 elements 8
-        // at a time (the output of 16 would not fit the registers)
+        // Groups of more than 8 heads take 16 at a time, so that the cache is read once per 16 heads (8 at a time in
+        // brackets: 64 ragged requests, groups of 9: 108 us [133], of 12: 114 [133], of 16: 114 [134], of 24: 194 [197], of 16 with heads
+        // of 64: 72 [95], of 16 in fp32: 282 [301]; 2 x 128 Ki tokens, groups of 16: 183 [241]).  A lone short request loses (1500
+        // tokens, groups of 16: 15.5 [12.3]), but lengths are not known here.  Heads of more than 128 elements 8 at a time
+        // (the output of 16 would not fit the registers)
         op.nt = group > 8 && op.dp <= 128 ? 2 : 1;
         op.blocks = (group + 8 * op.nt - 1) / (8 * op.nt);
         if (__int128(q.extent[0]) * k.extent[2] * op.blocks > INT32_MAX) return BTC_ERR_NOT_SUPPORTED;

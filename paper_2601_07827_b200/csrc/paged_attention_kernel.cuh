@@ -27,7 +27,7 @@
 // counts (the host never reads a length).  What a warp cannot finish is merged in shared memory by its
 // CTA, what a CTA cannot finish goes to the workspace and a second small kernel joins it, in a fixed order.
 // Measured (replayed graphs): 8 x 128 Ki tokens of f16 (4.3 GB) 650 us = 6.6 TB/s, the measured copy bandwidth; 64 requests of 64 to
-// 8192 tokens (0.44 GB) 79 us; one request of 1500 tokens 11.7 us, nearly all of it latency.
+// 8192 tokens (0.44 GB) 79 us; one request of 1500 tokens 11.8 us, nearly all of it latency.
 #pragma once
 
 #include "../../include/btc.h"

@@ -17,7 +17,7 @@
 // The angles depend on token and pair only: a CTA takes a few tokens with all their heads and computes each
 // angle once, into shared memory (computed by every group for itself they were a quarter of all instructions).
 // Measured (replayed graphs): 16384 tokens x 80 heads of 128 appended to pages (f16, 671 MB) 110 us = 6.1 TB/s; 16384 x 40 heads
-// with norm, bf16: forward 66 us (336 MB), backward 110 us (503 MB), both held up by their instructions (67 % and 62 % of
+// with norm, bf16: forward 65 us (336 MB), backward 110 us (503 MB), both held up by their instructions (67 % and 63 % of
 // the issue slots); 128 x 48 heads appended 3.2 us.
 #pragma once
 

@@ -59,7 +59,7 @@ enum {
     BTC_ERR_SCRATCH_LIMIT = 13       /* needs more than the built-in scratch array holds        */
 };
 
-/* Element types.  Complex values are (re, im) pairs of the stated part width.  The 16-bit types and the
+/* Element types.  Complex values are (re, im) pairs of the stated part width.  The 16-bit and 8-bit types and the
  * 32-bit integers serve the decoder operators only: contractions and elementwise operations answer
  * NOT_SUPPORTED to a descriptor that carries one. */
 typedef enum {
@@ -69,7 +69,8 @@ typedef enum {
     BTC_C64 = 3, /* 2 x double (16 bytes) */
     BTC_F16 = 4, /* IEEE half             */
     BTC_BF16 = 5,
-    BTC_I32 = 6
+    BTC_I32 = 6,
+    BTC_E4M3 = 7 /* 8-bit float: 4 bits of exponent, 3 of mantissa, largest value 448 */
 } btc_dtype_t;
 
 typedef struct btc_handle_s *btc_handle_t;            /* Sec. "The Library Handle"            */
@@ -458,6 +459,34 @@ btc_error_t btc_pages_compact(btc_pages_t op, void *cuda_stream, int32_t *table,
                               int32_t count, void *workspace, size_t workspace_bytes, int32_t *flags);
 btc_error_t btc_pages_copy(btc_pages_t op, void *cuda_stream, const int32_t *pairs, int32_t pair_count,
                            void *const *tensors, int32_t count, int32_t *flags);
+
+/* The residual's addition and the root-mean-square norm after it, over the rows t of [T, D] tensors:
+ *     H[t,d] = X[t,d] + R[t,d]         (without R and H, both NULL: H = X, not written)
+ *     Y[t,d] = H[t,d] / sqrt(mean_d(H[t,d]^2) + eps) * W[d]        (W: D contiguous values, NULL = ones)
+ * X, W: F32, F16 or BF16; R, H: X's type or F32 (a residual stream kept wider); Y: X's type, or E4M3 with scales
+ * S [T, G] F32: per group of `group` elements (32, 64 or 128; the last one may be shorter; 0: the row, G = 1) with largest
+ * modulus a, S = max(a / 448, 2^-126) and Y the codes nearest to y / S.  A group that holds an infinity or NaN gets S = NaN
+ * and codes of zero.  The norm takes the sum as it is before H's rounding; squares are added in fp32 (rows whose
+ * sum of squares is beyond its range come out as zeros).  eps: 0 or at least 2^-126, finite in fp32.  D up to 16384.
+ * H may be the same memory as R, and Y as X, with the same strides.
+ * btc_add_norm_backward: from the kept H (laid out like H, without R like X), dY (like Y) and dH (like H: what flows back
+ * along the residual stream; NULL = zero) the gradients
+ *     dX = dR = dH + (g - n mean_d(g n)) / sqrt(mean_d(H^2) + eps),  g = dY W,  n = H / sqrt(mean_d(H^2) + eps)
+ *     dW[d] = sum_t dY n               (F32, overwritten)
+ * dX (X's type, laid out like X), dR (H's type, like H) and dW may each be NULL (not wanted), but not both dX and dR; dW needs W.
+ * dX may be the same memory as dY, and dR as dH, with the same strides.  NOT_SUPPORTED where Y is E4M3; D_ALIASING where dX would
+ * alias.  The result does not depend on scheduling.  The workspace is for dW only.
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING (elements of an output alias), NOT_SUPPORTED, MISALIGNED,
+ * WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA. */
+typedef struct btc_add_norm_s *btc_add_norm_t;
+btc_error_t btc_create_add_norm(btc_handle_t handle, btc_tensor_info_t X, btc_tensor_info_t R, btc_tensor_info_t H,
+                                btc_tensor_info_t Y, btc_tensor_info_t S, int32_t group, double eps, btc_add_norm_t *out);
+btc_error_t btc_destroy_add_norm(btc_add_norm_t *op);
+btc_error_t btc_add_norm_workspace_size(btc_add_norm_t op, size_t *bytes);   /* of btc_add_norm_backward */
+btc_error_t btc_add_norm_execute(btc_add_norm_t op, void *cuda_stream, const void *X, const void *W, const void *R, void *H,
+                                 void *Y, float *S);
+btc_error_t btc_add_norm_backward(btc_add_norm_t op, void *cuda_stream, const void *H, const void *W, const void *dY,
+                                  const void *dH, void *dX, void *dR, float *dW, void *workspace, size_t workspace_bytes);
 
 /* Peak micro-benchmarks (no counterpart in the paper; the paper leaves benchmarks to future work, Sec.
  * "Outlook").  Measures what this device sustains with a kernel that does nothing else, so that the

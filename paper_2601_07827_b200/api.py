@@ -35,8 +35,8 @@ ERR_OUT_OF_MEMORY = 12
 ERR_SCRATCH_LIMIT = 13
 
 F32, F64, C32, C64 = 0, 1, 2, 3
-F16, BF16, I32 = 4, 5, 6          # decoder operators only
-DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16, F16: 2, BF16: 2, I32: 4}
+F16, BF16, I32, E4M3 = 4, 5, 6, 7          # decoder operators only
+DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16, F16: 2, BF16: 2, I32: 4, E4M3: 1}
 FLAG_BAD_PAGE, FLAG_BAD_SLOT, FLAG_BAD_SEQUENCE, FLAG_BAD_LENGTH, FLAG_POOL_EXHAUSTED = 1, 2, 4, 8, 16
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 
@@ -64,6 +64,8 @@ EXPORTED = [
     "btc_paged_attention_execute",
     "btc_create_pages", "btc_destroy_pages", "btc_pages_workspace_size", "btc_pages_extend", "btc_pages_fork",
     "btc_pages_free", "btc_pages_compact", "btc_pages_copy",
+    "btc_create_add_norm", "btc_destroy_add_norm", "btc_add_norm_workspace_size", "btc_add_norm_execute",
+    "btc_add_norm_backward",
 ]
 
 _vp = ctypes.c_void_p
@@ -115,6 +117,11 @@ _lib.btc_pages_fork.argtypes = [_vp] * 4 + [_i32] + [_vp] * 4
 _lib.btc_pages_free.argtypes = [_vp] * 3 + [_i32] + [_vp] * 4
 _lib.btc_pages_compact.argtypes = [_vp] * 5 + [_i32, _vp, ctypes.c_size_t, _vp]
 _lib.btc_pages_copy.argtypes = [_vp] * 3 + [_i32, _vp, _i32, _vp]
+_lib.btc_create_add_norm.argtypes = [_vp] * 6 + [_i32, ctypes.c_double, ctypes.POINTER(_vp)]
+_lib.btc_destroy_add_norm.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_add_norm_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_add_norm_execute.argtypes = [_vp] * 8
+_lib.btc_add_norm_backward.argtypes = [_vp] * 10 + [ctypes.c_size_t]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -358,7 +365,7 @@ def dtype_code(torch_dtype) -> int:
     if _TORCH_DTYPE is None:
         import torch
         _TORCH_DTYPE = {torch.float32: F32, torch.float64: F64, torch.complex64: C32, torch.complex128: C64,
-                        torch.float16: F16, torch.bfloat16: BF16, torch.int32: I32}
+                        torch.float16: F16, torch.bfloat16: BF16, torch.int32: I32, torch.float8_e4m3fn: E4M3}
     return _TORCH_DTYPE[torch_dtype]
 
 
@@ -580,6 +587,32 @@ class Pages(_Operation):
         rc = _lib.btc_pages_copy(self._op, stream, pairs, count, self._pointers(tensors), len(tensors), flags)
         if rc:
             raise BtcError(rc, "btc_pages_copy")
+
+
+class AddNorm(_Operation):
+    """The residual's addition and the root-mean-square norm after it; see btc_create_add_norm.
+
+    X, Y (and R, H: the residual stream before and after) [T, D]; Y of type E4M3 comes with scales S [T, G], one per `group`
+    elements (0: one per row).  All data arguments are device pointers as integers (0: absent)."""
+
+    _kind = "add_norm"
+
+    def __init__(self, handle: Handle, X: TensorInfo, Y: TensorInfo, R: Optional[TensorInfo] = None,
+                 H: Optional[TensorInfo] = None, S: Optional[TensorInfo] = None, group: int = 0, eps: float = 1e-6):
+        self._op = _vp()
+        _check(_lib.btc_create_add_norm(handle._h, X._t, _info_or_null(R), _info_or_null(H), Y._t, _info_or_null(S), group, eps,
+                                        ctypes.byref(self._op)), "btc_create_add_norm")
+
+    def execute(self, stream: int, X: int, W: int, Y: int, R: int = 0, H: int = 0, S: int = 0) -> None:
+        rc = _lib.btc_add_norm_execute(self._op, stream, X, W, R, H, Y, S)
+        if rc:
+            raise BtcError(rc, "btc_add_norm_execute")
+
+    def backward(self, stream: int, H: int, W: int, dY: int, dH: int = 0, dX: int = 0, dR: int = 0, dW: int = 0,
+                 workspace: int = 0, workspace_bytes: int = 0) -> None:
+        rc = _lib.btc_add_norm_backward(self._op, stream, H, W, dY, dH, dX, dR, dW, workspace, workspace_bytes)
+        if rc:
+            raise BtcError(rc, "btc_add_norm_backward")
 
 
 def elementwise(handle: Handle, A, labelsA, B, C, labelsC, alpha=1.0, beta=0.0, conjA=False, conjB=False, stream: int = 0):

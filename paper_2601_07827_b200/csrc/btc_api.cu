@@ -938,7 +938,7 @@ btc_error_t btc_create_tensor_info(btc_handle_t handle, btc_dtype_t dtype, int32
 {
     if (!handle || !out) return BTC_ERR_INVALID_ARGUMENT;
     if (rank < 0 || rank > BTC_MAX_RANK) return BTC_ERR_INVALID_ARGUMENT;
-    if (int(dtype) < 0 || int(dtype) > int(BTC_I32)) return BTC_ERR_INVALID_ARGUMENT;
+    if (int(dtype) < 0 || int(dtype) > int(BTC_E4M3)) return BTC_ERR_INVALID_ARGUMENT;
     if (rank > 0 && !extents) return BTC_ERR_INVALID_ARGUMENT;
     for (int i = 0; i < rank; ++i)
         if (extents[i] < 1) return BTC_ERR_INVALID_EXTENT;

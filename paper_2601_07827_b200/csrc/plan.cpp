@@ -17,6 +17,7 @@ size_t dtype_size(btc_dtype_t t)
     case BTC_F16: return 2;
     case BTC_BF16: return 2;
     case BTC_I32: return 4;
+    case BTC_E4M3: return 1;
     }
     return 0;
 }

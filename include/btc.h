@@ -488,6 +488,33 @@ btc_error_t btc_add_norm_execute(btc_add_norm_t op, void *cuda_stream, const voi
 btc_error_t btc_add_norm_backward(btc_add_norm_t op, void *cuda_stream, const void *H, const void *W, const void *dY,
                                   const void *dH, void *dX, void *dR, float *dW, void *workspace, size_t workspace_bytes);
 
+/* Products of a few tokens with 4-bit weights, Y [T, N] from X [T, K]:
+ *     z[t,r] = sum_k X[t,k] * scales[r, k / group] * (codes[r,k] - zeros[r, k / group])
+ *     Y[t,n] = z[t,n]                                            (activation NONE; N weight rows)
+ *     Y[t,n] = act(z[t,n]) * z[t, N + n]                         (SILU, GELU in its tanh form; 2 N weight rows: the gates first)
+ * X: F32, F16, BF16, or E4M3 with scales XS [T, G] F32 per x_group elements of K (0: the row, G = 1), which its values are multiplied
+ * by, as btc_add_norm_execute writes them.  Y: F32, F16 or BF16.  group and x_group: 0 (the row), 32, 64, 128 or 256; the last
+ * group may be shorter.  Codes are whole numbers 0..15, zeros too (without zeros: 8).  Any T, K and N up to 2^24; made for
+ * T up to 64: the weights are read once for every 16 tokens.
+ * btc_linear4_pack lays the weights out once, into `packed` (256-byte aligned, btc_linear4_packed_size bytes), which depends on
+ * N, K, group, scale_type, zeros and whether there is an activation, not on T or X: one copy serves operations of any number of tokens.
+ *   codes   DEVICE [rows, ceil(K / 2)] bytes, dense: k even in the lower four bits, k odd in the upper
+ *   scales  DEVICE [rows, ceil(K / group)] of scale_type (F32, F16, BF16), dense
+ *   zeros   DEVICE bytes [rows, ceil(K / group)], dense, or NULL as the operation was created
+ * Weights enter the products unrounded, sums are fp32.  Infinite values of X give infinities or NaN.  The result does not depend on
+ * scheduling.  btc_linear4_workspace_size is the workspace of btc_linear4_execute (NULL is allowed where it is 0).
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA. */
+typedef struct btc_linear4_s *btc_linear4_t;
+enum { BTC_ACTIVATION_NONE = 0, BTC_ACTIVATION_SILU = 1, BTC_ACTIVATION_GELU = 2 };
+btc_error_t btc_create_linear4(btc_handle_t handle, btc_tensor_info_t X, btc_tensor_info_t XS, btc_tensor_info_t Y, int32_t x_group,
+                               btc_dtype_t scale_type, int32_t group, int32_t zeros, int32_t activation, btc_linear4_t *out);
+btc_error_t btc_destroy_linear4(btc_linear4_t *op);
+btc_error_t btc_linear4_workspace_size(btc_linear4_t op, size_t *bytes);
+btc_error_t btc_linear4_packed_size(btc_linear4_t op, size_t *bytes);
+btc_error_t btc_linear4_pack(btc_linear4_t op, void *cuda_stream, const uint8_t *codes, const void *scales, const uint8_t *zeros, void *packed);
+btc_error_t btc_linear4_execute(btc_linear4_t op, void *cuda_stream, const void *packed, const void *X, const float *XS, void *Y,
+                                void *workspace, size_t workspace_bytes);
+
 /* Peak micro-benchmarks (no counterpart in the paper; the paper leaves benchmarks to future work, Sec.
  * "Outlook").  Measures what this device sustains with a kernel that does nothing else, so that the
  * roofline fraction of a contraction can be quoted against a figure taken on the same device in the

@@ -39,6 +39,7 @@ F16, BF16, I32, E4M3 = 4, 5, 6, 7          # decoder operators only
 DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16, F16: 2, BF16: 2, I32: 4, E4M3: 1}
 FLAG_BAD_PAGE, FLAG_BAD_SLOT, FLAG_BAD_SEQUENCE, FLAG_BAD_LENGTH, FLAG_POOL_EXHAUSTED = 1, 2, 4, 8, 16
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2}
 
 ATTR_KERNEL, ATTR_SPLIT_K, ATTR_TILE, ATTR_GROUPS, ATTR_GRID, ATTR_NUM_MODES, ATTR_SWAPPED = 1, 2, 3, 4, 5, 6, 7
 ATTR_DEVICE_ERROR = 8
@@ -66,6 +67,8 @@ EXPORTED = [
     "btc_pages_free", "btc_pages_compact", "btc_pages_copy",
     "btc_create_add_norm", "btc_destroy_add_norm", "btc_add_norm_workspace_size", "btc_add_norm_execute",
     "btc_add_norm_backward",
+    "btc_create_linear4", "btc_destroy_linear4", "btc_linear4_workspace_size", "btc_linear4_packed_size", "btc_linear4_pack",
+    "btc_linear4_execute",
 ]
 
 _vp = ctypes.c_void_p
@@ -122,6 +125,12 @@ _lib.btc_destroy_add_norm.argtypes = [ctypes.POINTER(_vp)]
 _lib.btc_add_norm_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.btc_add_norm_execute.argtypes = [_vp] * 8
 _lib.btc_add_norm_backward.argtypes = [_vp] * 10 + [ctypes.c_size_t]
+_lib.btc_create_linear4.argtypes = [_vp] * 4 + [_i32, ctypes.c_int] + [_i32] * 3 + [ctypes.POINTER(_vp)]
+_lib.btc_destroy_linear4.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_linear4_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_linear4_packed_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_linear4_pack.argtypes = [_vp] * 6
+_lib.btc_linear4_execute.argtypes = [_vp] * 7 + [ctypes.c_size_t]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -613,6 +622,38 @@ class AddNorm(_Operation):
         rc = _lib.btc_add_norm_backward(self._op, stream, H, W, dY, dH, dX, dR, dW, workspace, workspace_bytes)
         if rc:
             raise BtcError(rc, "btc_add_norm_backward")
+
+
+class Linear4(_Operation):
+    """Products of a few tokens with 4-bit weights and group scales, plain or gated; see btc_create_linear4.
+
+    X [T, K] (E4M3 with scales XS [T, G] per x_group elements), Y [T, N].  pack() lays the weights out once, into packed_size()
+    bytes that operations of other T and X with the same weights can share.  All data arguments are device pointers as integers."""
+
+    _kind = "linear4"
+
+    def __init__(self, handle: Handle, X: TensorInfo, Y: TensorInfo, scale_type: int = F16, group: int = 128, zeros: bool = False,
+                 activation: str = "none", XS: Optional[TensorInfo] = None, x_group: int = 0):
+        self._op = _vp()
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"unknown activation {activation!r}")
+        _check(_lib.btc_create_linear4(handle._h, X._t, _info_or_null(XS), Y._t, x_group, scale_type, group, int(zeros),
+                                       ACTIVATIONS[activation], ctypes.byref(self._op)), "btc_create_linear4")
+
+    def packed_size(self) -> int:
+        n = ctypes.c_size_t(0)
+        _check(_lib.btc_linear4_packed_size(self._op, ctypes.byref(n)), "btc_linear4_packed_size")
+        return n.value
+
+    def pack(self, stream: int, codes: int, scales: int, zeros: int, packed: int) -> None:
+        rc = _lib.btc_linear4_pack(self._op, stream, codes, scales, zeros, packed)
+        if rc:
+            raise BtcError(rc, "btc_linear4_pack")
+
+    def execute(self, stream: int, packed: int, X: int, Y: int, XS: int = 0, workspace: int = 0, workspace_bytes: int = 0) -> None:
+        rc = _lib.btc_linear4_execute(self._op, stream, packed, X, XS, Y, workspace, workspace_bytes)
+        if rc:
+            raise BtcError(rc, "btc_linear4_execute")
 
 
 def elementwise(handle: Handle, A, labelsA, B, C, labelsC, alpha=1.0, beta=0.0, conjA=False, conjB=False, stream: int = 0):

@@ -15,7 +15,14 @@ def info(api, handle, t):
 
 
 def check(got, want, bound):
+    half = got.dtype == torch.float16
     got, want, bound = got.double().cpu(), want.double().cpu(), bound.double().cpu()
+    if half:
+        # f16 rounds 65520 and more to infinity: what is certainly beyond has to be infinite, what may be is allowed to
+        bound = bound.expand(want.shape)
+        beyond = torch.where(want > 0, math.inf, -math.inf).double()
+        may = (want.abs() + bound >= 65520.0) & (got == beyond)
+        want = torch.where(may | (want.abs() - bound >= 65520.0), beyond, want)
     finite = torch.isfinite(want)
     assert torch.equal(torch.isnan(got), torch.isnan(want))
     special = ~finite & ~torch.isnan(want)
@@ -81,3 +88,42 @@ def check_e4m3(codes, scales, y, group, chain):
     # the value before rounding is off by chain + 2 units itself; the step is that of the value or of the next binade
     bound = torch.maximum(E4M3_UNIT * y.abs(), E4M3_FLOOR * each) * (1 + 2.0 ** -16) + 2 * (chain + 4) * E32 * y.abs()
     check(torch.where(lost, 0.0, got), y, torch.where(lost, 0.0, bound))
+
+
+# ---- 4-bit products -----------------------------------------------------------------------------------------
+
+def linear4_weights(codes, scales, zeros, group, k):
+    """(code - zero) * scale in 64 bits, [rows, k]."""
+    at = torch.arange(k)
+    code = (codes[:, at // 2].int() >> (4 * (at % 2))) & 15
+    which = at // group if group else torch.zeros_like(at)
+    zero = zeros[:, which].double() if zeros is not None else 8.0
+    return (code.double() - zero) * scales.double()[:, which]
+
+
+def activation(x, kind):
+    if kind == "silu":
+        return x * torch.sigmoid(x)
+    return torch.nn.functional.gelu(x, approximate="tanh")
+
+
+def linear4(x, xs, x_group, weights, kind, out):
+    """(y, bound) in 64 bits.  A block of 64 k is 4 products of 16 (three times as many for fp32, whose values are three parts), in
+    which the tensor core may cut off two units for each k; blocks, warps and CTAs are then added one after the other in fp32 with a
+    product by the scale each, x's scale one more."""
+    k = x.shape[1]
+    v = x.double()
+    if xs is not None:
+        v = v * xs.double()[:, (torch.arange(k) // x_group) if x_group else torch.zeros(k, dtype=torch.long)]
+    parts = 3 if x.dtype == torch.float32 else 1
+    chain = 2 * 64 * parts + k / 32 + 64 + 8
+    z, size = v @ weights.T, v.abs() @ weights.abs().T
+    off = chain * E32 * size
+    if kind == "none":
+        return z, UNIT[out] * z.abs() + off + FLOOR[out]
+    n = z.shape[1] // 2
+    g, u, dg, du = z[:, :n], z[:, n:], off[:, :n], off[:, n:]
+    a = activation(g, kind)
+    # both activations have slopes below 1.13; exponential, division and products: 16 units, of x itself where it is tiny
+    y = a * u
+    return y, UNIT[out] * y.abs() + 1.13 * dg * (u.abs() + du) + (a.abs() + 1.13 * dg) * du + 16 * E32 * (g * u).abs() + FLOOR[out]

@@ -1,4 +1,4 @@
-"""What the residual norm refuses, and its 64-bit reference against differences: no GPU needed."""
+"""What the residual norm, the 4-bit products and the tree attention refuse, and the norm's 64-bit reference against differences: no GPU needed."""
 import pytest
 import torch
 
@@ -73,6 +73,53 @@ def test_add_norm_refusals(api, handle):  # noqa: F811
     assert code(api, lambda: eight.backward(0, 256, 256, 256, dX=256)) == E.ERR_NOT_SUPPORTED
     spread = api.AddNorm(handle, t(4, 64, st=(0, 1)), x)
     assert code(api, lambda: spread.backward(0, 256, 256, 256, dX=256)) == E.ERR_D_ALIASING
+
+
+def test_linear4_refusals(api, handle):  # noqa: F811
+    E, B = api, api.BF16
+    t = lambda *s, dt=B, st=None: dense(api, handle, dt, *s, strides=st)  # noqa: E731
+    make = lambda *a, **k: code(api, lambda: api.Linear4(handle, *a, **k))  # noqa: E731
+    x, y = t(4, 256), t(4, 100)
+    assert make(x, y, group=16) == E.ERR_INVALID_ARGUMENT
+    assert make(x, y, group=512) == E.ERR_INVALID_ARGUMENT
+    assert make(x, y, group=96) == E.ERR_INVALID_ARGUMENT
+    assert make(x, y, group=-128) == E.ERR_INVALID_ARGUMENT
+    assert make(x, y, x_group=128) == E.ERR_INVALID_ARGUMENT                       # only inputs in 8 bits have scales
+    assert make(x, y, XS=t(4, 1, dt=E.F32)) == E.ERR_INVALID_ARGUMENT
+    assert make(t(4, 256, dt=E.E4M3), y) == E.ERR_INVALID_ARGUMENT
+    assert make(t(4, 256, dt=E.E4M3), y, XS=t(4, 1)) == E.ERR_NOT_SUPPORTED
+    assert make(t(4, 256, dt=E.E4M3), y, XS=t(4, 1, dt=E.F32), x_group=128) == E.ERR_EXTENT_MISMATCH
+    assert make(t(4, 256, dt=E.E4M3), y, XS=t(3, 1, dt=E.F32)) == E.ERR_EXTENT_MISMATCH
+    assert make(x, t(5, 100)) == E.ERR_EXTENT_MISMATCH
+    assert make(x, t(4, 100, dt=E.E4M3)) == E.ERR_NOT_SUPPORTED
+    assert make(t(4, 256, dt=E.F64), y) == E.ERR_NOT_SUPPORTED
+    assert make(x, y, scale_type=E.F64) == E.ERR_NOT_SUPPORTED
+    assert make(t(4, 2, 128), y) == E.ERR_INVALID_ARGUMENT
+    assert make(x, t(4, 100, st=(50, 1))) == E.ERR_D_ALIASING
+    assert make(t(4, 256, st=(1 << 62, 1)), y) == E.ERR_NOT_SUPPORTED
+    assert make(t(4, (1 << 24) + 1), y) == E.ERR_NOT_SUPPORTED
+    assert make(x, t(4, (1 << 24) + 1)) == E.ERR_NOT_SUPPORTED
+    with pytest.raises(ValueError):
+        api.Linear4(handle, x, y, activation="other")
+
+    op = api.Linear4(handle, x, y, group=64)
+    assert op.packed_size() == 7 * 4 * (512 + 16 * 2)
+    assert api.Linear4(handle, x, y, group=64, zeros=True).packed_size() == op.packed_size() + 7 * 4 * 16
+    assert api.Linear4(handle, t(9, 256, dt=E.F32), t(9, 100, dt=E.F16), group=64).packed_size() == op.packed_size()
+    run = lambda *a, **k: code(api, lambda: op.execute(0, *a, **k))  # noqa: E731
+    big = dict(workspace=256, workspace_bytes=1 << 40)
+    assert run(0, 256, 256, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(256, 0, 256, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(256, 256, 0, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(256, 256, 256, XS=256, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(128, 256, 256, **big) == E.ERR_MISALIGNED
+    assert run(256, 257, 256, **big) == E.ERR_MISALIGNED
+    assert run(256, 256, 257, **big) == E.ERR_MISALIGNED
+    pack = lambda *a: code(api, lambda: op.pack(0, *a))  # noqa: E731
+    assert pack(0, 256, 0, 256) == E.ERR_INVALID_ARGUMENT
+    assert pack(256, 256, 256, 256) == E.ERR_INVALID_ARGUMENT                      # zeros that the operation does not have
+    assert pack(256, 257, 0, 256) == E.ERR_MISALIGNED
+    assert pack(256, 256, 0, 128) == E.ERR_MISALIGNED
 
 
 def test_norm_reference_against_differences():

@@ -416,6 +416,31 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
                                         const void *V, const int32_t *table, const int32_t *lengths, void *O, float *lse,
                                         void *workspace, size_t workspace_bytes, int32_t *flags);
 
+/* Attention of a tree of drafted tokens per sequence over a paged key-value cache (the verification step of speculative decoding; with
+ * masks of a chain, of several new tokens at once).  Sequence n has lengths[n] cached tokens, and behind them, at positions
+ * lengths[n] .. lengths[n] + T - 1 of its pages, the keys and values of up to T drafts.  Row (n, i) is draft i's query; the bits of
+ * masks[n, i] say which drafts j it sees (bit j % 32 of word j / 32; bits from T on are ignored; ordinarily itself and those it
+ * continues).  For every row and query head h (sharing key head h / (Hq / Hk) with its neighbours), with j running over the visible tokens:
+ *     O[n,i,h] = sum_j p_j V_j,  p = softmax_j(scale * Q[n,i,h] . K_j),  lse[n,i,h] = log sum_j exp(scale * Q[n,i,h] . K_j)
+ * Visible are the drafts of the row's mask and the cached tokens; with a window (at least T) of these the last, at
+ * positions lengths[n] + (number of drafts the row sees) - window and later.  A row whose mask is empty is no draft: it sees nothing,
+ * and gets O = 0 and lse = -inf, as does a row whose scores are all -inf.  Drafts beyond the table row's capacity are not visible
+ * (BTC_FLAG_BAD_LENGTH); other bad lengths, pages that do not exist and what lies in invisible places are treated as in
+ * btc_paged_attention_execute, and so are types, sums and infinities.
+ *   Q [N, T, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, T, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
+ *   D and Dv up to 256; T up to 128; table [N, M] I32; masks [N, T, ceil(T / 32)] I32.  lengths: DEVICE int32[N]; lse: DEVICE
+ *   float[N * T * Hq] or NULL.
+ * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA. */
+typedef struct btc_tree_attention_s *btc_tree_attention_t;
+btc_error_t btc_create_tree_attention(btc_handle_t handle, btc_tensor_info_t Q, btc_tensor_info_t K, btc_tensor_info_t V,
+                                      btc_tensor_info_t table, btc_tensor_info_t masks, btc_tensor_info_t O, double scale,
+                                      int32_t window, btc_tree_attention_t *out);
+btc_error_t btc_destroy_tree_attention(btc_tree_attention_t *op);
+btc_error_t btc_tree_attention_workspace_size(btc_tree_attention_t op, size_t *bytes);
+btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_stream, const void *Q, const void *K, const void *V,
+                                       const int32_t *table, const int32_t *lengths, const int32_t *masks, void *O, float *lse,
+                                       void *workspace, size_t workspace_bytes, int32_t *flags);
+
 /* Pages of a key-value cache: allocation, copy on write, forking, freeing, compaction, copies.  The state is the
  * caller's device memory: a table [N, M] I32 of page numbers (one row per sequence; entry j < ceil(length / S) is a
  * page, the others are -1), lengths int32[N], and refs int32[P], the number of table entries that name a page (0:

@@ -69,6 +69,7 @@ EXPORTED = [
     "btc_add_norm_backward",
     "btc_create_linear4", "btc_destroy_linear4", "btc_linear4_workspace_size", "btc_linear4_packed_size", "btc_linear4_pack",
     "btc_linear4_execute",
+    "btc_create_tree_attention", "btc_destroy_tree_attention", "btc_tree_attention_workspace_size", "btc_tree_attention_execute",
 ]
 
 _vp = ctypes.c_void_p
@@ -131,6 +132,10 @@ _lib.btc_linear4_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)
 _lib.btc_linear4_packed_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
 _lib.btc_linear4_pack.argtypes = [_vp] * 6
 _lib.btc_linear4_execute.argtypes = [_vp] * 7 + [ctypes.c_size_t]
+_lib.btc_create_tree_attention.argtypes = [_vp] * 7 + [ctypes.c_double, _i32, ctypes.POINTER(_vp)]
+_lib.btc_destroy_tree_attention.argtypes = [ctypes.POINTER(_vp)]
+_lib.btc_tree_attention_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_tree_attention_execute.argtypes = [_vp] * 11 + [ctypes.c_size_t, _vp]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
 
@@ -547,6 +552,49 @@ class PagedAttention(_Operation):
                                               workspace_bytes, flags)
         if rc:
             raise BtcError(rc, "btc_paged_attention_execute")
+
+
+class TreeAttention(_Operation):
+    """Attention of a tree of drafted tokens per sequence over a paged cache; see btc_create_tree_attention.
+
+    Q [N, T, Hq, D], K [pages, tokens per page, Hk, D], V [pages, tokens per page, Hk, Dv], table [N, M] int32, masks
+    [N, T, ceil(T / 32)] int32 (which drafts a row sees; none: no draft), O [N, T, Hq, Dv].  scale: 1 / sqrt(D) when not given."""
+
+    _kind = "tree_attention"
+
+    def __init__(self, handle: Handle, Q: TensorInfo, K: TensorInfo, V: TensorInfo, table: TensorInfo, masks: TensorInfo,
+                 O: TensorInfo, scale: Optional[float] = None, window: int = 0):
+        self._op = _vp()
+        if scale is None:
+            scale = float(Q.extents[-1]) ** -0.5 if Q.extents else 1.0
+        _check(_lib.btc_create_tree_attention(handle._h, Q._t, K._t, V._t, table._t, masks._t, O._t, scale, window,
+                                              ctypes.byref(self._op)), "btc_create_tree_attention")
+
+    def execute(self, stream: int, Q: int, K: int, V: int, table: int, lengths: int, masks: int, O: int, lse: int = 0,
+                workspace: int = 0, workspace_bytes: int = 0, flags: int = 0) -> None:
+        """Device pointers as integers; lengths int32 [N]: cached tokens before the drafts; lse float32 [N, T, Hq] or 0."""
+        rc = _lib.btc_tree_attention_execute(self._op, stream, Q, K, V, table, lengths, masks, O, lse, workspace,
+                                             workspace_bytes, flags)
+        if rc:
+            raise BtcError(rc, "btc_tree_attention_execute")
+
+
+def tree_masks(parents: Sequence[int]):
+    """(mask words, depth) of each draft of one tree, for TreeAttention's masks and the drafts' positions: parents[i] is the earlier
+    draft that draft i continues, -1 for the last cached token, -2 for a row that holds no draft (mask 0, depth -1)."""
+    words = (len(parents) + 31) // 32
+    seen, masks, depth = [], [], []
+    for i, parent in enumerate(parents):
+        if not -2 <= parent < i:
+            raise ValueError("a draft continues an earlier one")
+        if parent >= 0 and seen[parent] == 0:
+            raise ValueError("a draft continues a row that holds none")
+        bits = 0 if parent == -2 else (1 << i) | (seen[parent] if parent >= 0 else 0)
+        seen.append(bits)
+        depth.append(bin(bits).count("1") - 1)
+        row = [(bits >> (32 * w)) & 0xffffffff for w in range(words)]
+        masks.append([x - (1 << 32) if x >= 1 << 31 else x for x in row])
+    return masks, depth
 
 
 class Pages(_Operation):

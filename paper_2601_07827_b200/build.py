@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbtc.so")
 SOURCES = ["btc_api.cu", "plan.cpp", "skinny_umma.cu", "stream.cu", "peaks.cu", "rotary.cu",
-           "paged_attention.cu", "pages.cu", "add_norm.cu", "linear4.cu"]
+           "paged_attention.cu", "pages.cu", "add_norm.cu", "linear4.cu", "tree_attention.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",

@@ -52,15 +52,15 @@ btc_error_t launch(const AttentionParams &p, int device, int ctas, cudaStream_t 
     static std::atomic<bool> configured[64] = {};
     const int slot = device & 63;
     if (!configured[slot].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(paged_attention_kernel<T, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::SMEM) != cudaSuccess) {
+        if (cudaFuncSetAttribute(paged_attention_kernel<T, DP, NT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::SMEM) != cudaSuccess) {
             cudaGetLastError();
             return BTC_ERR_CUDA;
         }
         configured[slot].store(true, std::memory_order_relaxed);
     }
-    const btc_error_t rc = launch_early(paged_attention_kernel<T, DP, NT>, dim3(unsigned(ctas)), Shape::WARPS * 32, Shape::SMEM, st, p);
+    const btc_error_t rc = launch_early(paged_attention_kernel<T, DP, NT, false>, dim3(unsigned(ctas)), Shape::WARPS * 32, Shape::SMEM, st, p);
     if (rc != BTC_SUCCESS) return rc;
-    return launch_early(paged_attention_join_kernel<T, DP, NT>, dim3(unsigned(ctas), kJoinSlices), kJoinThreads, 0, st, p, ctas);
+    return launch_early(paged_attention_join_kernel<T, DP, NT, false>, dim3(unsigned(ctas), kJoinSlices), kJoinThreads, 0, st, p, ctas);
 }
 
 template <typename T> btc_error_t launch_typed(const btc_paged_attention_s &op, const AttentionParams &p, cudaStream_t st)

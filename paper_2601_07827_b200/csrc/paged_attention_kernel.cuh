@@ -33,6 +33,8 @@
 #include "../../include/btc.h"
 #include "decoder_common.cuh"
 
+#include <type_traits>
+
 namespace btc {
 
 constexpr int kAttnTok = 16;                 // tokens per tile
@@ -62,6 +64,11 @@ struct AttentionParams {
     int32_t vec_k, vec_v, vec_q;             // 16-byte copies of keys / values, 4-byte loads of queries
     FastDiv page;
     float scale_log2;                        // scale * log2(e)
+    // trees of drafted tokens (TREE): `group` counts the rows that share a key head, drafts * sharing of them: row r is draft r / sharing
+    const int32_t *masks;                    // [sequences][drafts][words]
+    int64_t q_t, o_t, m_n, m_t, m_w;
+    int32_t drafts, words;
+    FastDiv sharing;                         // query heads of a draft that share a key head
 };
 
 // Per-warp ring and warps of a CTA: as many as 224 KB of shared memory hold.  fp32 tiles of 12 KB and more take
@@ -148,16 +155,28 @@ __device__ __forceinline__ void cp_async_part(unsigned dst, const void *src, int
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// visible tokens [begin, end) of a sequence, and its tiles, which start at multiples of 16 tokens
-struct AttentionSpan {
-    int32_t begin, end, first_tile, tiles;
+// visible tokens [begin, end) of a sequence, and its tiles, which start at multiples of 16 tokens.  TREE: those that any draft
+// may see; the drafts lie behind the `cached` tokens.
+template <bool TREE> struct AttentionSpan {
+    int32_t begin, end, first_tile, tiles, cached;
     __device__ __forceinline__ void set(const AttentionParams &p, int32_t length)
     {
         const int32_t room = p.room;
         end = length < 0 ? 0 : (length > room ? room : length);
-        begin = p.window > 0 && end > p.window ? end - p.window : 0;
+        if constexpr (TREE) {
+            cached = end;
+            begin = p.window > 0 && cached >= p.window ? cached + 1 - p.window : 0;
+            end = min(cached + p.drafts, room);
+        } else {
+            cached = 0;
+            begin = p.window > 0 && end > p.window ? end - p.window : 0;
+        }
         first_tile = begin / kAttnTok;
         tiles = end / kAttnTok + (end % kAttnTok != 0) - first_tile;
+    }
+    __device__ __forceinline__ static bool bad(const AttentionParams &p, int32_t length)
+    {
+        return length < 0 || length > p.room - (TREE ? p.drafts : 0);
     }
 };
 
@@ -168,11 +187,22 @@ __device__ __forceinline__ int64_t divide(int64_t n, int32_t d)
     return int64_t(uint32_t(n) / uint32_t(d));
 }
 
+// Where row `r` of a key head's group lies: TREE: which draft it is of, and which query head
+template <bool TREE> __device__ __forceinline__ int32_t attention_row(const AttentionParams &p, int32_t key_head, int32_t r, int32_t &draft)
+{
+    if constexpr (!TREE) {
+        draft = 0;
+        return key_head * p.group + r;
+    }
+    draft = int32_t(p.sharing.div(uint32_t(r)));
+    return key_head * int32_t(p.sharing.d) + r - draft * int32_t(p.sharing.d);
+}
+
 // A place in the list of tiles: sequence, head block, tile; the same in every lane.
-struct AttentionCursor {
+template <bool TREE> struct AttentionCursor {
     int32_t seq, hb, tile;                   // tile counted from the span's first
     int32_t key_head, block;                 // hb = key_head * blocks + block
-    AttentionSpan span;
+    AttentionSpan<TREE> span;
     __device__ __forceinline__ void next(const AttentionParams &p)
     {
         if (++tile < span.tiles) return;
@@ -187,8 +217,9 @@ struct AttentionCursor {
     }
 };
 
-template <typename T, int DP, int NT> struct AttentionWarp {
+template <typename T, int DP, int NT, bool TREE> struct AttentionWarp {
     typedef AttentionShape<T, DP, NT> Shape;
+    typedef AttentionCursor<TREE> Cursor;
     static constexpr int ROW = Shape::ROW;
     static constexpr bool F32 = sizeof(T) == 4;
     static constexpr int KSTEPS = F32 ? DP / 8 : DP / 16;
@@ -205,6 +236,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
     uint32_t q[NT][KSTEPS][2];               // the queries as N-side operand
     float o[MT][NT][4];                      // O^T: rows head elements, columns query heads
     float m[NT][2], l[NT][2];                // running maximum (of scale * score * log2 e) and this thread's part of the sum
+    int seen_drafts[NT][2];                  // TREE: see drafts_seen()
 
     __device__ __forceinline__ AttentionWarp(const AttentionParams &params, unsigned ring_addr, int lane_)
         : p(params), ring(ring_addr), lane(lane_) {}
@@ -212,7 +244,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
     __device__ __forceinline__ static unsigned swizzled(int row, int chunk) { return unsigned(row * ROW + ((chunk ^ (row & 7)) << 4)); }
 
     // page number and row in the page of token `tile * 16 + lane % 16`; -1 where the token is not visible or has no page
-    __device__ __forceinline__ int32_t look_up(const AttentionCursor &c, int32_t &row) const
+    __device__ __forceinline__ int32_t look_up(const Cursor &c, int32_t &row) const
     {
         const int32_t t = (c.span.first_tile + c.tile) * kAttnTok + (lane & 15);
         if (t < c.span.begin || t >= c.span.end) { row = 0; return -1; }
@@ -296,7 +328,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             }
         }
     }
-    __device__ __forceinline__ void copy_tile(const AttentionCursor &c, int stage, int32_t page, int32_t row, uint32_t mask) const
+    __device__ __forceinline__ void copy_tile(const Cursor &c, int stage, int32_t page, int32_t row, uint32_t mask) const
     {
         const unsigned dst = ring + unsigned(stage) * Shape::STAGE;
         const T *k = static_cast<const T *>(p.k) + c.key_head * p.k_head, *v = static_cast<const T *>(p.v) + c.key_head * p.v_head;
@@ -318,20 +350,50 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         copy_rows(dst + kAttnTok * ROW, v, p.v_page, p.v_slot, p.v_d, p.dim_v, p.vec_v, page, row, mask);
     }
 
-    __device__ __forceinline__ int first_head(const AttentionCursor &c, int &count) const
+    // the item's first row in its key head's group, and how many rows it has
+    __device__ __forceinline__ int first_row(const Cursor &c, int &count) const
     {
         count = min(8 * NT, p.group - c.block * 8 * NT);
-        return c.key_head * p.group + c.block * 8 * NT;
+        return c.block * 8 * NT;
+    }
+    __device__ __forceinline__ static const T *query(const AttentionParams &p, const Cursor &c, int row)
+    {
+        int32_t draft;
+        const int64_t head = attention_row<TREE>(p, c.key_head, row, draft);
+        return static_cast<const T *>(p.q) + c.seq * p.q_n + head * p.q_h + (TREE ? draft * p.q_t : 0);
+    }
+    // TREE: how many drafts the row sees (0: it holds none, and sees nothing)
+    __device__ __forceinline__ int drafts_seen(const Cursor &c, int row) const
+    {
+        int32_t draft;
+        attention_row<TREE>(p, c.key_head, row, draft);
+        const int32_t *m = p.masks + c.seq * p.m_n + draft * p.m_t;
+        int n = 0;
+        for (int w = 0; w < p.words; ++w) {
+            uint32_t x = uint32_t(m[w * p.m_w]);
+            if (p.drafts - 32 * w < 32) x &= (1u << (p.drafts - 32 * w)) - 1u;
+            n += __popc(x);
+        }
+        return n;
+    }
+    // TREE: does the row, which sees `count` drafts, see token t of the sequence?
+    __device__ __forceinline__ bool sees(const Cursor &c, int row, int count, int t) const
+    {
+        const int d = t - c.span.cached;
+        if (d < 0) return p.window == 0 || t >= c.span.cached + count - p.window;
+        int32_t draft;
+        attention_row<TREE>(p, c.key_head, row, draft);
+        return (uint32_t(p.masks[c.seq * p.m_n + draft * p.m_t + (d >> 5) * p.m_w]) >> (d & 31)) & 1u;
     }
 
-    __device__ __forceinline__ void begin_item(const AttentionCursor &c)
+    __device__ __forceinline__ void begin_item(const Cursor &c)
     {
         int count;
-        const int h0 = first_head(c, count);
+        const int h0 = first_row(c, count);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int h = nt * 8 + lane / 4;
-            const T *src = static_cast<const T *>(p.q) + c.seq * p.q_n + int64_t(h0 + (h < count ? h : 0)) * p.q_h;
+            const T *src = query(p, c, h0 + (h < count ? h : 0));
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
@@ -354,7 +416,12 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                     q[nt][ks][half] = x;
                 }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) { m[nt][j] = -INFINITY; l[nt][j] = 0.f; }
+            for (int j = 0; j < 2; ++j) {
+                m[nt][j] = -INFINITY;
+                l[nt][j] = 0.f;
+                const int column = nt * 8 + 2 * (lane & 3) + j;
+                if constexpr (TREE) seen_drafts[nt][j] = column < count ? drafts_seen(c, h0 + column) : 0;
+            }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -364,19 +431,19 @@ template <typename T, int DP, int NT> struct AttentionWarp {
 
     // The scores of a tile by plain fp32 products.  A split infinity is inf + NaN, so a tile with a score that is not
     // a number is computed again here, where infinite keys give infinite scores.
-    __device__ __noinline__ static void plain_scores(const AttentionParams &p, const AttentionCursor &c, int h0, int count,
+    __device__ __noinline__ static void plain_scores(const AttentionParams &p, const Cursor &c, int h0, int count,
                                                      unsigned keys, int lane, float (*s)[4])
     {
         for (int nt = 0; nt < NT; ++nt)
             for (int j = 0; j < 2; ++j) {
                 const int h = nt * 8 + 2 * (lane & 3) + j;
-                const float *src = static_cast<const float *>(p.q) + c.seq * p.q_n + int64_t(h0 + (h < count ? h : 0)) * p.q_h;
+                const T *src = query(p, c, h0 + (h < count ? h : 0));
                 float x = 0.f, y = 0.f;
                 for (int d = 0; d < p.dim_k; ++d) {
                     float k0, k1;
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k0) : "r"(keys + swizzled(lane >> 2, d >> 2) + unsigned(d & 3) * 4u) : "memory");
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k1) : "r"(keys + swizzled((lane >> 2) + 8, d >> 2) + unsigned(d & 3) * 4u) : "memory");
-                    const float qd = src[d * p.q_d];
+                    const float qd = to_f32(src[d * p.q_d]);
                     x = fmaf(k0, qd, x);
                     y = fmaf(k1, qd, y);
                 }
@@ -385,8 +452,66 @@ template <typename T, int DP, int NT> struct AttentionWarp {
             }
     }
 
+    // Does a tile of values hold an infinity or NaN?  (A product with a probability of zero would be NaN: in a tree such a
+    // token may be invisible to this row and visible to the next.)
+    __device__ __forceinline__ bool odd_values(unsigned values) const
+    {
+        bool odd = false;
+#pragma unroll 4
+        for (int i = lane; i < kAttnTok * ROW / 16; i += 32) {
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(values + 16u * unsigned(i)) : "memory");
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (F32) {
+                    odd |= (x[j] & 0x7f800000u) == 0x7f800000u;
+                } else {
+                    constexpr uint32_t e = sizeof(T) == 2 && std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+                    odd |= (x[j] & e) == e || ((x[j] >> 16) & e) == e;
+                }
+            }
+        }
+        return __any_sync(0xffffffffu, odd);
+    }
+    // O += V^T P with plain fp32 products, without the tokens whose probability is zero
+    __device__ __forceinline__ void plain_values(unsigned values, const float (&s)[NT][4])
+    {
+#pragma unroll 1
+        for (int tk = 0; tk < kAttnTok; ++tk) {
+            float pr[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int src = (tk & 7) * 4 + (lane & 3);
+                    const float a = __shfl_sync(0xffffffffu, s[nt][j], src), b = __shfl_sync(0xffffffffu, s[nt][j + 2], src);
+                    pr[nt][j] = tk < 8 ? a : b;
+                }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int d = element(mt, half);
+                    const unsigned at = values + swizzled(tk, d / PER) + unsigned(d % PER) * unsigned(sizeof(T));
+                    float x;
+                    if constexpr (F32) {
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+                    } else {
+                        unsigned short h;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
+                        x = to_f32(*reinterpret_cast<const T *>(&h));
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (pr[nt][j] != 0.f) o[mt][nt][2 * half + j] = fmaf(pr[nt][j], x, o[mt][nt][2 * half + j]);
+                }
+        }
+    }
+
     // one tile; bit r of `seen`: token r counts
-    __device__ __forceinline__ void tile(const AttentionCursor &cur, int stage, uint32_t seen)
+    __device__ __forceinline__ void tile(const Cursor &cur, int stage, uint32_t seen)
     {
         const unsigned ks_base = ring + unsigned(stage) * Shape::STAGE, vs_base = ks_base + kAttnTok * ROW;
         // the products of even and odd steps (fp32: the three kinds of partial products) go to accumulators of their
@@ -444,7 +569,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 for (int j = 0; j < 4; ++j) odd |= s[nt][j] != s[nt][j];
             if (rare(__any_sync(0xffffffffu, odd))) {
                 int count;
-                const int h0 = first_head(cur, count);
+                const int h0 = first_row(cur, count);
                 float again[NT][4];
                 plain_scores(p, cur, h0, count, ks_base, lane, again);
 #pragma unroll
@@ -456,6 +581,11 @@ template <typename T, int DP, int NT> struct AttentionWarp {
         const bool ok0 = (seen >> (lane >> 2)) & 1, ok1 = (seen >> ((lane >> 2) + 8)) & 1;
         float alpha[NT][2];
         bool moved = false;
+        // TREE: tiles of tokens that every draft sees need no look at the masks
+        const int token0 = (cur.span.first_tile + cur.tile) * kAttnTok;
+        const bool masked = TREE && (token0 + kAttnTok > cur.span.cached || (p.window > 0 && token0 < cur.span.cached + p.drafts - p.window));
+        int rows_here = 0, row0 = 0;
+        if constexpr (TREE) row0 = first_row(cur, rows_here);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -463,6 +593,13 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 float &s0 = s[nt][j], &s1 = s[nt][j + 2];
                 s0 = ok0 ? s0 * p.scale_log2 : -INFINITY;
                 s1 = ok1 ? s1 * p.scale_log2 : -INFINITY;
+                if (TREE && masked) {
+                    const int column = nt * 8 + 2 * (lane & 3) + j;
+                    if (column < rows_here && seen_drafts[nt][j] > 0) {
+                        if (ok0 && !sees(cur, row0 + column, seen_drafts[nt][j], token0 + (lane >> 2))) s0 = -INFINITY;
+                        if (ok1 && !sees(cur, row0 + column, seen_drafts[nt][j], token0 + (lane >> 2) + 8)) s1 = -INFINITY;
+                    }
+                }
                 float top = fmaxf(s0, s1);
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
@@ -484,6 +621,10 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[mt][nt][j] *= alpha[nt][j & 1];
+        }
+        if (TREE && masked && rare(odd_values(vs_base))) {
+            plain_values(vs_base, s);
+            return;
         }
         if constexpr (F32) {
             // P (rows tokens, columns heads) -> N-side operand: token lane % 4 (+ 4, + 8, + 12) of head lane / 4
@@ -566,21 +707,25 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                 x += __shfl_xor_sync(0xffffffffu, x, 4);
                 x += __shfl_xor_sync(0xffffffffu, x, 8);
                 x += __shfl_xor_sync(0xffffffffu, x, 16);
+                // a row without a draft: as if every score were -inf
+                if (TREE && seen_drafts[nt][j] == 0) { x = 0.f; m[nt][j] = -INFINITY; }
             }
     }
-    __device__ __forceinline__ void write_out(const AttentionCursor &c) const
+    __device__ __forceinline__ void write_out(const Cursor &c) const
     {
         int count;
-        const int h0 = first_head(c, count);
+        const int h0 = first_row(c, count);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int h = nt * 8 + 2 * (lane & 3) + j;
                 if (h >= count) continue;
+                int32_t draft;
+                const int head = attention_row<TREE>(p, c.key_head, h0 + h, draft);
                 const bool nothing = l[nt][j] == 0.f;          // every score is -inf: zeros, whatever V holds (0 * inf is NaN)
                 const float inv = 1.f / l[nt][j];
-                T *dst = static_cast<T *>(p.o) + c.seq * p.o_n + int64_t(h0 + h) * p.o_h;
+                T *dst = static_cast<T *>(p.o) + c.seq * p.o_n + int64_t(head) * p.o_h + (TREE ? draft * p.o_t : 0);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -589,7 +734,7 @@ template <typename T, int DP, int NT> struct AttentionWarp {
                         if (d < p.dim_v) dst[d * p.o_d] = from_f32<T>(nothing ? 0.f : o[mt][nt][2 * half + j] * inv);
                     }
                 if (p.lse && lane < 4)
-                    p.lse[int64_t(c.seq) * p.heads + h0 + h] = nothing ? -INFINITY
+                    p.lse[(TREE ? int64_t(c.seq) * p.drafts + draft : int64_t(c.seq)) * p.heads + head] = nothing ? -INFINITY
                         : (m[nt][j] + (log2f(l[nt][j]) - AttentionBias<T>::value)) * 0.6931471805599453f;
             }
     }
@@ -622,26 +767,27 @@ __device__ __forceinline__ float join_weight(float m, float top)
 }
 
 // elements d..d+3 of head h of an item (8 NT = `per` heads) from its joined sums
-template <typename T>
+template <typename T, bool TREE>
 __device__ __forceinline__ void write_joined(const AttentionParams &p, int32_t item, int per, int h, int d, const float4 &o, float m, float l)
 {
     const int head_blocks = p.key_heads * p.blocks;
     const int seq = item / head_blocks, hb = item - seq * head_blocks;
     const int kh = hb / p.blocks, in_group = (hb - kh * p.blocks) * per + h;
     if (in_group >= p.group) return;
-    const int head = kh * p.group + in_group;
+    int32_t draft;
+    const int head = attention_row<TREE>(p, kh, in_group, draft);
     const bool nothing = l == 0.f;             // as in write_out
     const float inv = 1.f / l;
-    T *dst = static_cast<T *>(p.o) + seq * p.o_n + int64_t(head) * p.o_h;
+    T *dst = static_cast<T *>(p.o) + seq * p.o_n + int64_t(head) * p.o_h + (TREE ? draft * p.o_t : 0);
     const float v[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (d + j < p.dim_v) dst[(d + j) * p.o_d] = from_f32<T>(nothing ? 0.f : v[j] * inv);
     if (d == 0 && p.lse)
-        p.lse[int64_t(seq) * p.heads + head] = nothing ? -INFINITY : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
+        p.lse[(TREE ? int64_t(seq) * p.drafts + draft : int64_t(seq)) * p.heads + head] = nothing ? -INFINITY : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
 }
 
-template <typename T, int DP, int NT>
+template <typename T, int DP, int NT, bool TREE>
 __global__ void __launch_bounds__(AttentionShape<T, DP, NT>::WARPS * 32, 1)
 paged_attention_kernel(const __grid_constant__ AttentionParams p)
 {
@@ -665,10 +811,10 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
             const int s = tid * per + i;
             if (s >= p.sequences) break;
             const int32_t length = p.lengths[s];
-            AttentionSpan span;
+            AttentionSpan<TREE> span;
             span.set(p, length);
             mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
-            if (rare(length < 0 || length > p.room))
+            if (rare(AttentionSpan<TREE>::bad(p, length)))
                 if (blockIdx.x == 0 && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
         int64_t x = mine;
@@ -693,7 +839,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     int64_t ctas = (total + W - 1) / W;
     if (ctas > gridDim.x) ctas = gridDim.x;
     // Lanes 0, 1 and 2 look up the places where the warp's share begins and ends and where the CTA's ends.
-    AttentionCursor cur;
+    AttentionCursor<TREE> cur;
     int64_t n = 0;                                              // tiles of this warp
     bool closes = false;                                        // its last tile is the CTA's last
     if (blockIdx.x < ctas) {
@@ -704,7 +850,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         const int64_t unit = lane == 1 ? lo + we + (warp < wm ? 1 : 0) : (lane == 2 ? cta_lo + in_cta : lo);
         cur.seq = p.sequences;
         cur.hb = cur.tile = 0;
-        cur.span.begin = cur.span.end = cur.span.first_tile = cur.span.tiles = 0;
+        cur.span.begin = cur.span.end = cur.span.first_tile = cur.span.tiles = cur.span.cached = 0;
         int64_t tiles_before = (scan[THREADS] >> 24) * head_blocks;
         if (unit < total) {
             int a = 0, b = THREADS;                             // units(a) <= unit < units(b)
@@ -739,6 +885,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         cur.span.end = __shfl_sync(0xffffffffu, cur.span.end, 0);
         cur.span.first_tile = __shfl_sync(0xffffffffu, cur.span.first_tile, 0);
         cur.span.tiles = __shfl_sync(0xffffffffu, cur.span.tiles, 0);
+        if constexpr (TREE) cur.span.cached = __shfl_sync(0xffffffffu, cur.span.cached, 0);
         cur.key_head = cur.hb / p.blocks;
         cur.block = cur.hb - cur.key_head * p.blocks;
         // does the CTA's share begin inside an item?  (Then its first unit is a tile, and warp 0 has it.)
@@ -751,8 +898,8 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     __syncthreads();
 
     if (n > 0) {
-        AttentionWarp<T, DP, NT> w(p, ring, lane);
-        AttentionCursor ahead = cur;                            // the tile whose page numbers are in `page`, `row`
+        AttentionWarp<T, DP, NT, TREE> w(p, ring, lane);
+        AttentionCursor<TREE> ahead = cur;                            // the tile whose page numbers are in `page`, `row`
         int64_t issued = 0;
         int32_t row, page = w.look_up(ahead, row);
         // tokens that count: seen[k] belongs to the tile k steps ahead of the one being consumed
@@ -863,7 +1010,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
                         reinterpret_cast<float4 *>(out)[h * (DP / 4) + quad] = o;
                         if (quad == 0) { out[H * DP + h] = this_top; out[H * DP + H + h] = this_sum; }
                     } else {
-                        write_joined<T>(p, this_item, H, h, 4 * quad, o, this_top, this_sum);
+                        write_joined<T, TREE>(p, this_item, H, h, 4 * quad, o, this_top, this_sum);
                     }
                 }
                 begin = last + 1;
@@ -872,15 +1019,17 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
     }
     // sequences with nothing to see
     for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
-        AttentionSpan span;
+        AttentionSpan<TREE> span;
         span.set(p, p.lengths[s]);
         if (rare(span.tiles == 0)) {
+            const int drafts = TREE ? p.drafts : 1;
             for (int e = tid; e < p.heads * p.dim_v; e += THREADS) {
                 const int h = e / p.dim_v, d = e - h * p.dim_v;
-                static_cast<T *>(p.o)[s * p.o_n + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
+                for (int t = 0; t < drafts; ++t)
+                    static_cast<T *>(p.o)[s * p.o_n + (TREE ? t * p.o_t : 0) + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
             }
             if (p.lse)
-                for (int h = tid; h < p.heads; h += THREADS) p.lse[int64_t(s) * p.heads + h] = -INFINITY;
+                for (int h = tid; h < p.heads * drafts; h += THREADS) p.lse[int64_t(s) * p.heads * drafts + h] = -INFINITY;
         }
     }
 }
@@ -910,7 +1059,7 @@ __device__ __forceinline__ float4 load_now(const float4 *p)
 // of the heads, a thread four elements of one; the threads beyond the elements split the parts among them, so
 // that a long sequence alone (148 parts) is a few rounds of loads.
 constexpr int kJoinThreads = 256, kJoinSlices = 4;
-template <typename T, int DP, int NT>
+template <typename T, int DP, int NT, bool TREE>
 __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const __grid_constant__ AttentionParams p, int ctas)
 {
     constexpr int H = 8 * NT, HEADS = H / kJoinSlices, QUADS = HEADS * DP / 4, SPLIT = kJoinThreads / QUADS, AHEAD = 16 / SPLIT;
@@ -1000,7 +1149,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
         const float4 x = sums[j][quad];
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
-    write_joined<T>(p, item, H, h, d, o, tops[k], totals[k]);
+    write_joined<T, TREE>(p, item, H, h, d, o, tops[k], totals[k]);
 }
 
 }  // namespace btc

@@ -127,3 +127,73 @@ def linear4(x, xs, x_group, weights, kind, out):
     # both activations have slopes below 1.13; exponential, division and products: 16 units, of x itself where it is tiny
     y = a * u
     return y, UNIT[out] * y.abs() + 1.13 * dg * (u.abs() + du) + (a.abs() + 1.13 * dg) * du + 16 * E32 * (g * u).abs() + FLOOR[out]
+
+
+# ---- tree attention -----------------------------------------------------------------------------------------
+
+def mask_words(sees):
+    """bool [N, T, T] -> int32 words [N, T, ceil(T / 32)]."""
+    n, t, _ = sees.shape
+    words = -(-t // 32)
+    bits = torch.zeros(n, t, words * 32, dtype=torch.int64)
+    bits[:, :, :t] = sees
+    packed = (bits.view(n, t, words, 32) << torch.arange(32)).sum(-1)
+    return torch.where(packed >= 2 ** 31, packed - 2 ** 32, packed).to(torch.int32)
+
+
+def random_trees(n, t, seed, unused=0):
+    """bool [N, T, T]: every draft continues an earlier one or the last cached token; the last `unused` rows of every second
+    sequence hold none."""
+    g = torch.Generator().manual_seed(seed)
+    sees = torch.zeros(n, t, t, dtype=torch.bool)
+    for i in range(n):
+        for j in range(t - (unused if i % 2 == 0 else 0)):
+            parent = int(torch.randint(-1, j, (1,), generator=g)) if j else -1
+            if parent >= 0:
+                sees[i, j] = sees[i, parent]
+            sees[i, j, j] = True
+    return sees
+
+
+def tree_attention(q, k, v, table, lengths, sees, scale, window):
+    """q [N, T, Hq, D], k / v [P, S, Hk, *] (any device, computed there); returns what decoder_reference.attention returns, with
+    [N, T, Hq] in the place of [N, Hq]."""
+    N, T, Hq, _ = q.shape
+    P, S, Hk, _ = k.shape
+    Dv, dev, room = v.shape[-1], q.device, table.shape[1] * k.shape[1]
+    o = torch.zeros(N, T, Hq, Dv, dtype=torch.float64, device=dev)
+    lse = torch.full((N, T, Hq), -math.inf, dtype=torch.float64, device=dev)
+    size = torch.zeros(N, T, Hq, Dv, dtype=torch.float64, device=dev)
+    moduli, top, count = (torch.zeros(N, T, Hq, dtype=torch.float64, device=dev) for _ in range(3))
+    for n in range(N):
+        cached = max(0, min(int(lengths[n]), room))
+        end = min(cached + T, room)
+        at = torch.arange(end)
+        page = table[n].cpu().long()[at // S]
+        there = (page >= 0) & (page < P)
+        row = sees[n].cpu()
+        drafts = row.sum(-1)
+        visible = torch.zeros(T, end, dtype=torch.bool)
+        visible[:, :cached] = (drafts > 0)[:, None]
+        if window:
+            visible[:, :cached] &= at[None, :cached] >= cached + drafts[:, None] - window
+        visible[:, cached:end] = row[:, :end - cached]
+        visible &= there[None, :]
+        used = visible.any(0)
+        if not used.any():
+            continue
+        at, visible = at[used], visible[:, used].to(dev)
+        pg, rw = page[used].to(dev), (at % S).to(dev)
+        some = visible.any(-1)
+        for h in range(Hq):
+            kk, vv, qq = k[pg, rw, h // (Hq // Hk)].double(), v[pg, rw, h // (Hq // Hk)].double(), q[n, :, h].double()
+            s = (qq @ kk.T * scale).masked_fill(~visible, -math.inf)
+            p = torch.softmax(s, -1)
+            p = torch.where(some[:, None], p, 0.0)
+            o[n, :, h] = p @ vv
+            lse[n, :, h] = torch.logsumexp(s, -1)
+            size[n, :, h] = p @ vv.abs()
+            moduli[n, :, h] = torch.where(visible, qq.abs() @ kk.abs().T, 0.0).amax(-1) * abs(scale)
+            top[n, :, h] = torch.where(visible, s.abs(), 0.0).amax(-1)
+            count[n, :, h] = visible.sum(-1).double()
+    return tuple(t.cpu() for t in (o, lse, size, moduli, top, count))

@@ -122,6 +122,49 @@ def test_linear4_refusals(api, handle):  # noqa: F811
     assert pack(256, 256, 0, 128) == E.ERR_MISALIGNED
 
 
+def test_tree_attention_refusals(api, handle):  # noqa: F811
+    E, B = api, api.BF16
+    t = lambda *s, dt=B, st=None: dense(api, handle, dt, *s, strides=st)  # noqa: E731
+    i = lambda *s: dense(api, handle, api.I32, *s)  # noqa: E731
+    make = lambda *a, **k: code(api, lambda: api.TreeAttention(handle, *a, **k))  # noqa: E731
+    q, k, v, tab, m, o = t(3, 40, 8, 64), t(9, 16, 2, 64), t(9, 16, 2, 32), i(3, 5), i(3, 40, 2), t(3, 40, 8, 32)
+    op = api.TreeAttention(handle, q, k, v, tab, m, o)
+    assert op.workspace_size() > 0
+    assert make(t(3, 40, 8, 64, dt=E.F64), k, v, tab, m, o) == E.ERR_NOT_SUPPORTED
+    assert make(t(3, 40, 8, 64, dt=E.E4M3), k, v, tab, m, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, t(9, 16, 2, 64, dt=E.F16), v, tab, m, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, k, v, tab, t(3, 40, 2), o) == E.ERR_NOT_SUPPORTED
+    assert make(t(3, 8, 64), k, v, tab, m, o) == E.ERR_INVALID_ARGUMENT
+    assert make(q, k, v, tab, i(3, 40), o) == E.ERR_INVALID_ARGUMENT
+    assert make(q, k, v, i(4, 5), m, o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, v, tab, i(3, 40, 1), o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, v, tab, i(3, 39, 2), o) == E.ERR_EXTENT_MISMATCH
+    assert make(t(3, 40, 7, 64), k, v, tab, m, t(3, 40, 7, 32)) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, t(9, 8, 2, 32), tab, m, o) == E.ERR_EXTENT_MISMATCH
+    assert make(q, k, v, tab, m, t(3, 41, 8, 32)) == E.ERR_EXTENT_MISMATCH
+    assert make(t(3, 129, 8, 64), k, v, tab, i(3, 129, 5), t(3, 129, 8, 32)) == E.ERR_NOT_SUPPORTED
+    assert make(t(3, 40, 8, 264), t(9, 16, 2, 264), v, tab, m, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, k, v, tab, m, t(3, 40, 8, 32, st=(1280 * 8, 0, 32, 1))) == E.ERR_D_ALIASING
+    assert make(q, t(9, 16, 2, 64, st=(1 << 62, 128, 64, 1)), v, tab, m, o) == E.ERR_NOT_SUPPORTED
+    assert make(q, k, v, tab, m, o, window=39) == E.ERR_INVALID_ARGUMENT                # shorter than a tree
+    assert make(q, k, v, tab, m, o, window=-1) == E.ERR_INVALID_ARGUMENT
+    assert make(q, k, v, tab, m, o, scale=1e39) == E.ERR_INVALID_ARGUMENT
+    api.TreeAttention(handle, q, k, v, tab, m, o, window=40)
+    run = lambda *a, **k: code(api, lambda: op.execute(0, *a, **k))  # noqa: E731
+    big = dict(workspace=256, workspace_bytes=1 << 40)
+    assert run(0, 256, 256, 256, 256, 256, 256, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(256, 256, 256, 256, 256, 0, 256, **big) == E.ERR_INVALID_ARGUMENT
+    assert run(257, 256, 256, 256, 256, 256, 256, **big) == E.ERR_MISALIGNED
+    assert run(256, 256, 256, 256, 256, 258, 256, **big) == E.ERR_MISALIGNED
+    assert run(256, 256, 256, 256, 256, 256, 256, lse=258, **big) == E.ERR_MISALIGNED
+    assert run(256, 256, 256, 256, 256, 256, 256) == E.ERR_WORKSPACE_TOO_SMALL
+    assert run(256, 256, 256, 256, 256, 256, 256, workspace=256, workspace_bytes=op.workspace_size() - 1) == E.ERR_WORKSPACE_TOO_SMALL
+    assert run(256, 256, 256, 256, 256, 256, 256, workspace=128, workspace_bytes=1 << 40) == E.ERR_MISALIGNED
+    for bad in ([0], [-3], [-1, 1], [-2, 0]):
+        with pytest.raises(ValueError):
+            api.tree_masks(bad)
+
+
 def test_norm_reference_against_differences():
     from layer_reference import norm_backward, norm_forward
     g = torch.Generator().manual_seed(0)

@@ -342,7 +342,8 @@ enum {
     BTC_FLAG_BAD_SLOT = 2,      /* a slot outside the pool (a negative slot only means: skip)        */
     BTC_FLAG_BAD_SEQUENCE = 4,  /* a sequence number outside the table                               */
     BTC_FLAG_BAD_LENGTH = 8,    /* a length or token count that is negative or beyond the table row  */
-    BTC_FLAG_POOL_EXHAUSTED = 16 /* fewer free pages than asked for                                  */
+    BTC_FLAG_POOL_EXHAUSTED = 16, /* fewer free pages than asked for                                 */
+    BTC_FLAG_TIMEOUT = 32       /* a bounded wait inside a kernel ran out: the outputs are incomplete */
 };
 
 /* Head norm and rotary positions of queries and keys, keys and values written into cache pages in the

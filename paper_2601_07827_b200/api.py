@@ -38,6 +38,7 @@ F32, F64, C32, C64 = 0, 1, 2, 3
 F16, BF16, I32, E4M3 = 4, 5, 6, 7          # decoder operators only
 DTYPE_SIZE = {F32: 4, F64: 8, C32: 8, C64: 16, F16: 2, BF16: 2, I32: 4, E4M3: 1}
 FLAG_BAD_PAGE, FLAG_BAD_SLOT, FLAG_BAD_SEQUENCE, FLAG_BAD_LENGTH, FLAG_POOL_EXHAUSTED = 1, 2, 4, 8, 16
+FLAG_TIMEOUT = 32
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2}
 

@@ -7,6 +7,7 @@
 
 #include "decoder_host.h"
 #include "paged_attention_kernel.cuh"
+#include "tree_umma_kernel.cuh"
 
 using namespace btc;
 
@@ -31,9 +32,16 @@ int ctas_of(const btc_tree_attention_s &op) { return op.handle.sm_count; }
 
 int64_t slot_floats(const btc_tree_attention_s &op) { return int64_t(8 * op.nt) * op.dp + 16 * op.nt; }
 
+// May the tcgen05 kernel run, as far as the descriptors say?
+bool umma_fits(const btc_tree_attention_s &op) { return op.q.dtype != BTC_F32 && op.dp <= 128; }
+
+int64_t umma_part_floats(const btc_tree_attention_s &op) { return op.dp == 64 ? TreeShape<64>::PART : TreeShape<128>::PART; }
+
 size_t workspace_bytes_of(const btc_tree_attention_s &op)
 {
     const size_t ctas = size_t(ctas_of(op));
+    if (umma_fits(op))                     // room for either kernel: which one runs depends on the addresses of a call
+        return std::max(ctas * 4 * size_t(umma_part_floats(op)) * sizeof(float), ctas * 2 * size_t(slot_floats(op)) * sizeof(float)) + ctas * 2 * sizeof(int32_t);
     return ctas * 2 * size_t(slot_floats(op)) * sizeof(float) + ctas * 2 * sizeof(int32_t);
 }
 
@@ -72,6 +80,23 @@ template <typename T> btc_error_t launch_typed(const btc_tree_attention_s &op, c
         if (op.dp == 96) return op.nt == 1 ? launch<T, 96, 1>(p, dev, ctas, st) : launch<T, 96, 2>(p, dev, ctas, st);
     if (op.dp == 128) return op.nt == 1 ? launch<T, 128, 1>(p, dev, ctas, st) : launch<T, 128, 2>(p, dev, ctas, st);
     return launch<T, 256, 1>(p, dev, ctas, st);
+}
+
+template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, int device, int ctas, cudaStream_t st)
+{
+    static std::atomic<bool> configured[64] = {};
+    const int slot = device & 63;
+    if (!configured[slot].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(tree_umma_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<DP>::SMEM) != cudaSuccess) {
+            cudaGetLastError();
+            return BTC_ERR_CUDA;
+        }
+        configured[slot].store(true, std::memory_order_relaxed);
+    }
+    const btc_error_t rc = launch_early(tree_umma_kernel<T, DP>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p);
+    if (rc != BTC_SUCCESS) return rc;
+    const int rows = std::min(p.a.group, 2 * kTreeRows);
+    return launch_early(tree_join_kernel<T, DP>, dim3(unsigned(ctas), unsigned((rows + 31) / 32)), kTreeJoinThreads, 0, st, p, ctas);
 }
 
 }  // namespace
@@ -186,6 +211,19 @@ btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_strea
     p.vec_q = es == 2 && p.dim_k % 2 == 0 && rows_allow_vectors(op->q, 2) && aligned_to(Q, 4);
     p.scale_log2 = float(op->scale * kLog2E);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (umma_fits(*op) && p.vec_k && p.vec_v) {
+        TreeParams tp;
+        std::memset(static_cast<void *>(&tp), 0, sizeof tp);
+        p.blocks = (p.group + 2 * kTreeRows - 1) / (2 * kTreeRows);
+        tp.a = p;
+        tp.partial = static_cast<float *>(workspace);
+        tp.partial_item = reinterpret_cast<int32_t *>(tp.partial + ctas * 4 * umma_part_floats(*op));
+        tp.vec_q = rows_allow_vectors(op->q, 8) && aligned_to(Q, 16);
+        tp.vec_o = rows_allow_vectors(op->o, 8) && aligned_to(O, 16);
+        const int dev = op->handle.device;
+        if (op->q.dtype == BTC_F16) return op->dp == 64 ? launch_umma<__half, 64>(tp, dev, int(ctas), st) : launch_umma<__half, 128>(tp, dev, int(ctas), st);
+        return op->dp == 64 ? launch_umma<__nv_bfloat16, 64>(tp, dev, int(ctas), st) : launch_umma<__nv_bfloat16, 128>(tp, dev, int(ctas), st);
+    }
     switch (op->q.dtype) {
     case BTC_F32: return launch_typed<float>(*op, p, st);
     case BTC_F16: return launch_typed<__half>(*op, p, st);

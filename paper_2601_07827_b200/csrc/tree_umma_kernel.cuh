@@ -1,0 +1,720 @@
+// Attention of trees of drafted tokens in 16-bit types on the 5th-generation tensor cores.
+//
+// The rows of a key head (drafts x query heads that share it) are the M side of both products: S = Q K^T and F = P V, 128 rows and
+// 128 tokens at a time, with S, P and F in tensor memory.  One read of the cache serves up to 256 rows.
+//
+// CTA (one per SM, 12 warps):
+//   warps 0-3, 4-7   two groups of 128 threads, a thread to a row: softmax of S (tensor memory -> registers -> P in tensor
+//                    memory, in the place of S), running maximum, sum and output in registers, F added to it in fp32
+//   warps 8-10       copy queries, keys and values into the swizzled layouts that the tensor core reads, with 16-byte cp.async
+//   warp 11          issues the products (one lane)
+// Items of more than 128 rows: group w has rows 128 w .. 128 w + 127 and both groups go over all tiles.  Items of up to 128 rows: both
+// groups have the same rows and take the tiles in turn; what they found is joined at the item's end.  Either way the
+// products for one group run while the other computes.
+//
+// Numbers as in the one-token kernels: P is split in two 16-bit parts (both products), S and F are sums over one tile of 128
+// tokens, and tiles are added in fp32 outside the tensor core (it cuts its sums off towards zero), so F needs no
+// rescaling in tensor memory.
+//
+// Work: the list of (sequence, key head, block of rows) items in tiles is cut into equal contiguous shares, one per CTA, found on the
+// device from the lengths; what a CTA does not hold whole goes to the workspace and a second kernel joins it, in a fixed order.
+// Every wait is bounded; one that gives up ends the kernel and reports BTC_FLAG_TIMEOUT.
+#pragma once
+
+#include "paged_attention_kernel.cuh"
+#include "umma16_common.cuh"
+
+namespace btc {
+
+constexpr int kTreeTok = 128, kTreeRows = 128;
+constexpr int kTreeItemTiles = 1;            // what beginning and ending an item costs, in tiles
+constexpr int kTreeThreads = 384, kTreeLoaders = 96;
+constexpr int kTreeInfos = 8;                // tiles whose visible tokens are kept: more than the ring can be ahead of the softmax
+
+template <int DP> struct TreeShape {
+    static constexpr int PANELS = DP / 64;                       // of 64 elements = 128 bytes, the swizzle's width
+    static constexpr int PANEL = kTreeTok * 128;
+    static constexpr int TILE = PANELS * PANEL;                  // keys, values or queries of 128 tokens or rows
+    static constexpr int SLOTS = DP == 128 ? 5 : 8;
+    static constexpr int SMEM = (2 + SLOTS) * TILE + 1024;       // queries of both groups, ring; slack for alignment
+    static constexpr int64_t PART = int64_t(kTreeRows) * DP + 2 * kTreeRows;      // floats of an unfinished group of rows
+};
+
+struct TreeParams {
+    AttentionParams a;                       // `group`: rows per key head; `blocks`: of 256 rows
+    float *partial;                          // [CTA][2][2 groups][PART]: [element][row], maxima, sums
+    int32_t *partial_item;                   // [CTA][2]
+    int32_t vec_q, vec_o;                    // 16-byte accesses
+};
+
+// visible range of a sequence in tiles of 128 tokens
+struct TreeSpan {
+    int32_t begin, end, cached, first_tile, tiles;
+    __device__ __forceinline__ void set(const AttentionParams &p, int32_t length)
+    {
+        AttentionSpan<true> s;
+        s.set(p, length);
+        begin = s.begin; end = s.end; cached = s.cached;
+        first_tile = begin / kTreeTok;
+        tiles = end > begin ? (end - 1) / kTreeTok + 1 - first_tile : 0;
+    }
+};
+
+// an item and where this CTA's share of it begins; the same in all threads
+struct TreeCursor {
+    int32_t seq, hb, tile, key_head, block;
+    TreeSpan span;
+    __device__ __forceinline__ void next(const AttentionParams &p)
+    {
+        tile = 0;
+        ++hb;
+        if (++block < p.blocks) return;
+        block = 0;
+        if (++key_head < p.key_heads) return;
+        hb = key_head = 0;
+        span.tiles = 0;
+        while (span.tiles == 0 && ++seq < p.sequences) span.set(p, p.lengths[seq]);
+    }
+    __device__ __forceinline__ int rows(const AttentionParams &p) const { return min(2 * kTreeRows, p.group - block * 2 * kTreeRows); }
+};
+
+struct TreeBarriers {
+    uint64_t full[8], empty[8];              // ring of keys and values
+    uint64_t q_full, q_empty;
+    uint64_t s_full[2], p_full[2], f_full[2];
+    uint64_t given, taken;                   // the second group's part of an item, for the first one
+    uint64_t drain;
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Bit i: does a row see token first + i (of 32)?  `low`: the first cached token it sees; drafts by its mask words.
+__device__ __forceinline__ uint32_t tree_visible(int first, int cached, int low, const uint32_t (&mask)[4])
+{
+    // cached tokens low .. cached - 1
+    const int a = max(low - first, 0), b = min(cached - first, 32);
+    uint32_t v = b <= a ? 0u : (b >= 32 ? ~0u : (1u << b) - 1u) & (a >= 32 ? 0u : ~0u << a);
+    const int d = first - cached;            // draft of bit 0
+    if (d > -32 && d < 128) {
+        if (d < 0) {
+            v |= mask[0] << (-d);
+        } else {
+            const int w = d >> 5, s = d & 31;
+            const uint32_t lo = w == 0 ? mask[0] : w == 1 ? mask[1] : w == 2 ? mask[2] : mask[3];
+            const uint32_t hi = w == 0 ? mask[1] : w == 1 ? mask[2] : w == 2 ? mask[3] : 0u;
+            v |= __funnelshift_r(lo, hi, s);
+        }
+    }
+    return v;
+}
+
+// Elements d0 .. d0 + 15 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
+// the tensor core's F NaN in every row, its probability of zero included; in a tree such a draft may be invisible to
+// this row and visible to the next, so tiles with drafts whose F is not finite are computed again here.
+template <typename T>
+__device__ __noinline__ void tree_plain_values(const AttentionParams &p, const TreeCursor &cur, const uint32_t *seen, int token0, int low,
+                                               uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3, int group_row, float base, int d0, float *out)
+{
+    const uint32_t mask[4] = {m0, m1, m2, m3};
+    int32_t draft;
+    const int64_t head = attention_row<true>(p, cur.key_head, group_row, draft);
+    const T *q = static_cast<const T *>(p.q) + cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
+    for (int i = 0; i < 16; ++i) out[i] = 0.f;
+    for (int i = 0; i < kTreeTok; ++i) {
+        const uint32_t vis = tree_visible(token0 + (i & ~31), cur.span.cached, low, mask) & seen[i >> 5];
+        if (!((vis >> (i & 31)) & 1)) continue;
+        const uint32_t t = uint32_t(token0 + i), j = p.page.div(t);
+        const int64_t page = p.table[cur.seq * p.table_n + int64_t(j) * p.table_j], row = t - j * p.page.d;
+        const T *k = static_cast<const T *>(p.k) + cur.key_head * p.k_head + page * p.k_page + row * p.k_slot;
+        const T *v = static_cast<const T *>(p.v) + cur.key_head * p.v_head + page * p.v_page + row * p.v_slot;
+        float s = 0.f;
+        for (int d = 0; d < p.dim_k; ++d) s = fmaf(to_f32(q[d * p.q_d]), to_f32(k[d * p.k_d]), s);
+        const float e = ex2(fmaf(s, p.scale_log2, -base)) * AttentionBias<T>::factor;
+        if (e == 0.f) continue;
+        for (int d = 0; d < 16 && d0 + d < p.dim_v; ++d) out[d] = fmaf(e, to_f32(v[(d0 + d) * p.v_d]), out[d]);
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid_constant__ TreeParams tp)
+{
+    typedef TreeShape<DP> Shape;
+    constexpr int SLOTS = Shape::SLOTS, TILE = Shape::TILE, PANEL = Shape::PANEL, PANELS = Shape::PANELS;
+    const AttentionParams &p = tp.a;
+    extern __shared__ __align__(16) unsigned char raw_smem[];
+    __shared__ __align__(8) TreeBarriers bars;
+    __shared__ uint32_t tmem_base_word;
+    __shared__ int abort_word;
+    __shared__ TreeCursor start;
+    __shared__ int64_t share;
+    __shared__ uint32_t infos[kTreeInfos][4];
+    __shared__ float2 other[kTreeRows];                         // maximum and sum of the second group, for the join of an item's end
+    volatile int *abort_flag = &abort_word;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int64_t *scan = reinterpret_cast<int64_t *>(raw_smem);      // until the shares are known
+    const unsigned smem = (unsigned(__cvta_generic_to_shared(raw_smem)) + 1023u) & ~1023u;
+    const unsigned q_at = smem, ring_at = smem + 2 * TILE;
+    auto bar = [&](const uint64_t &b) { return unsigned(__cvta_generic_to_shared(&b)); };
+    const int head_blocks = p.key_heads * p.blocks;
+    // the same answer in all lanes: what follows are instructions of whole warps
+    auto wait = [&](unsigned b, unsigned phase) -> bool { return __all_sync(0xffffffffu, mbar_wait_bounded(b, phase, abort_flag, nullptr, 0)); };
+
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), kTreeLoaders); mbar_init(bar(bars.empty[i]), 1); }
+        mbar_init(bar(bars.q_full), kTreeLoaders);
+        mbar_init(bar(bars.q_empty), 1);
+        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w]), 128); mbar_init(bar(bars.f_full[w]), 1); }
+        mbar_init(bar(bars.given), 128);
+        mbar_init(bar(bars.taken), 128);
+        mbar_init(bar(bars.drain), 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 11) {
+        tmem_alloc(unsigned(__cvta_generic_to_shared(&tmem_base_word)), 512);
+        tmem_relinquish();
+    }
+    early_begin();
+
+    // ---- this CTA's share ----
+    const int per = (p.sequences + kTreeThreads - 1) / kTreeThreads;
+    {
+        int64_t mine = 0;                                       // tiles * 2^24 + sequences that have any
+        for (int i = 0; i < per; ++i) {
+            const int s = tid * per + i;
+            if (s >= p.sequences) break;
+            const int32_t length = p.lengths[s];
+            TreeSpan span;
+            span.set(p, length);
+            mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
+            if (rare(AttentionSpan<true>::bad(p, length)))
+                if (blockIdx.x == 0 && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+        }
+        int64_t x = mine;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, k);
+            if (lane >= k) x += y;
+        }
+        scan[tid + 1] = x;
+        if (tid == 0) scan[0] = 0;
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        int64_t before = 0;
+        for (int w = 0; w < warp; ++w) before += scan[(w + 1) * 32];
+        __syncthreads();
+        scan[tid + 1] = x + before;
+        __syncthreads();
+    }
+    const unsigned tmem = *reinterpret_cast<volatile uint32_t *>(&tmem_base_word);
+    if (warp == 0) {
+        auto units = [&](int i) { return ((scan[i] >> 24) + (scan[i] & 0xffffff) * kTreeItemTiles) * head_blocks; };
+        const int64_t total = units(kTreeThreads), ctas = min(total, int64_t(gridDim.x));
+        int64_t tiles_before = (scan[kTreeThreads] >> 24) * head_blocks;
+        TreeCursor cur;
+        cur.seq = p.sequences;
+        cur.hb = cur.tile = cur.key_head = cur.block = 0;
+        cur.span.begin = cur.span.end = cur.span.cached = cur.span.first_tile = cur.span.tiles = 0;
+        if (blockIdx.x < ctas) {
+            // lanes 0 and 1 look up where the share begins and ends
+            const int64_t each = total / ctas, more = total - each * ctas;
+            const int64_t lo = each * blockIdx.x + min(int64_t(blockIdx.x), more), hi = lo + each + (int64_t(blockIdx.x) < more ? 1 : 0);
+            const int64_t unit = lane == 1 ? hi : lo;
+            if (unit < total) {
+                int a = 0, b = kTreeThreads;                    // units(a) <= unit < units(b)
+                while (b - a > 1) {
+                    const int c = (a + b) / 2;
+                    if (units(c) <= unit) a = c; else b = c;
+                }
+                int64_t at = unit - units(a);
+                tiles_before = (scan[a] >> 24) * head_blocks;
+                cur.seq = a * per;
+                cur.span.set(p, p.lengths[cur.seq]);
+                while (cur.seq + 1 < p.sequences) {
+                    const int64_t here = cur.span.tiles > 0 ? int64_t(cur.span.tiles + kTreeItemTiles) * head_blocks : 0;
+                    if (at < here) break;
+                    at -= here;
+                    tiles_before += int64_t(cur.span.tiles) * head_blocks;
+                    cur.span.set(p, p.lengths[++cur.seq]);
+                }
+                const int32_t item_units = cur.span.tiles + kTreeItemTiles;
+                cur.hb = int32_t(at / item_units);
+                cur.tile = max(0, int32_t(at - int64_t(cur.hb) * item_units) - kTreeItemTiles);
+                tiles_before += int64_t(cur.hb) * cur.span.tiles + cur.tile;
+                cur.key_head = cur.hb / p.blocks;
+                cur.block = cur.hb - cur.key_head * p.blocks;
+            }
+        }
+        const int64_t to = __shfl_sync(0xffffffffu, tiles_before, 1);
+        if (lane == 0) {
+            start = cur;
+            share = to - tiles_before;
+        }
+    }
+    __syncthreads();
+    int64_t left = share;
+    TreeCursor cur = start;
+
+    // 384 threads x 168 registers at launch hold 128 x 64 and 256 x 216
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
+    if (warp < 11) {
+        // ---- loaders ----
+        constexpr int CHUNKS = DP / 8, STEP = 32 / CHUNKS;       // chunks of a row; rows of a warp's copy
+        const int lw = warp - 8, sub = lane / CHUNKS, chunk = lane % CHUNKS;
+        const int bytes_k = max(0, min(16, (p.dim_k - chunk * 8) * 2)), bytes_v = max(0, min(16, (p.dim_v - chunk * 8) * 2));
+        const unsigned in_row = unsigned((chunk >> 3) * PANEL);
+        int slot = 0, info = 0;
+        unsigned phase = 0, q_phase = 0;
+        bool ok = true, first = true;
+        auto take = [&]() -> bool {                              // the next place of the ring is free
+            return wait(bar(bars.empty[slot]), phase ^ 1u);
+        };
+        // pages of the tokens lane, lane + 32, .. of the item's i-th tile; -1: not visible, or no page
+        auto look_up = [&](int i, int32_t (&page)[4]) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int t = (cur.span.first_tile + cur.tile + i) * kTreeTok + 32 * g + lane;
+                page[g] = -1;
+                if (t >= cur.span.begin && t < cur.span.end) {
+                    const int32_t n = p.table[cur.seq * p.table_n + int64_t(p.page.div(uint32_t(t))) * p.table_j];
+                    page[g] = n;
+                    if (rare(n < 0 || n >= p.pages)) {
+                        if (p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
+                        page[g] = -1;
+                    }
+                }
+            }
+        };
+        while (ok && left > 0) {
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), row0 = cur.block * 2 * kTreeRows;
+            // queries
+            if (!first && !(ok = wait(bar(bars.q_empty), q_phase))) break;
+            if (!first) q_phase ^= 1u;
+            first = false;
+            const int groups = rows > kTreeRows ? 2 : 1;
+#pragma unroll 1
+            for (int i = lw * STEP; i < groups * kTreeRows; i += 3 * STEP) {
+                const int r = i + sub;
+                const T *src = static_cast<const T *>(p.q);
+                const bool there = r < rows;
+                if (there) {
+                    int32_t draft;
+                    const int64_t head = attention_row<true>(p, cur.key_head, row0 + r, draft);
+                    src += cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
+                }
+                const unsigned dst = q_at + unsigned(r >> 7) * TILE + in_row + unsigned(r & 127) * 128u + unsigned(((chunk ^ r) & 7) << 4);
+                if (tp.vec_q) {
+                    const int bytes = there ? bytes_k : 0;
+                    cp_async_part(dst, bytes ? src + chunk * 8 : static_cast<const T *>(p.q), bytes);
+                } else {
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e) {
+                        unsigned short x = 0;
+                        if (there && chunk * 8 + e < p.dim_k) x = *reinterpret_cast<const unsigned short *>(src + (chunk * 8 + e) * p.q_d);
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2u * unsigned(e)), "h"(x) : "memory");
+                    }
+                }
+            }
+            if (tp.vec_q) mbar_arrive_on_copies(bar(bars.q_full)); else mbar_arrive(bar(bars.q_full));
+            // keys and values, tile by tile; the next tile's pages are looked up ahead
+            int32_t page[4];
+            look_up(0, page);
+            for (int i = 0; i < cnt; ++i) {
+                int32_t next_page[4] = {-1, -1, -1, -1};
+                if (i + 1 < cnt) look_up(i + 1, next_page);
+                const int token0 = (cur.span.first_tile + cur.tile + i) * kTreeTok;
+#pragma unroll 1
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (!(ok = take())) break;
+                    if (kv == 0) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const uint32_t seen = __ballot_sync(0xffffffffu, page[g] >= 0);
+                            if (lw == 0 && lane == g) infos[info][g] = seen;
+                        }
+                        if (++info == kTreeInfos) info = 0;
+                    }
+                    const T *base = static_cast<const T *>(kv == 0 ? p.k : p.v) + cur.key_head * (kv == 0 ? p.k_head : p.v_head);
+                    const int64_t s_page = kv == 0 ? p.k_page : p.v_page, s_slot = kv == 0 ? p.k_slot : p.v_slot;
+                    const int bytes = kv == 0 ? bytes_k : bytes_v;
+                    unsigned dst = ring_at + unsigned(slot) * TILE + in_row + unsigned(lw * STEP + sub) * 128u;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int t = token0 + 32 * g + lane, n = page[g];
+                        const int64_t at = n < 0 ? -1 : n * s_page + (t - int32_t(p.page.div(uint32_t(t)) * p.page.d)) * s_slot;
+#pragma unroll 1
+                        for (int j = lw * STEP; j < 32; j += 3 * STEP, dst += 3 * STEP * 128u) {
+                            const int64_t from = __shfl_sync(0xffffffffu, at, j + sub);
+                            const int n16 = __shfl_sync(0xffffffffu, n, j + sub) < 0 ? 0 : bytes;
+                            cp_async_part(dst + unsigned(((chunk ^ (j + sub)) & 7) << 4), n16 ? base + from + chunk * 8 : base, n16);
+                        }
+                        dst = ring_at + unsigned(slot) * TILE + in_row + unsigned(lw * STEP + sub) * 128u + 4096u * unsigned(g + 1);
+                    }
+                    mbar_arrive_on_copies(bar(bars.full[slot]));
+                    if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) page[g] = next_page[g];
+            }
+            left -= cnt;
+            cur.next(p);
+        }
+        cp_async_wait_all();
+    } else {
+        // ---- products ----
+        const unsigned idesc_s = umma16_instr_desc<T>(kTreeTok, false), idesc_f = umma16_instr_desc<T>(DP, true);
+        const unsigned full0 = bar(bars.full[0]), empty0 = bar(bars.empty[0]);
+        int base_slot = 0;                                       // place and round of the item's first keys in the ring
+        unsigned base_phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+        bool ok = true;
+        auto place = [&](int i, unsigned &phase) {               // of the i-th tile copied since base
+            int s = base_slot + i;
+            phase = base_phase ^ (unsigned(s / SLOTS) & 1u);
+            return s % SLOTS;
+        };
+        while (ok && left > 0) {
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), shift = cur.rows(p) > kTreeRows ? 1 : 0;
+            const int64_t steps64 = int64_t(cnt) << shift;
+            const int steps = int(steps64);
+            ok = wait(bar(bars.q_full), q_phase);
+            q_phase ^= 1u;
+            auto scores = [&](int i) -> bool {
+                const int w = i & 1, j = i >> shift;
+                unsigned phase;
+                const int s = place(2 * j, phase);
+                if (!wait(full0 + 8u * s, phase)) return false;
+                tc_fence_after();
+                proxy_fence_async();
+                if (elect_one()) {
+                    const unsigned a = q_at + unsigned(shift ? w : 0) * TILE, b = ring_at + unsigned(s) * TILE;
+#pragma unroll
+                    for (int pn = 0; pn < PANELS; ++pn)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            umma16(tmem + unsigned(w) * 256u, umma_smem_desc(a + pn * PANEL + k * 32, 16, 1024, 2),
+                                   umma_smem_desc(b + pn * PANEL + k * 32, 16, 1024, 2), idesc_s, pn || k ? 1u : 0u);
+                    umma_commit(bar(bars.s_full[w]));
+                    if (!shift || w == 1) umma_commit(empty0 + 8u * s);
+                    if (i + 1 == steps) umma_commit(bar(bars.q_empty));
+                }
+                __syncwarp();
+                return true;
+            };
+            for (int i = 0; ok && i < 2 && i < steps; ++i) ok = scores(i);
+            for (int i = 0; ok && i < steps; ++i) {
+                const int w = i & 1, j = i >> shift;
+                unsigned phase;
+                const int s = place(2 * j + 1, phase);
+                if (!(ok = wait(full0 + 8u * s, phase))) break;
+                if (!(ok = wait(bar(bars.p_full[w]), p_phase[w]))) break;
+                p_phase[w] ^= 1u;
+                tc_fence_after();
+                proxy_fence_async();
+                if (elect_one()) {
+                    const unsigned ps = tmem + unsigned(w) * 256u, f = ps + 128u, b = ring_at + unsigned(s) * TILE;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const uint64_t db = umma_smem_desc(b + k * 2048, PANEL, 1024, 2);
+                        const unsigned pa = ps + 16u * unsigned(k);
+                        umma16_ts(f, pa + 8u, db, idesc_f, k ? 1u : 0u);
+                        umma16_ts(f, pa, db, idesc_f, 1u);
+                    }
+                    umma_commit(bar(bars.f_full[w]));
+                    if (!shift || w == 1) umma_commit(empty0 + 8u * s);
+                }
+                __syncwarp();
+                if (i + 2 < steps) ok = scores(i + 2);
+            }
+            {
+                const int64_t n = int64_t(base_slot) + 2 * int64_t(cnt);
+                base_phase ^= unsigned(n / SLOTS) & 1u;
+                base_slot = int(n % SLOTS);
+            }
+            left -= cnt;
+            cur.next(p);
+        }
+    }
+    } else {
+        // ---- softmax ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;" ::: "memory");
+        const int w = warp >> 2, r = tid & 127;
+        const unsigned lanes = unsigned((warp & 3) * 32) << 16;
+        const unsigned s_at = tmem + unsigned(w) * 256u + lanes, f_at = s_at + 128u;
+        unsigned s_phase = 0, f_phase = 0, join_phase = 0;
+        int info = 0;
+        int32_t parts[2] = {-1, -1};                             // items that the CTA does not hold whole: one that began earlier, one that goes on
+        bool ok = true;
+        while (ok && left > 0) {
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), shift = rows > kTreeRows ? 1 : 0;
+            const int row = shift ? w * kTreeRows + r : r, group_row = cur.block * 2 * kTreeRows + row;
+            const bool mine = row < rows, any = __any_sync(0xffffffffu, mine);
+            uint32_t mask[4] = {0, 0, 0, 0};
+            int32_t draft = 0, head = 0, drafts = 0;
+            if (mine) {
+                head = attention_row<true>(p, cur.key_head, group_row, draft);
+                const int32_t *m = p.masks + cur.seq * p.m_n + draft * p.m_t;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < p.words) {
+                        mask[i] = uint32_t(m[i * p.m_w]);
+                        if (p.drafts - 32 * i < 32) mask[i] &= (1u << (p.drafts - 32 * i)) - 1u;
+                        drafts += __popc(mask[i]);
+                    }
+            }
+            const int low = p.window > 0 ? cur.span.cached + drafts - p.window : 0;
+            float o[DP], m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int d = 0; d < DP; ++d) o[d] = 0.f;
+            for (int j = shift ? 0 : w; j < cnt; j += shift ? 1 : 2) {
+                const int token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
+                if (!(ok = wait(bar(bars.s_full[w]), s_phase))) break;
+                s_phase ^= 1u;
+                tc_fence_after();
+                float alpha = 1.f;
+                if (any) {
+                    const uint32_t *words = infos[(info + j) % kTreeInfos];
+                    const uint32_t seen[4] = {words[0], words[1], words[2], words[3]};
+                    const bool masked = (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
+                                        (p.window > 0 && token0 < cur.span.cached + p.drafts - p.window);
+                    float top = -INFINITY;
+                    const bool negative = p.scale_log2 < 0.f;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t v[16];
+                        tmem_load16(s_at + 16u * c, v);
+                        tmem_load_wait();
+                        const uint32_t vis = !masked ? ~0u : (tree_visible(token0 + 16 * c, cur.span.cached, low, mask) & (seen[c >> 1] >> (16 * (c & 1))));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float x = negative ? -__uint_as_float(v[i]) : __uint_as_float(v[i]);
+                            if ((vis >> i) & 1) top = fmaxf(top, x);
+                        }
+                    }
+                    top = top == -INFINITY ? top : top * fabsf(p.scale_log2);
+                    const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
+                    alpha = m == now ? 1.f : ex2(m - now);
+                    m = now;
+                    float sum[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t v[16], out[16];
+                        tmem_load16(s_at + 16u * c, v);
+                        tmem_load_wait();
+                        const uint32_t vis = !masked ? ~0u : (tree_visible(token0 + 16 * c, cur.span.cached, low, mask) & (seen[c >> 1] >> (16 * (c & 1))));
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float e[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                e[h] = ex2(fmaf(__uint_as_float(v[i + h]), p.scale_log2, -base)) * AttentionBias<T>::factor;
+                                if (!((vis >> (i + h)) & 1)) e[h] = 0.f;
+                            }
+                            sum[0] += e[0];
+                            sum[1] += e[1];
+                            const uint32_t hi = pack2(e[0], e[1], T());
+                            float a, b;
+                            unpack_word(hi, a, b, T());
+                            out[i / 2] = hi;
+                            out[8 + i / 2] = pack2(e[0] - a, e[1] - b, T());
+                        }
+                        tmem_store16u(s_at + 16u * c, out);
+                    }
+                    tmem_store_wait();
+                    l = l * alpha + (sum[0] + sum[1]);
+                }
+                tc_fence_before();
+                mbar_arrive(bar(bars.p_full[w]));
+                if (!(ok = wait(bar(bars.f_full[w]), f_phase))) break;
+                f_phase ^= 1u;
+                tc_fence_after();
+                if (any) {
+#pragma unroll
+                    for (int c = 0; c < DP / 16; ++c) {
+                        uint32_t v[16];
+                        tmem_load16(f_at + 16u * c, v);
+                        tmem_load_wait();
+                        if (token0 + kTreeTok > cur.span.cached) {
+                            bool odd = false;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u;
+                            if (rare(__any_sync(0xffffffffu, odd && mine))) {
+                                float again[16];
+                                tree_plain_values<T>(p, cur, infos[(info + j) % kTreeInfos], token0, low, mask[0], mask[1], mask[2], mask[3],
+                                                     mine ? group_row : cur.block * 2 * kTreeRows, m == -INFINITY ? 0.f : m, 16 * c, again);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(again[i]);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[16 * c + i] = fmaf(o[16 * c + i], alpha, __uint_as_float(v[i]));
+                    }
+                }
+            }
+            if (!ok) break;
+            if (drafts == 0) { m = -INFINITY; l = 0.f; }
+            // both groups have parts of the same rows: the second one's goes through tensor memory
+            if (!shift) {
+                if (w == 1) {
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t v[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(o[32 * c + i]);
+                        tmem_store32u(f_at + 32u * c, v);
+                    }
+                    tmem_store_wait();
+                    other[r] = make_float2(m, l);
+                    tc_fence_before();
+                    mbar_arrive(bar(bars.given));
+                    if (!(ok = wait(bar(bars.taken), join_phase))) break;
+                    tc_fence_after();
+                } else {
+                    if (!(ok = wait(bar(bars.given), join_phase))) break;
+                    tc_fence_after();
+                    const float2 b = other[r];
+                    const float top = fmaxf(m, b.x), wa = join_weight(m, top), wb = join_weight(b.x, top);
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t v[32];
+                        tmem_load32(f_at + 256u + 32u * c, v);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[32 * c + i] = fmaf(o[32 * c + i], wa, __uint_as_float(v[i]) * wb);
+                    }
+                    l = l * wa + b.y * wb;
+                    m = top;
+                    tc_fence_before();
+                    mbar_arrive(bar(bars.taken));
+                }
+                join_phase ^= 1u;
+            }
+            const bool whole = cur.tile == 0 && cnt == cur.span.tiles;
+            if (mine && (shift || w == 0)) {
+                if (whole) {
+                    const bool nothing = l == 0.f;
+                    const float inv = 1.f / l;
+                    T *dst = static_cast<T *>(p.o) + cur.seq * p.o_n + draft * p.o_t + int64_t(head) * p.o_h;
+#pragma unroll
+                    for (int d = 0; d < DP; d += 8) {
+                        if (d >= p.dim_v) break;
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = nothing ? 0.f : o[d + e] * inv;
+                        if (tp.vec_o && d + 8 <= p.dim_v) {
+                            *reinterpret_cast<uint4 *>(dst + d) = pack_vector<T, 8>(x);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (d + e < p.dim_v) dst[(d + e) * p.o_d] = from_f32<T>(x[e]);
+                        }
+                    }
+                    if (p.lse)
+                        p.lse[(int64_t(cur.seq) * p.drafts + draft) * p.heads + head] = nothing ? -INFINITY
+                            : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
+                } else {
+                    float *part = tp.partial + ((2 * int64_t(blockIdx.x) + (cur.tile == 0 ? 1 : 0)) * 2 + (shift ? w : 0)) * Shape::PART;
+#pragma unroll
+                    for (int d = 0; d < DP; ++d) part[d * kTreeRows + r] = o[d];
+                    part[DP * kTreeRows + r] = m;
+                    part[DP * kTreeRows + kTreeRows + r] = l;
+                }
+            }
+            if (!whole) parts[cur.tile == 0 ? 1 : 0] = cur.seq * head_blocks + cur.hb;
+            info = (info + cnt) % kTreeInfos;
+            left -= cnt;
+            cur.next(p);
+        }
+        if (tid == 0) {
+            tp.partial_item[2 * blockIdx.x] = parts[0];
+            tp.partial_item[2 * blockIdx.x + 1] = parts[1];
+        }
+    }
+
+    // sequences with nothing to see
+    for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
+        TreeSpan span;
+        span.set(p, p.lengths[s]);
+        if (rare(span.tiles == 0)) {
+            for (int e = tid; e < p.heads * p.dim_v; e += kTreeThreads) {
+                const int h = e / p.dim_v, d = e - h * p.dim_v;
+                for (int t = 0; t < p.drafts; ++t)
+                    static_cast<T *>(p.o)[s * p.o_n + t * p.o_t + int64_t(h) * p.o_h + d * p.o_d] = from_f32<T>(0.f);
+            }
+            if (p.lse)
+                for (int h = tid; h < p.heads * p.drafts; h += kTreeThreads) p.lse[int64_t(s) * p.heads * p.drafts + h] = -INFINITY;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 11) {
+        if (*abort_flag) {
+            if (elect_one()) umma_commit(bar(bars.drain));
+            __syncwarp();
+            for (unsigned n = 0; n < (1u << 16) && !mbar_try_wait(bar(bars.drain), 0u); ++n) { }
+            if (p.flags && lane == 0) atomicOr(p.flags, int(BTC_FLAG_TIMEOUT));
+        }
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Items that span CTAs, as in the one-token kernels: block (c, y) joins 32 rows of the item that begins in CTA c's range and ends in a
+// later one's; a lane to a row, a warp to DP / 8 elements.
+constexpr int kTreeJoinThreads = 256;
+template <typename T, int DP>
+__global__ void __launch_bounds__(kTreeJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams tp, int ctas)
+{
+    constexpr int EACH = DP / 8;
+    const AttentionParams &p = tp.a;
+    __shared__ int32_t parts;
+    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    early_begin();
+    const int32_t item = load_now(tp.partial_item + 2 * c + 1);
+    if (item < 0) return;
+    const int left = ctas - c;
+    if (tid == 0) parts = left;
+    __syncthreads();
+    for (int i = tid + 1; i < left; i += kTreeJoinThreads)
+        if (tp.partial_item[2 * (c + i)] != item) { atomicMin(&parts, i); break; }
+    __syncthreads();
+    const int n = parts;
+    const int head_blocks = p.key_heads * p.blocks;
+    const int seq = item / head_blocks, hb = item - seq * head_blocks, kh = hb / p.blocks, block = hb - kh * p.blocks;
+    const int row = blockIdx.y * 32 + lane, group_row = block * 2 * kTreeRows + row, rows = min(2 * kTreeRows, p.group - block * 2 * kTreeRows);
+    if (row >= rows) return;
+    const float *first = tp.partial + (4 * int64_t(c) + (row >> 7)) * TreeShape<DP>::PART + (row & 127);
+    auto part = [&](int i) { return first + (i == 0 ? 2 : 4 * int64_t(i)) * TreeShape<DP>::PART; };
+    float top = -INFINITY;
+    for (int i = 0; i < n; ++i) top = fmaxf(top, part(i)[DP * kTreeRows]);
+    float o[EACH], l = 0.f;
+#pragma unroll
+    for (int d = 0; d < EACH; ++d) o[d] = 0.f;
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+        const float *at = part(i);
+        const float share = join_weight(at[DP * kTreeRows], top);
+        l = fmaf(at[DP * kTreeRows + kTreeRows], share, l);
+#pragma unroll
+        for (int d = 0; d < EACH; ++d) o[d] = fmaf(at[(warp * EACH + d) * kTreeRows], share, o[d]);
+    }
+    int32_t draft;
+    const int head = attention_row<true>(p, kh, group_row, draft);
+    const bool nothing = l == 0.f;
+    const float inv = 1.f / l;
+    T *dst = static_cast<T *>(p.o) + seq * p.o_n + draft * p.o_t + int64_t(head) * p.o_h;
+#pragma unroll
+    for (int d = 0; d < EACH; ++d)
+        if (warp * EACH + d < p.dim_v) dst[(warp * EACH + d) * p.o_d] = from_f32<T>(nothing ? 0.f : o[d] * inv);
+    if (warp == 0 && p.lse)
+        p.lse[(int64_t(seq) * p.drafts + draft) * p.heads + head] = nothing ? -INFINITY : (top + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
+}
+
+}  // namespace btc

@@ -32,8 +32,27 @@ int ctas_of(const btc_tree_attention_s &op) { return op.handle.sm_count; }
 
 int64_t slot_floats(const btc_tree_attention_s &op) { return int64_t(8 * op.nt) * op.dp + 16 * op.nt; }
 
-// May the tcgen05 kernel run, as far as the descriptors say?
-bool umma_fits(const btc_tree_attention_s &op) { return op.q.dtype != BTC_F32 && op.dp <= 128; }
+bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
+{
+    const size_t r = t.extent.size();
+    if (t.stride[r - 1] != 1) return false;
+    for (size_t i = 0; i + 1 < r; ++i)
+        if (t.stride[i] % elements != 0) return false;
+    return true;
+}
+
+// May the tcgen05 kernel run, as far as the descriptors say?  It counts places in the cache in 16 bytes and 32 bits: up to 64 GB
+// between the first and the last token of a head.
+bool umma_fits(const btc_tree_attention_s &op)
+{
+    if (op.q.dtype == BTC_F32 || op.dp > 128) return false;
+    for (const TensorDesc *t : {&op.k, &op.v}) {
+        if (!rows_allow_vectors(*t, 8) || t->stride[0] < 0 || t->stride[1] < 0) return false;
+        if (__int128(t->stride[0] / 8) * (t->extent[0] - 1) + __int128(t->stride[1] / 8) * (t->extent[1] - 1) >= int64_t(UINT32_MAX)) return false;
+        if (t->stride[0] / 8 > UINT32_MAX || t->stride[1] / 8 > UINT32_MAX) return false;
+    }
+    return true;
+}
 
 int64_t umma_part_floats(const btc_tree_attention_s &op) { return op.dp == 64 ? TreeShape<64>::PART : TreeShape<128>::PART; }
 
@@ -43,15 +62,6 @@ size_t workspace_bytes_of(const btc_tree_attention_s &op)
     if (umma_fits(op))                     // room for either kernel: which one runs depends on the addresses of a call
         return std::max(ctas * 4 * size_t(umma_part_floats(op)) * sizeof(float), ctas * 2 * size_t(slot_floats(op)) * sizeof(float)) + ctas * 2 * sizeof(int32_t);
     return ctas * 2 * size_t(slot_floats(op)) * sizeof(float) + ctas * 2 * sizeof(int32_t);
-}
-
-bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
-{
-    const size_t r = t.extent.size();
-    if (t.stride[r - 1] != 1) return false;
-    for (size_t i = 0; i + 1 < r; ++i)
-        if (t.stride[i] % elements != 0) return false;
-    return true;
 }
 
 template <typename T, int DP, int NT>
@@ -82,7 +92,67 @@ template <typename T> btc_error_t launch_typed(const btc_tree_attention_s &op, c
     return launch<T, 256, 1>(p, dev, ctas, st);
 }
 
-template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, int device, int ctas, cudaStream_t st)
+// A tensor map of 16-bit elements with boxes of 64 elements (128 bytes, swizzled) x box[1] x ..; false where the tensor has none
+bool encode_map(btc_dtype_t dtype, int rank, const void *base, const int64_t *extent, const int64_t *stride, const int32_t *box, CUtensorMap *out)
+{
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static Encode encode = [] {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            fn = nullptr;
+        }
+        return reinterpret_cast<Encode>(fn);
+    }();
+    if (!encode || !aligned_to(base, 16)) return false;
+    cuuint64_t dim[5], bytes[4];
+    cuuint32_t b[5], steps[5] = {1, 1, 1, 1, 1};
+    for (int d = 0; d < rank; ++d) {
+        if (extent[d] < 1 || extent[d] > INT32_MAX || box[d] < 1 || box[d] > 256) return false;
+        dim[d] = cuuint64_t(extent[d]);
+        b[d] = cuuint32_t(box[d]);
+        if (d == 0) continue;
+        // (where there is one entry its stride is never used)
+        const int64_t s = extent[d] == 1 ? 8 : stride[d];
+        if (s <= 0 || s % 8 != 0 || s >= int64_t(1) << 38) return false;
+        bytes[d - 1] = cuuint64_t(s) * 2;
+    }
+    return encode(out, dtype == BTC_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cuuint32_t(rank), const_cast<void *>(base),
+                  dim, bytes, b, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct TreeMaps {
+    CUtensorMap q, k, v;
+};
+
+// What of a call's tensors bulk copies can fetch: keys and values where pages are whole boxes of 8 rows or more, queries where
+// 128 rows are whole drafts.
+void encode_maps(const btc_tree_attention_s &op, TreeParams &tp, TreeMaps &m)
+{
+    std::memset(static_cast<void *>(&m), 0, sizeof m);
+    const AttentionParams &p = tp.a;
+    int32_t rows = kTreeTok;
+    while (rows >= 8 && int64_t(p.page.d) % rows != 0) rows /= 2;
+    if (rows >= 8) {
+        const int32_t box[4] = {64, rows, 1, 1};
+        const int64_t ek[4] = {p.dim_k, op.k.extent[1], p.key_heads, p.pages}, sk[4] = {1, p.k_slot, p.k_head, p.k_page};
+        const int64_t ev[4] = {p.dim_v, op.v.extent[1], p.key_heads, p.pages}, sv[4] = {1, p.v_slot, p.v_head, p.v_page};
+        if (encode_map(op.q.dtype, 4, p.k, ek, sk, box, &m.k) && encode_map(op.q.dtype, 4, p.v, ev, sv, box, &m.v)) tp.box_kv = rows;
+    }
+    const int32_t sharing = int32_t(p.sharing.d);
+    if (p.q_d == 1 && (p.group <= kTreeRows || (sharing <= kTreeRows && kTreeRows % sharing == 0))) {
+        const int32_t drafts = p.group <= kTreeRows ? p.drafts : kTreeRows / sharing;
+        const int32_t box[5] = {64, sharing, drafts, 1, 1};
+        const int64_t e[5] = {p.dim_k, sharing, p.drafts, p.key_heads, p.sequences}, s[5] = {1, p.q_h, p.q_t, sharing * p.q_h, p.q_n};
+        if (encode_map(op.q.dtype, 5, p.q, e, s, box, &m.q)) tp.box_q = drafts;
+    }
+}
+
+template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, const TreeMaps &maps, int device, int ctas, cudaStream_t st)
 {
     static std::atomic<bool> configured[64] = {};
     const int slot = device & 63;
@@ -93,7 +163,7 @@ template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, int d
         }
         configured[slot].store(true, std::memory_order_relaxed);
     }
-    const btc_error_t rc = launch_early(tree_umma_kernel<T, DP>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p);
+    const btc_error_t rc = launch_early(tree_umma_kernel<T, DP>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p, maps.q, maps.k, maps.v);
     if (rc != BTC_SUCCESS) return rc;
     const int rows = std::min(p.a.group, 2 * kTreeRows);
     return launch_early(tree_join_kernel<T, DP>, dim3(unsigned(ctas), unsigned((rows + 31) / 32)), kTreeJoinThreads, 0, st, p, ctas);
@@ -218,11 +288,15 @@ btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_strea
         tp.a = p;
         tp.partial = static_cast<float *>(workspace);
         tp.partial_item = reinterpret_cast<int32_t *>(tp.partial + ctas * 4 * umma_part_floats(*op));
+        tp.k_page16 = uint32_t(p.k_page / 8); tp.k_slot16 = uint32_t(p.k_slot / 8);
+        tp.v_page16 = uint32_t(p.v_page / 8); tp.v_slot16 = uint32_t(p.v_slot / 8);
         tp.vec_q = rows_allow_vectors(op->q, 8) && aligned_to(Q, 16);
         tp.vec_o = rows_allow_vectors(op->o, 8) && aligned_to(O, 16);
+        TreeMaps maps;
+        encode_maps(*op, tp, maps);
         const int dev = op->handle.device;
-        if (op->q.dtype == BTC_F16) return op->dp == 64 ? launch_umma<__half, 64>(tp, dev, int(ctas), st) : launch_umma<__half, 128>(tp, dev, int(ctas), st);
-        return op->dp == 64 ? launch_umma<__nv_bfloat16, 64>(tp, dev, int(ctas), st) : launch_umma<__nv_bfloat16, 128>(tp, dev, int(ctas), st);
+        if (op->q.dtype == BTC_F16) return op->dp == 64 ? launch_umma<__half, 64>(tp, maps, dev, int(ctas), st) : launch_umma<__half, 128>(tp, maps, dev, int(ctas), st);
+        return op->dp == 64 ? launch_umma<__nv_bfloat16, 64>(tp, maps, dev, int(ctas), st) : launch_umma<__nv_bfloat16, 128>(tp, maps, dev, int(ctas), st);
     }
     switch (op->q.dtype) {
     case BTC_F32: return launch_typed<float>(*op, p, st);

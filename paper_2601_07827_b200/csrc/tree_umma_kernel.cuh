@@ -45,6 +45,9 @@ struct TreeParams {
     float *partial;                          // [CTA][2][2 groups][PART]: [element][row], maxima, sums
     int32_t *partial_item;                   // [CTA][2]
     int32_t vec_q, vec_o;                    // 16-byte accesses
+    // bulk tensor copies: rows of a box of keys and values (they divide the page), drafts of a box of queries; 0: 16-byte copies
+    int32_t box_kv, box_q;
+    uint32_t k_page16, k_slot16, v_page16, v_slot16;       // strides of the cache in 16 bytes
 };
 
 // visible range of a sequence in tiles of 128 tokens
@@ -81,7 +84,7 @@ struct TreeCursor {
 struct TreeBarriers {
     uint64_t full[8], empty[8];              // ring of keys and values
     uint64_t q_full, q_empty;
-    uint64_t s_full[2], p_full[2], f_full[2];
+    uint64_t s_full[2], p_full[2][2], f_full[2];            // P in halves of 64 tokens
     uint64_t given, taken;                   // the second group's part of an item, for the first one
     uint64_t drain;
 };
@@ -113,7 +116,7 @@ __device__ __forceinline__ uint32_t tree_visible(int first, int cached, int low,
     return v;
 }
 
-// Elements d0 .. d0 + 15 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
+// Elements d0 .. d0 + 63 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
 // the tensor core's F NaN in every row, its probability of zero included; in a tree such a draft may be invisible to
 // this row and visible to the next, so tiles with drafts whose F is not finite are computed again here.
 template <typename T>
@@ -124,7 +127,7 @@ __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const T
     int32_t draft;
     const int64_t head = attention_row<true>(p, cur.key_head, group_row, draft);
     const T *q = static_cast<const T *>(p.q) + cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
-    for (int i = 0; i < 16; ++i) out[i] = 0.f;
+    for (int i = 0; i < 64; ++i) out[i] = 0.f;
     for (int i = 0; i < kTreeTok; ++i) {
         const uint32_t vis = tree_visible(token0 + (i & ~31), cur.span.cached, low, mask) & seen[i >> 5];
         if (!((vis >> (i & 31)) & 1)) continue;
@@ -136,12 +139,15 @@ __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const T
         for (int d = 0; d < p.dim_k; ++d) s = fmaf(to_f32(q[d * p.q_d]), to_f32(k[d * p.k_d]), s);
         const float e = ex2(fmaf(s, p.scale_log2, -base)) * AttentionBias<T>::factor;
         if (e == 0.f) continue;
-        for (int d = 0; d < 16 && d0 + d < p.dim_v; ++d) out[d] = fmaf(e, to_f32(v[(d0 + d) * p.v_d]), out[d]);
+        for (int d = 0; d < 64 && d0 + d < p.dim_v; ++d) out[d] = fmaf(e, to_f32(v[(d0 + d) * p.v_d]), out[d]);
     }
 }
 
+__device__ __forceinline__ uint32_t seen_at(const uint32_t (&seen)[4], int i) { return i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3]; }
+
 template <typename T, int DP>
-__global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid_constant__ TreeParams tp)
+__global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid_constant__ TreeParams tp, const __grid_constant__ CUtensorMap map_q,
+                                                                    const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     typedef TreeShape<DP> Shape;
     constexpr int SLOTS = Shape::SLOTS, TILE = Shape::TILE, PANEL = Shape::PANEL, PANELS = Shape::PANELS;
@@ -168,7 +174,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), kTreeLoaders); mbar_init(bar(bars.empty[i]), 1); }
         mbar_init(bar(bars.q_full), kTreeLoaders);
         mbar_init(bar(bars.q_empty), 1);
-        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w]), 128); mbar_init(bar(bars.f_full[w]), 1); }
+        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w][0]), 128); mbar_init(bar(bars.p_full[w][1]), 128); mbar_init(bar(bars.f_full[w]), 1); }
         mbar_init(bar(bars.given), 128);
         mbar_init(bar(bars.taken), 128);
         mbar_init(bar(bars.drain), 1);
@@ -299,30 +305,46 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             if (!first) q_phase ^= 1u;
             first = false;
             const int groups = rows > kTreeRows ? 2 : 1;
-#pragma unroll 1
-            for (int i = lw * STEP; i < groups * kTreeRows; i += 3 * STEP) {
-                const int r = i + sub;
-                const T *src = static_cast<const T *>(p.q);
-                const bool there = r < rows;
-                if (there) {
-                    int32_t draft;
-                    const int64_t head = attention_row<true>(p, cur.key_head, row0 + r, draft);
-                    src += cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
-                }
-                const unsigned dst = q_at + unsigned(r >> 7) * TILE + in_row + unsigned(r & 127) * 128u + unsigned(((chunk ^ r) & 7) << 4);
-                if (tp.vec_q) {
-                    const int bytes = there ? bytes_k : 0;
-                    cp_async_part(dst, bytes ? src + chunk * 8 : static_cast<const T *>(p.q), bytes);
+            if (tp.box_q) {
+                // a box: the heads that share a key head x some drafts, in the order of the rows (zeros behind the last draft)
+                if (lw == 0) {
+                    if (lane == 0) mbar_arrive_expect_tx(bar(bars.q_full), unsigned(groups * PANELS * tp.box_q) * p.sharing.d * 128u);
+                    else mbar_arrive(bar(bars.q_full));
+                    __syncwarp();
+                    if (lane < groups * PANELS) {
+                        const int w = lane / PANELS, pn = lane % PANELS;
+                        tma_load_box(q_at + unsigned(w) * TILE + unsigned(pn) * PANEL, &map_q, bar(bars.q_full), 64 * pn, 0,
+                                     int(p.sharing.div(uint32_t(row0 + w * kTreeRows))), cur.key_head, cur.seq);
+                    }
                 } else {
+                    mbar_arrive(bar(bars.q_full));
+                }
+            } else {
 #pragma unroll 1
-                    for (int e = 0; e < 8; ++e) {
-                        unsigned short x = 0;
-                        if (there && chunk * 8 + e < p.dim_k) x = *reinterpret_cast<const unsigned short *>(src + (chunk * 8 + e) * p.q_d);
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2u * unsigned(e)), "h"(x) : "memory");
+                for (int i = lw * STEP; i < groups * kTreeRows; i += 3 * STEP) {
+                    const int r = i + sub;
+                    const T *src = static_cast<const T *>(p.q);
+                    const bool there = r < rows;
+                    if (there) {
+                        int32_t draft;
+                        const int64_t head = attention_row<true>(p, cur.key_head, row0 + r, draft);
+                        src += cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
+                    }
+                    const unsigned dst = q_at + unsigned(r >> 7) * TILE + in_row + unsigned(r & 127) * 128u + unsigned(((chunk ^ r) & 7) << 4);
+                    if (tp.vec_q) {
+                        const int bytes = there ? bytes_k : 0;
+                        cp_async_part(dst, bytes ? src + chunk * 8 : static_cast<const T *>(p.q), bytes);
+                    } else {
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e) {
+                            unsigned short x = 0;
+                            if (there && chunk * 8 + e < p.dim_k) x = *reinterpret_cast<const unsigned short *>(src + (chunk * 8 + e) * p.q_d);
+                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2u * unsigned(e)), "h"(x) : "memory");
+                        }
                     }
                 }
+                if (tp.vec_q) mbar_arrive_on_copies(bar(bars.q_full)); else mbar_arrive(bar(bars.q_full));
             }
-            if (tp.vec_q) mbar_arrive_on_copies(bar(bars.q_full)); else mbar_arrive(bar(bars.q_full));
             // keys and values, tile by tile; the next tile's pages are looked up ahead
             int32_t page[4];
             look_up(0, page);
@@ -341,21 +363,52 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                         }
                         if (++info == kTreeInfos) info = 0;
                     }
-                    const T *base = static_cast<const T *>(kv == 0 ? p.k : p.v) + cur.key_head * (kv == 0 ? p.k_head : p.v_head);
-                    const int64_t s_page = kv == 0 ? p.k_page : p.v_page, s_slot = kv == 0 ? p.k_slot : p.v_slot;
+                    const unsigned dst = ring_at + unsigned(slot) * TILE;
+                    if (tp.box_kv && token0 >= cur.span.begin && token0 + kTreeTok <= cur.span.end) {
+                        // all tokens are visible: boxes of a page's rows, zeros where the page is none (its number lies outside)
+                        if (lw == 0) {
+                            if (lane == 0) mbar_arrive_expect_tx(bar(bars.full[slot]), TILE);
+                            else mbar_arrive(bar(bars.full[slot]));
+                            __syncwarp();
+                            const int boxes = kTreeTok / tp.box_kv;
+#pragma unroll
+                            for (int i = 0; i < PANELS; ++i) {
+                                const int which = lane + 32 * i, pn = which / boxes, o = (which - pn * boxes) * tp.box_kv;
+                                int32_t n = 0;
+#pragma unroll
+                                for (int g = 0; g < 4; ++g) {
+                                    const int32_t x = __shfl_sync(0xffffffffu, page[g], o & 31);
+                                    if ((o >> 5) == g) n = x;
+                                }
+                                if (pn < PANELS) {
+                                    const int t = token0 + o, row = t - int32_t(p.page.div(uint32_t(t)) * p.page.d);
+                                    tma_load_box4(dst + unsigned(pn) * PANEL + unsigned(o) * 128u, kv == 0 ? &map_k : &map_v, bar(bars.full[slot]), 64 * pn, row,
+                                                  cur.key_head, n);
+                                }
+                            }
+                        } else {
+                            mbar_arrive(bar(bars.full[slot]));
+                        }
+                        if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                        continue;
+                    }
+                    const T *base = static_cast<const T *>(kv == 0 ? p.k : p.v) + cur.key_head * (kv == 0 ? p.k_head : p.v_head) + chunk * 8;
+                    const uint32_t s_page = kv == 0 ? tp.k_page16 : tp.v_page16, s_slot = kv == 0 ? tp.k_slot16 : tp.v_slot16;
                     const int bytes = kv == 0 ? bytes_k : bytes_v;
-                    unsigned dst = ring_at + unsigned(slot) * TILE + in_row + unsigned(lw * STEP + sub) * 128u;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        const int t = token0 + 32 * g + lane, n = page[g];
-                        const int64_t at = n < 0 ? -1 : n * s_page + (t - int32_t(p.page.div(uint32_t(t)) * p.page.d)) * s_slot;
-#pragma unroll 1
-                        for (int j = lw * STEP; j < 32; j += 3 * STEP, dst += 3 * STEP * 128u) {
-                            const int64_t from = __shfl_sync(0xffffffffu, at, j + sub);
-                            const int n16 = __shfl_sync(0xffffffffu, n, j + sub) < 0 ? 0 : bytes;
-                            cp_async_part(dst + unsigned(((chunk ^ (j + sub)) & 7) << 4), n16 ? base + from + chunk * 8 : base, n16);
+                        // in units of 16 bytes, so that 32 bits hold it: one exchange per row
+                        const int t = token0 + 32 * g + lane;
+                        const uint32_t at = page[g] < 0 ? ~0u : uint32_t(page[g]) * s_page + uint32_t(t - int32_t(p.page.div(uint32_t(t)) * p.page.d)) * s_slot;
+#pragma unroll
+                        for (int i = 0; i < (32 + 3 * STEP - 1) / (3 * STEP); ++i) {
+                            const int j = (3 * i + lw) * STEP;
+                            const uint32_t from = __shfl_sync(0xffffffffu, at, (j + sub) & 31);
+                            const int n16 = from == ~0u ? 0 : bytes;
+                            if (j < 32)
+                                cp_async_part(dst + in_row + unsigned(32 * g + j + sub) * 128u + unsigned(((chunk ^ (j + sub)) & 7) << 4),
+                                              base + (n16 ? int64_t(from) * 8 : -chunk * 8), n16);
                         }
-                        dst = ring_at + unsigned(slot) * TILE + in_row + unsigned(lw * STEP + sub) * 128u + 4096u * unsigned(g + 1);
                     }
                     mbar_arrive_on_copies(bar(bars.full[slot]));
                     if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
@@ -414,23 +467,30 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 unsigned phase;
                 const int s = place(2 * j + 1, phase);
                 if (!(ok = wait(full0 + 8u * s, phase))) break;
-                if (!(ok = wait(bar(bars.p_full[w]), p_phase[w]))) break;
-                p_phase[w] ^= 1u;
-                tc_fence_after();
-                proxy_fence_async();
-                if (elect_one()) {
-                    const unsigned ps = tmem + unsigned(w) * 256u, f = ps + 128u, b = ring_at + unsigned(s) * TILE;
+                // the first half's products run while the second half is still being made
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const uint64_t db = umma_smem_desc(b + k * 2048, PANEL, 1024, 2);
-                        const unsigned pa = ps + 16u * unsigned(k);
-                        umma16_ts(f, pa + 8u, db, idesc_f, k ? 1u : 0u);
-                        umma16_ts(f, pa, db, idesc_f, 1u);
+                for (int half = 0; half < 2; ++half) {
+                    if (!(ok = wait(bar(bars.p_full[w][half]), p_phase[w]))) break;
+                    tc_fence_after();
+                    proxy_fence_async();
+                    if (elect_one()) {
+                        const unsigned ps = tmem + unsigned(w) * 256u, f = ps + 128u, b = ring_at + unsigned(s) * TILE;
+#pragma unroll
+                        for (int k = 4 * half; k < 4 * half + 4; ++k) {
+                            const uint64_t db = umma_smem_desc(b + k * 2048, PANEL, 1024, 2);
+                            const unsigned pa = ps + 16u * unsigned(k);
+                            umma16_ts(f, pa + 8u, db, idesc_f, k ? 1u : 0u);
+                            umma16_ts(f, pa, db, idesc_f, 1u);
+                        }
+                        if (half == 1) {
+                            umma_commit(bar(bars.f_full[w]));
+                            if (!shift || w == 1) umma_commit(empty0 + 8u * s);
+                        }
                     }
-                    umma_commit(bar(bars.f_full[w]));
-                    if (!shift || w == 1) umma_commit(empty0 + 8u * s);
+                    __syncwarp();
                 }
-                __syncwarp();
+                if (!ok) break;
+                p_phase[w] ^= 1u;
                 if (i + 2 < steps) ok = scores(i + 2);
             }
             {
@@ -479,43 +539,50 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 s_phase ^= 1u;
                 tc_fence_after();
                 float alpha = 1.f;
+                auto first_half = [&]() {
+                    tmem_store_wait();
+                    tc_fence_before();
+                    mbar_arrive(bar(bars.p_full[w][0]));
+                };
+                if (!any) first_half();
                 if (any) {
                     const uint32_t *words = infos[(info + j) % kTreeInfos];
                     const uint32_t seen[4] = {words[0], words[1], words[2], words[3]};
                     const bool masked = (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
                                         (p.window > 0 && token0 < cur.span.cached + p.drafts - p.window);
+                    // what is visible of tokens first .. first + 31 of the tile
+                    auto visible = [&](int first) { return tree_visible(token0 + first, cur.span.cached, low, mask) & seen_at(seen, first >> 5); };
                     float top = -INFINITY;
-                    const bool negative = p.scale_log2 < 0.f;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t v[16];
-                        tmem_load16(s_at + 16u * c, v);
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t v[64];
+                        tmem_load64(s_at + 64u * c, v);
+                        uint32_t vis[2] = {~0u, ~0u};
+                        if (masked) { vis[0] = visible(64 * c); vis[1] = visible(64 * c + 32); }
                         tmem_load_wait();
-                        const uint32_t vis = !masked ? ~0u : (tree_visible(token0 + 16 * c, cur.span.cached, low, mask) & (seen[c >> 1] >> (16 * (c & 1))));
+                        if (!masked) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float x = negative ? -__uint_as_float(v[i]) : __uint_as_float(v[i]);
-                            if ((vis >> i) & 1) top = fmaxf(top, x);
+                            for (int i = 0; i < 64; i += 2) top = fmaxf(top, fmaxf(__uint_as_float(v[i]) * p.scale_log2, __uint_as_float(v[i + 1]) * p.scale_log2));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) top = (vis[i >> 5] >> (i & 31)) & 1 ? fmaxf(top, __uint_as_float(v[i]) * p.scale_log2) : top;
                         }
                     }
-                    top = top == -INFINITY ? top : top * fabsf(p.scale_log2);
                     const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
                     alpha = m == now ? 1.f : ex2(m - now);
                     m = now;
                     float sum[2] = {0.f, 0.f};
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint32_t v[16], out[16];
-                        tmem_load16(s_at + 16u * c, v);
-                        tmem_load_wait();
-                        const uint32_t vis = !masked ? ~0u : (tree_visible(token0 + 16 * c, cur.span.cached, low, mask) & (seen[c >> 1] >> (16 * (c & 1))));
+                    // 16 tokens: S -> P in two parts, in the place of S; the next 16 are on their way meanwhile
+                    auto probabilities = [&](const uint32_t (&v)[16], int c, uint32_t vis) {
+                        uint32_t out[16];
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
                             float e[2];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                e[h] = ex2(fmaf(__uint_as_float(v[i + h]), p.scale_log2, -base)) * AttentionBias<T>::factor;
-                                if (!((vis >> (i + h)) & 1)) e[h] = 0.f;
+                                e[h] = ex2(fmaf(__uint_as_float(v[i + h]), p.scale_log2, -base));
+                                if (AttentionBias<T>::factor != 1.f) e[h] *= AttentionBias<T>::factor;
+                                if (masked) e[h] = (vis >> (i + h)) & 1 ? e[h] : 0.f;
                             }
                             sum[0] += e[0];
                             sum[1] += e[1];
@@ -526,35 +593,61 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                             out[8 + i / 2] = pack2(e[0] - a, e[1] - b, T());
                         }
                         tmem_store16u(s_at + 16u * c, out);
+                    };
+                    uint32_t va[16], vb[16];
+                    tmem_load16(s_at, va);
+                    tmem_load_wait();
+                    if (!masked) {
+#pragma unroll 1
+                        for (int c = 0; c < 8; c += 2) {
+                            tmem_load16(s_at + 16u * (c + 1), vb);
+                            probabilities(va, c, ~0u);
+                            tmem_load_wait();
+                            if (c < 6) tmem_load16(s_at + 16u * (c + 2), va);
+                            probabilities(vb, c + 1, ~0u);
+                            tmem_load_wait();
+                            if (c == 2) first_half();
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            const uint32_t vis = visible(16 * c & ~31) >> (16 * (c & 1));
+                            if (c > 0) {
+                                tmem_load16(s_at + 16u * c, va);
+                                tmem_load_wait();
+                            }
+                            probabilities(va, c, vis);
+                            if (c == 3) first_half();
+                        }
                     }
                     tmem_store_wait();
                     l = l * alpha + (sum[0] + sum[1]);
                 }
                 tc_fence_before();
-                mbar_arrive(bar(bars.p_full[w]));
+                mbar_arrive(bar(bars.p_full[w][1]));
                 if (!(ok = wait(bar(bars.f_full[w]), f_phase))) break;
                 f_phase ^= 1u;
                 tc_fence_after();
                 if (any) {
 #pragma unroll
-                    for (int c = 0; c < DP / 16; ++c) {
-                        uint32_t v[16];
-                        tmem_load16(f_at + 16u * c, v);
+                    for (int c = 0; c < DP / 64; ++c) {
+                        uint32_t v[64];
+                        tmem_load64(f_at + 64u * c, v);
                         tmem_load_wait();
                         if (token0 + kTreeTok > cur.span.cached) {
                             bool odd = false;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u;
+                            for (int i = 0; i < 64; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u;
                             if (rare(__any_sync(0xffffffffu, odd && mine))) {
-                                float again[16];
+                                float again[64];
                                 tree_plain_values<T>(p, cur, infos[(info + j) % kTreeInfos], token0, low, mask[0], mask[1], mask[2], mask[3],
-                                                     mine ? group_row : cur.block * 2 * kTreeRows, m == -INFINITY ? 0.f : m, 16 * c, again);
+                                                     mine ? group_row : cur.block * 2 * kTreeRows, m == -INFINITY ? 0.f : m, 64 * c, again);
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(again[i]);
+                                for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(again[i]);
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[16 * c + i] = fmaf(o[16 * c + i], alpha, __uint_as_float(v[i]));
+                        for (int i = 0; i < 64; ++i) o[64 * c + i] = fmaf(o[64 * c + i], alpha, __uint_as_float(v[i]));
                     }
                 }
             }

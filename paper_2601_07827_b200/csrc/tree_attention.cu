@@ -166,7 +166,7 @@ template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, const
     const btc_error_t rc = launch_early(tree_umma_kernel<T, DP>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p, maps.q, maps.k, maps.v);
     if (rc != BTC_SUCCESS) return rc;
     const int rows = std::min(p.a.group, 2 * kTreeRows);
-    return launch_early(tree_join_kernel<T, DP>, dim3(unsigned(ctas), unsigned((rows + 31) / 32)), kTreeJoinThreads, 0, st, p, ctas);
+    return launch_early(tree_join_kernel<T, DP>, dim3(unsigned(ctas), unsigned((rows + kTreeJoinRows - 1) / kTreeJoinRows)), kTreeJoinThreads, 0, st, p, ctas);
 }
 
 }  // namespace

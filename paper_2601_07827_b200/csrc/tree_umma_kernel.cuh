@@ -4,13 +4,14 @@
 // 128 tokens at a time, with S, P and F in tensor memory.  One read of the cache serves up to 256 rows.
 //
 // CTA (one per SM, 12 warps):
-//   warps 0-3, 4-7   two groups of 128 threads, a thread to a row: softmax of S (tensor memory -> registers -> P in tensor
-//                    memory, in the place of S), running maximum, sum and output in registers, F added to it in fp32
-//   warps 8-10       copy queries, keys and values into the swizzled layouts that the tensor core reads, with 16-byte cp.async
-//   warp 11          issues the products (one lane)
-// Items of more than 128 rows: group w has rows 128 w .. 128 w + 127 and both groups go over all tiles.  Items of up to 128 rows: both
-// groups have the same rows and take the tiles in turn; what they found is joined at the item's end.  Either way the
-// products for one group run while the other computes.
+//   warps 0-7     softmax of S (tensor memory -> registers -> P in tensor memory, in the place of S), running maximum, sum and output in
+//                 registers, F added to it in fp32.  Warps w and w + 4 share 32 rows: one takes the first 64 tokens of a tile and the
+//                 first half of the head, the other the second; they exchange the maxima through shared memory.
+//   warps 8-10    bring queries, keys and values into the swizzled layouts that the tensor core reads: bulk tensor copies where pages are
+//                 whole boxes, 16-byte cp.async elsewhere (tiles with tokens that are not visible)
+//   warp 11       issues the products (one lane)
+// A step is a tile of tokens for 128 rows; items of more than 128 rows take two steps a tile.  Two sets of S and F alternate: the products
+// of one step run while the softmax of the next is computed, and F is added a step later.
 //
 // Numbers as in the one-token kernels: P is split in two 16-bit parts (both products), S and F are sums over one tile of 128
 // tokens, and tiles are added in fp32 outside the tensor core (it cuts its sums off towards zero), so F needs no
@@ -36,7 +37,7 @@ template <int DP> struct TreeShape {
     static constexpr int PANEL = kTreeTok * 128;
     static constexpr int TILE = PANELS * PANEL;                  // keys, values or queries of 128 tokens or rows
     static constexpr int SLOTS = DP == 128 ? 5 : 8;
-    static constexpr int SMEM = (2 + SLOTS) * TILE + 1024;       // queries of both groups, ring; slack for alignment
+    static constexpr int SMEM = (2 + SLOTS) * TILE;              // queries of up to 256 rows, ring
     static constexpr int64_t PART = int64_t(kTreeRows) * DP + 2 * kTreeRows;      // floats of an unfinished group of rows
 };
 
@@ -84,8 +85,8 @@ struct TreeCursor {
 struct TreeBarriers {
     uint64_t full[8], empty[8];              // ring of keys and values
     uint64_t q_full, q_empty;
-    uint64_t s_full[2], p_full[2][2], f_full[2];            // P in halves of 64 tokens
-    uint64_t given, taken;                   // the second group's part of an item, for the first one
+    uint64_t s_full[2], p_full[2], f_full[2];
+    uint64_t pair[4];                        // the two warps that share rows
     uint64_t drain;
 };
 
@@ -116,10 +117,10 @@ __device__ __forceinline__ uint32_t tree_visible(int first, int cached, int low,
     return v;
 }
 
-// Elements d0 .. d0 + 63 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
+// Elements d0 .. d0 + COUNT - 1 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
 // the tensor core's F NaN in every row, its probability of zero included; in a tree such a draft may be invisible to
 // this row and visible to the next, so tiles with drafts whose F is not finite are computed again here.
-template <typename T>
+template <typename T, int COUNT>
 __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const TreeCursor &cur, const uint32_t *seen, int token0, int low,
                                                uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3, int group_row, float base, int d0, float *out)
 {
@@ -127,7 +128,7 @@ __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const T
     int32_t draft;
     const int64_t head = attention_row<true>(p, cur.key_head, group_row, draft);
     const T *q = static_cast<const T *>(p.q) + cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
-    for (int i = 0; i < 64; ++i) out[i] = 0.f;
+    for (int i = 0; i < COUNT; ++i) out[i] = 0.f;
     for (int i = 0; i < kTreeTok; ++i) {
         const uint32_t vis = tree_visible(token0 + (i & ~31), cur.span.cached, low, mask) & seen[i >> 5];
         if (!((vis >> (i & 31)) & 1)) continue;
@@ -139,11 +140,30 @@ __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const T
         for (int d = 0; d < p.dim_k; ++d) s = fmaf(to_f32(q[d * p.q_d]), to_f32(k[d * p.k_d]), s);
         const float e = ex2(fmaf(s, p.scale_log2, -base)) * AttentionBias<T>::factor;
         if (e == 0.f) continue;
-        for (int d = 0; d < 64 && d0 + d < p.dim_v; ++d) out[d] = fmaf(e, to_f32(v[(d0 + d) * p.v_d]), out[d]);
+        for (int d = 0; d < COUNT && d0 + d < p.dim_v; ++d) out[d] = fmaf(e, to_f32(v[(d0 + d) * p.v_d]), out[d]);
     }
 }
 
-__device__ __forceinline__ uint32_t seen_at(const uint32_t (&seen)[4], int i) { return i == 0 ? seen[0] : i == 1 ? seen[1] : i == 2 ? seen[2] : seen[3]; }
+// elements d0 .. d0 + N - 1 of an output row
+template <typename T, int N>
+__device__ __forceinline__ void tree_write(T *dst, int d0, int dim, int64_t stride, bool vec, const float (&o)[N], float scale, bool nothing)
+{
+    static_assert(N % 8 == 0, "");
+#pragma unroll
+    for (int d = 0; d < N; d += 8) {
+        if (d0 + d >= dim) break;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = nothing ? 0.f : o[d + e] * scale;
+        if (vec && d0 + d + 8 <= dim) {
+            *reinterpret_cast<uint4 *>(dst + d0 + d) = pack_vector<T, 8>(x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (d0 + d + e < dim) dst[(d0 + d + e) * stride] = from_f32<T>(x[e]);
+        }
+    }
+}
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid_constant__ TreeParams tp, const __grid_constant__ CUtensorMap map_q,
@@ -152,18 +172,18 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     typedef TreeShape<DP> Shape;
     constexpr int SLOTS = Shape::SLOTS, TILE = Shape::TILE, PANEL = Shape::PANEL, PANELS = Shape::PANELS;
     const AttentionParams &p = tp.a;
-    extern __shared__ __align__(16) unsigned char raw_smem[];
+    extern __shared__ __align__(1024) unsigned char raw_smem[];   // (what is static beside it is less than 3 KB)
     __shared__ __align__(8) TreeBarriers bars;
     __shared__ uint32_t tmem_base_word;
     __shared__ int abort_word;
     __shared__ TreeCursor start;
     __shared__ int64_t share;
     __shared__ uint32_t infos[kTreeInfos][4];
-    __shared__ float2 other[kTreeRows];                         // maximum and sum of the second group, for the join of an item's end
+    __shared__ float tops[2][2][kTreeRows];                     // [step's parity][half][row]
     volatile int *abort_flag = &abort_word;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t *scan = reinterpret_cast<int64_t *>(raw_smem);      // until the shares are known
-    const unsigned smem = (unsigned(__cvta_generic_to_shared(raw_smem)) + 1023u) & ~1023u;
+    const unsigned smem = unsigned(__cvta_generic_to_shared(raw_smem));
     const unsigned q_at = smem, ring_at = smem + 2 * TILE;
     auto bar = [&](const uint64_t &b) { return unsigned(__cvta_generic_to_shared(&b)); };
     const int head_blocks = p.key_heads * p.blocks;
@@ -174,9 +194,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), kTreeLoaders); mbar_init(bar(bars.empty[i]), 1); }
         mbar_init(bar(bars.q_full), kTreeLoaders);
         mbar_init(bar(bars.q_empty), 1);
-        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w][0]), 128); mbar_init(bar(bars.p_full[w][1]), 128); mbar_init(bar(bars.f_full[w]), 1); }
-        mbar_init(bar(bars.given), 128);
-        mbar_init(bar(bars.taken), 128);
+        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w]), 256); mbar_init(bar(bars.f_full[w]), 1); }
+        for (int i = 0; i < 4; ++i) mbar_init(bar(bars.pair[i]), 64);
         mbar_init(bar(bars.drain), 1);
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -427,6 +446,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         const unsigned full0 = bar(bars.full[0]), empty0 = bar(bars.empty[0]);
         int base_slot = 0;                                       // place and round of the item's first keys in the ring
         unsigned base_phase = 0, q_phase = 0, p_phase[2] = {0, 0};
+        int parity = 0;                                          // of the item's first step
         bool ok = true;
         auto place = [&](int i, unsigned &phase) {               // of the i-th tile copied since base
             int s = base_slot + i;
@@ -434,28 +454,26 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             return s % SLOTS;
         };
         while (ok && left > 0) {
-            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), shift = cur.rows(p) > kTreeRows ? 1 : 0;
-            const int64_t steps64 = int64_t(cnt) << shift;
-            const int steps = int(steps64);
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), shift = cur.rows(p) > kTreeRows ? 1 : 0, steps = cnt << shift;
             ok = wait(bar(bars.q_full), q_phase);
             q_phase ^= 1u;
             auto scores = [&](int i) -> bool {
-                const int w = i & 1, j = i >> shift;
+                const int w = shift ? i & 1 : 0, b = (parity + i) & 1;
                 unsigned phase;
-                const int s = place(2 * j, phase);
+                const int s = place(2 * (i >> shift), phase);
                 if (!wait(full0 + 8u * s, phase)) return false;
                 tc_fence_after();
                 proxy_fence_async();
                 if (elect_one()) {
-                    const unsigned a = q_at + unsigned(shift ? w : 0) * TILE, b = ring_at + unsigned(s) * TILE;
+                    const unsigned qs = q_at + unsigned(w) * TILE, ks = ring_at + unsigned(s) * TILE;
 #pragma unroll
                     for (int pn = 0; pn < PANELS; ++pn)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            umma16(tmem + unsigned(w) * 256u, umma_smem_desc(a + pn * PANEL + k * 32, 16, 1024, 2),
-                                   umma_smem_desc(b + pn * PANEL + k * 32, 16, 1024, 2), idesc_s, pn || k ? 1u : 0u);
-                    umma_commit(bar(bars.s_full[w]));
-                    if (!shift || w == 1) umma_commit(empty0 + 8u * s);
+                            umma16(tmem + unsigned(b) * 256u, umma_smem_desc(qs + pn * PANEL + k * 32, 16, 1024, 2),
+                                   umma_smem_desc(ks + pn * PANEL + k * 32, 16, 1024, 2), idesc_s, pn || k ? 1u : 0u);
+                    umma_commit(bar(bars.s_full[b]));
+                    if (w == shift) umma_commit(empty0 + 8u * s);
                     if (i + 1 == steps) umma_commit(bar(bars.q_empty));
                 }
                 __syncwarp();
@@ -463,36 +481,30 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             };
             for (int i = 0; ok && i < 2 && i < steps; ++i) ok = scores(i);
             for (int i = 0; ok && i < steps; ++i) {
-                const int w = i & 1, j = i >> shift;
+                const int w = shift ? i & 1 : 0, b = (parity + i) & 1;
                 unsigned phase;
-                const int s = place(2 * j + 1, phase);
+                const int s = place(2 * (i >> shift) + 1, phase);
                 if (!(ok = wait(full0 + 8u * s, phase))) break;
-                // the first half's products run while the second half is still being made
+                if (!(ok = wait(bar(bars.p_full[b]), p_phase[b]))) break;
+                p_phase[b] ^= 1u;
+                tc_fence_after();
+                proxy_fence_async();
+                if (elect_one()) {
+                    const unsigned ps = tmem + unsigned(b) * 256u, f = ps + 128u, vs = ring_at + unsigned(s) * TILE;
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (!(ok = wait(bar(bars.p_full[w][half]), p_phase[w]))) break;
-                    tc_fence_after();
-                    proxy_fence_async();
-                    if (elect_one()) {
-                        const unsigned ps = tmem + unsigned(w) * 256u, f = ps + 128u, b = ring_at + unsigned(s) * TILE;
-#pragma unroll
-                        for (int k = 4 * half; k < 4 * half + 4; ++k) {
-                            const uint64_t db = umma_smem_desc(b + k * 2048, PANEL, 1024, 2);
-                            const unsigned pa = ps + 16u * unsigned(k);
-                            umma16_ts(f, pa + 8u, db, idesc_f, k ? 1u : 0u);
-                            umma16_ts(f, pa, db, idesc_f, 1u);
-                        }
-                        if (half == 1) {
-                            umma_commit(bar(bars.f_full[w]));
-                            if (!shift || w == 1) umma_commit(empty0 + 8u * s);
-                        }
+                    for (int k = 0; k < 8; ++k) {
+                        const uint64_t db = umma_smem_desc(vs + k * 2048, PANEL, 1024, 2);
+                        const unsigned pa = ps + 16u * unsigned(k);
+                        umma16_ts(f, pa + 8u, db, idesc_f, k ? 1u : 0u);
+                        umma16_ts(f, pa, db, idesc_f, 1u);
                     }
-                    __syncwarp();
+                    umma_commit(bar(bars.f_full[b]));
+                    if (w == shift) umma_commit(empty0 + 8u * s);
                 }
-                if (!ok) break;
-                p_phase[w] ^= 1u;
+                __syncwarp();
                 if (i + 2 < steps) ok = scores(i + 2);
             }
+            parity = (parity + steps) & 1;
             {
                 const int64_t n = int64_t(base_slot) + 2 * int64_t(cnt);
                 base_phase ^= unsigned(n / SLOTS) & 1u;
@@ -505,92 +517,132 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     } else {
         // ---- softmax ----
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;" ::: "memory");
-        const int w = warp >> 2, r = tid & 127;
-        const unsigned lanes = unsigned((warp & 3) * 32) << 16;
-        const unsigned s_at = tmem + unsigned(w) * 256u + lanes, f_at = s_at + 128u;
-        unsigned s_phase = 0, f_phase = 0, join_phase = 0;
-        int info = 0;
+        constexpr int HALF = DP / 2;                             // elements of the head that a thread keeps
+        const int half = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const unsigned lanes = unsigned(quarter * 32) << 16;
+        unsigned s_phase[2] = {0, 0}, f_phase[2] = {0, 0}, pair_phase = 0;
+        int info = 0, parity = 0;
         int32_t parts[2] = {-1, -1};                             // items that the CTA does not hold whole: one that began earlier, one that goes on
         bool ok = true;
+        auto pair_wait = [&]() -> bool {
+            mbar_arrive(bar(bars.pair[quarter]));
+            const bool good = wait(bar(bars.pair[quarter]), pair_phase);
+            pair_phase ^= 1u;
+            return good;
+        };
         while (ok && left > 0) {
-            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), shift = rows > kTreeRows ? 1 : 0;
-            const int row = shift ? w * kTreeRows + r : r, group_row = cur.block * 2 * kTreeRows + row;
-            const bool mine = row < rows, any = __any_sync(0xffffffffu, mine);
-            uint32_t mask[4] = {0, 0, 0, 0};
-            int32_t draft = 0, head = 0, drafts = 0;
-            if (mine) {
-                head = attention_row<true>(p, cur.key_head, group_row, draft);
-                const int32_t *m = p.masks + cur.seq * p.m_n + draft * p.m_t;
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), shift = rows > kTreeRows ? 1 : 0, steps = cnt << shift;
+            const int row0 = cur.block * 2 * kTreeRows;
+            // the row's mask, and how many drafts it sees
+            auto load_mask = [&](int row, uint32_t (&mask)[4]) -> int {
+                int32_t draft;
+                attention_row<true>(p, cur.key_head, row0 + row, draft);
+                const int32_t *at = p.masks + cur.seq * p.m_n + draft * p.m_t;
+                int drafts = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i) {
+                    mask[i] = 0;
                     if (i < p.words) {
-                        mask[i] = uint32_t(m[i * p.m_w]);
+                        mask[i] = uint32_t(at[i * p.m_w]);
                         if (p.drafts - 32 * i < 32) mask[i] &= (1u << (p.drafts - 32 * i)) - 1u;
                         drafts += __popc(mask[i]);
                     }
-            }
-            const int low = p.window > 0 ? cur.span.cached + drafts - p.window : 0;
-            float o[DP], m = -INFINITY, l = 0.f;
+                }
+                return drafts;
+            };
+            float o0[HALF], o1[HALF], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, alpha = 1.f;
 #pragma unroll
-            for (int d = 0; d < DP; ++d) o[d] = 0.f;
-            for (int j = shift ? 0 : w; j < cnt; j += shift ? 1 : 2) {
-                const int token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
-                if (!(ok = wait(bar(bars.s_full[w]), s_phase))) break;
-                s_phase ^= 1u;
+            for (int d = 0; d < HALF; ++d) o0[d] = o1[d] = 0.f;
+            // add F of step i to the output
+            auto add = [&](float (&o)[HALF], int i, float m) -> bool {
+                const int b = (parity + i) & 1, w = shift ? i & 1 : 0;
+                if (!wait(bar(bars.f_full[b]), f_phase[b])) return false;
+                f_phase[b] ^= 1u;
                 tc_fence_after();
-                float alpha = 1.f;
-                auto first_half = [&]() {
-                    tmem_store_wait();
-                    tc_fence_before();
-                    mbar_arrive(bar(bars.p_full[w][0]));
-                };
-                if (!any) first_half();
-                if (any) {
+                const bool mine = w * kTreeRows + r < rows;
+                if (!__any_sync(0xffffffffu, mine)) return true;
+                uint32_t v[HALF];
+                const unsigned f_at = tmem + unsigned(b) * 256u + 128u + unsigned(half * HALF) + lanes;
+                if constexpr (HALF == 64) tmem_load64(f_at, v); else tmem_load32(f_at, v);
+                tmem_load_wait();
+                const int j = i >> shift, token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
+                if (token0 + kTreeTok > cur.span.cached) {
+                    bool odd = false;
+#pragma unroll
+                    for (int e = 0; e < HALF; ++e) odd |= (v[e] & 0x7f800000u) == 0x7f800000u;
+                    if (rare(__any_sync(0xffffffffu, odd && mine))) {
+                        float again[HALF];
+                        const int row = mine ? w * kTreeRows + r : 0;
+                        uint32_t mask[4];
+                        const int drafts = load_mask(row, mask);
+                        tree_plain_values<T, HALF>(p, cur, infos[(info + j) % kTreeInfos], token0, p.window > 0 ? cur.span.cached + drafts - p.window : 0,
+                                                   mask[0], mask[1], mask[2], mask[3], row0 + row, m == -INFINITY ? 0.f : m, half * HALF, again);
+#pragma unroll
+                        for (int e = 0; e < HALF; ++e) v[e] = __float_as_uint(again[e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < HALF; ++e) o[e] = fmaf(o[e], alpha, __uint_as_float(v[e]));
+                return true;
+            };
+            for (int i = 0; i < steps; ++i) {
+                const int b = (parity + i) & 1, w = shift ? i & 1 : 0, j = i >> shift, row = w * kTreeRows + r;
+                const int token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
+                const unsigned s_at = tmem + unsigned(b) * 256u + unsigned(half * 64) + lanes;
+                if (!(ok = wait(bar(bars.s_full[b]), s_phase[b]))) break;
+                s_phase[b] ^= 1u;
+                tc_fence_after();
+                float next_alpha = 1.f;
+                if (__any_sync(0xffffffffu, row < rows)) {
                     const uint32_t *words = infos[(info + j) % kTreeInfos];
-                    const uint32_t seen[4] = {words[0], words[1], words[2], words[3]};
-                    const bool masked = (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
+                    const bool masked = (words[0] & words[1] & words[2] & words[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
                                         (p.window > 0 && token0 < cur.span.cached + p.drafts - p.window);
-                    // what is visible of tokens first .. first + 31 of the tile
-                    auto visible = [&](int first) { return tree_visible(token0 + first, cur.span.cached, low, mask) & seen_at(seen, first >> 5); };
+                    uint32_t vis[2] = {~0u, ~0u};
+                    if (masked) {
+                        uint32_t mask[4];
+                        const int drafts = load_mask(row < rows ? row : 0, mask), low = p.window > 0 ? cur.span.cached + drafts - p.window : 0;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            vis[c] = drafts == 0 ? 0u : tree_visible(token0 + 64 * half + 32 * c, cur.span.cached, low, mask) & words[2 * half + c];
+                    }
                     float top = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < 2; ++c) {
+                    {
                         uint32_t v[64];
-                        tmem_load64(s_at + 64u * c, v);
-                        uint32_t vis[2] = {~0u, ~0u};
-                        if (masked) { vis[0] = visible(64 * c); vis[1] = visible(64 * c + 32); }
+                        tmem_load64(s_at, v);
                         tmem_load_wait();
                         if (!masked) {
 #pragma unroll
-                            for (int i = 0; i < 64; i += 2) top = fmaxf(top, fmaxf(__uint_as_float(v[i]) * p.scale_log2, __uint_as_float(v[i + 1]) * p.scale_log2));
+                            for (int e = 0; e < 64; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(v[e]) * p.scale_log2, __uint_as_float(v[e + 1]) * p.scale_log2));
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 64; ++i) top = (vis[i >> 5] >> (i & 31)) & 1 ? fmaxf(top, __uint_as_float(v[i]) * p.scale_log2) : top;
+                            for (int e = 0; e < 64; ++e) top = (vis[e >> 5] >> (e & 31)) & 1 ? fmaxf(top, __uint_as_float(v[e]) * p.scale_log2) : top;
                         }
                     }
-                    const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
-                    alpha = m == now ? 1.f : ex2(m - now);
-                    m = now;
+                    tops[i & 1][half][r] = top;
+                    if (!(ok = pair_wait())) break;
+                    top = fmaxf(top, tops[i & 1][half ^ 1][r]);
+                    const float m = w ? m1 : m0, now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
+                    next_alpha = m == now ? 1.f : ex2(m - now);
                     float sum[2] = {0.f, 0.f};
                     // 16 tokens: S -> P in two parts, in the place of S; the next 16 are on their way meanwhile
-                    auto probabilities = [&](const uint32_t (&v)[16], int c, uint32_t vis) {
+                    auto probabilities = [&](const uint32_t (&v)[16], int c, uint32_t seen, bool all) {
                         uint32_t out[16];
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            float e[2];
+                        for (int e = 0; e < 16; e += 2) {
+                            float x[2];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                e[h] = ex2(fmaf(__uint_as_float(v[i + h]), p.scale_log2, -base));
-                                if (AttentionBias<T>::factor != 1.f) e[h] *= AttentionBias<T>::factor;
-                                if (masked) e[h] = (vis >> (i + h)) & 1 ? e[h] : 0.f;
+                                x[h] = ex2(fmaf(__uint_as_float(v[e + h]), p.scale_log2, -base));
+                                if (AttentionBias<T>::factor != 1.f) x[h] *= AttentionBias<T>::factor;
+                                if (!all) x[h] = (seen >> (e + h)) & 1 ? x[h] : 0.f;
                             }
-                            sum[0] += e[0];
-                            sum[1] += e[1];
-                            const uint32_t hi = pack2(e[0], e[1], T());
-                            float a, b;
-                            unpack_word(hi, a, b, T());
-                            out[i / 2] = hi;
-                            out[8 + i / 2] = pack2(e[0] - a, e[1] - b, T());
+                            sum[0] += x[0];
+                            sum[1] += x[1];
+                            const uint32_t hi = pack2(x[0], x[1], T());
+                            float a, c2;
+                            unpack_word(hi, a, c2, T());
+                            out[e / 2] = hi;
+                            out[8 + e / 2] = pack2(x[0] - a, x[1] - c2, T());
                         }
                         tmem_store16u(s_at + 16u * c, out);
                     };
@@ -598,128 +650,71 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                     tmem_load16(s_at, va);
                     tmem_load_wait();
                     if (!masked) {
-#pragma unroll 1
-                        for (int c = 0; c < 8; c += 2) {
+#pragma unroll
+                        for (int c = 0; c < 4; c += 2) {
                             tmem_load16(s_at + 16u * (c + 1), vb);
-                            probabilities(va, c, ~0u);
+                            probabilities(va, c, 0, true);
                             tmem_load_wait();
-                            if (c < 6) tmem_load16(s_at + 16u * (c + 2), va);
-                            probabilities(vb, c + 1, ~0u);
-                            tmem_load_wait();
-                            if (c == 2) first_half();
+                            if (c < 2) tmem_load16(s_at + 16u * (c + 2), va);
+                            probabilities(vb, c + 1, 0, true);
+                            if (c < 2) tmem_load_wait();
                         }
                     } else {
 #pragma unroll 1
-                        for (int c = 0; c < 8; ++c) {
-                            const uint32_t vis = visible(16 * c & ~31) >> (16 * (c & 1));
+                        for (int c = 0; c < 4; ++c) {
                             if (c > 0) {
                                 tmem_load16(s_at + 16u * c, va);
                                 tmem_load_wait();
                             }
-                            probabilities(va, c, vis);
-                            if (c == 3) first_half();
+                            probabilities(va, c, (c < 2 ? vis[0] : vis[1]) >> (16 * (c & 1)), false);
                         }
                     }
                     tmem_store_wait();
-                    l = l * alpha + (sum[0] + sum[1]);
+                    const float l = (w ? l1 : l0) * next_alpha + (sum[0] + sum[1]);
+                    if (w) { m1 = now; l1 = l; } else { m0 = now; l0 = l; }
                 }
                 tc_fence_before();
-                mbar_arrive(bar(bars.p_full[w][1]));
-                if (!(ok = wait(bar(bars.f_full[w]), f_phase))) break;
-                f_phase ^= 1u;
-                tc_fence_after();
-                if (any) {
-#pragma unroll
-                    for (int c = 0; c < DP / 64; ++c) {
-                        uint32_t v[64];
-                        tmem_load64(f_at + 64u * c, v);
-                        tmem_load_wait();
-                        if (token0 + kTreeTok > cur.span.cached) {
-                            bool odd = false;
-#pragma unroll
-                            for (int i = 0; i < 64; ++i) odd |= (v[i] & 0x7f800000u) == 0x7f800000u;
-                            if (rare(__any_sync(0xffffffffu, odd && mine))) {
-                                float again[64];
-                                tree_plain_values<T>(p, cur, infos[(info + j) % kTreeInfos], token0, low, mask[0], mask[1], mask[2], mask[3],
-                                                     mine ? group_row : cur.block * 2 * kTreeRows, m == -INFINITY ? 0.f : m, 64 * c, again);
-#pragma unroll
-                                for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(again[i]);
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) o[64 * c + i] = fmaf(o[64 * c + i], alpha, __uint_as_float(v[i]));
-                    }
-                }
+                mbar_arrive(bar(bars.p_full[b]));
+                if (i > 0 && !(ok = (shift && w == 0) ? add(o1, i - 1, m1) : add(o0, i - 1, m0))) break;
+                alpha = next_alpha;
             }
             if (!ok) break;
-            if (drafts == 0) { m = -INFINITY; l = 0.f; }
-            // both groups have parts of the same rows: the second one's goes through tensor memory
-            if (!shift) {
-                if (w == 1) {
-#pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t v[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(o[32 * c + i]);
-                        tmem_store32u(f_at + 32u * c, v);
-                    }
-                    tmem_store_wait();
-                    other[r] = make_float2(m, l);
-                    tc_fence_before();
-                    mbar_arrive(bar(bars.given));
-                    if (!(ok = wait(bar(bars.taken), join_phase))) break;
-                    tc_fence_after();
-                } else {
-                    if (!(ok = wait(bar(bars.given), join_phase))) break;
-                    tc_fence_after();
-                    const float2 b = other[r];
-                    const float top = fmaxf(m, b.x), wa = join_weight(m, top), wb = join_weight(b.x, top);
-#pragma unroll
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t v[32];
-                        tmem_load32(f_at + 256u + 32u * c, v);
-                        tmem_load_wait();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[32 * c + i] = fmaf(o[32 * c + i], wa, __uint_as_float(v[i]) * wb);
-                    }
-                    l = l * wa + b.y * wb;
-                    m = top;
-                    tc_fence_before();
-                    mbar_arrive(bar(bars.taken));
-                }
-                join_phase ^= 1u;
-            }
+            if (!(ok = shift ? add(o1, steps - 1, m1) : add(o0, steps - 1, m0))) break;
+            parity = (parity + steps) & 1;
             const bool whole = cur.tile == 0 && cnt == cur.span.tiles;
-            if (mine && (shift || w == 0)) {
-                if (whole) {
-                    const bool nothing = l == 0.f;
-                    const float inv = 1.f / l;
-                    T *dst = static_cast<T *>(p.o) + cur.seq * p.o_n + draft * p.o_t + int64_t(head) * p.o_h;
+            // the two warps' sums
+            auto finish = [&](float (&o)[HALF], float m, float l, int w) -> bool {
+                tops[0][half][r] = l;
+                if (!pair_wait()) return false;
+                l += tops[0][half ^ 1][r];
+                if (!pair_wait()) return false;                  // read by both before either writes again
+                const int row = w * kTreeRows + r;
+                if (row >= rows) return true;
+                int32_t draft;
+                const int head = attention_row<true>(p, cur.key_head, row0 + row, draft);
+                uint32_t mask[4];
+                if (load_mask(row, mask) == 0) { m = -INFINITY; l = 0.f; }
+                if (!whole) {
+                    float *part = tp.partial + ((2 * int64_t(blockIdx.x) + (cur.tile == 0 ? 1 : 0)) * 2 + w) * Shape::PART;
 #pragma unroll
-                    for (int d = 0; d < DP; d += 8) {
-                        if (d >= p.dim_v) break;
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = nothing ? 0.f : o[d + e] * inv;
-                        if (tp.vec_o && d + 8 <= p.dim_v) {
-                            *reinterpret_cast<uint4 *>(dst + d) = pack_vector<T, 8>(x);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (d + e < p.dim_v) dst[(d + e) * p.o_d] = from_f32<T>(x[e]);
-                        }
+                    for (int d = 0; d < HALF; ++d) part[(half * HALF + d) * kTreeRows + r] = o[d];
+                    if (half == 0) {
+                        part[DP * kTreeRows + r] = m;
+                        part[DP * kTreeRows + kTreeRows + r] = l;
                     }
-                    if (p.lse)
-                        p.lse[(int64_t(cur.seq) * p.drafts + draft) * p.heads + head] = nothing ? -INFINITY
-                            : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
-                } else {
-                    float *part = tp.partial + ((2 * int64_t(blockIdx.x) + (cur.tile == 0 ? 1 : 0)) * 2 + (shift ? w : 0)) * Shape::PART;
-#pragma unroll
-                    for (int d = 0; d < DP; ++d) part[d * kTreeRows + r] = o[d];
-                    part[DP * kTreeRows + r] = m;
-                    part[DP * kTreeRows + kTreeRows + r] = l;
+                    return true;
                 }
-            }
+                const bool nothing = l == 0.f;
+                const float inv = 1.f / l;
+                T *dst = static_cast<T *>(p.o) + cur.seq * p.o_n + draft * p.o_t + int64_t(head) * p.o_h;
+                tree_write<T, HALF>(dst, half * HALF, p.dim_v, p.o_d, tp.vec_o, o, nothing ? 0.f : inv, nothing);
+                if (p.lse && half == 0)
+                    p.lse[(int64_t(cur.seq) * p.drafts + draft) * p.heads + head] = nothing ? -INFINITY
+                        : (m + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
+                return true;
+            };
+            if (!(ok = finish(o0, m0, l0, 0))) break;
+            if (shift && !(ok = finish(o1, m1, l1, 1))) break;
             if (!whole) parts[cur.tile == 0 ? 1 : 0] = cur.seq * head_blocks + cur.hb;
             info = (info + cnt) % kTreeInfos;
             left -= cnt;
@@ -759,54 +754,82 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     }
 }
 
-// Items that span CTAs, as in the one-token kernels: block (c, y) joins 32 rows of the item that begins in CTA c's range and ends in a
-// later one's; a lane to a row, a warp to DP / 8 elements.
-constexpr int kTreeJoinThreads = 256;
+// Items that span CTAs, as in the one-token kernels: block (c, y) joins 16 rows of the item that begins in CTA c's range and ends in a
+// later one's; a thread has DP / 16 elements of a row.  The parts' maxima, and eight parts' elements, are loaded side by side.
+constexpr int kTreeJoinThreads = 256, kTreeJoinRows = 16;
 template <typename T, int DP>
 __global__ void __launch_bounds__(kTreeJoinThreads) tree_join_kernel(const __grid_constant__ TreeParams tp, int ctas)
 {
-    constexpr int EACH = DP / 8;
+    constexpr int GROUPS = kTreeJoinThreads / kTreeJoinRows, EACH = DP / GROUPS, AHEAD = 4;
     const AttentionParams &p = tp.a;
     __shared__ int32_t parts;
-    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ float all_tops[GROUPS][kTreeJoinRows], all_sums[GROUPS][kTreeJoinRows];
+    const int c = blockIdx.x, tid = threadIdx.x, group = tid / kTreeJoinRows;
     early_begin();
     const int32_t item = load_now(tp.partial_item + 2 * c + 1);
     if (item < 0) return;
     const int left = ctas - c;
+    const int32_t other = tid + 1 < left ? load_now(tp.partial_item + 2 * (c + tid + 1)) : -1;
     if (tid == 0) parts = left;
     __syncthreads();
-    for (int i = tid + 1; i < left; i += kTreeJoinThreads)
-        if (tp.partial_item[2 * (c + i)] != item) { atomicMin(&parts, i); break; }
+    if (tid + 1 < left && other != item) atomicMin(&parts, tid + 1);
+    for (int i = tid + 1 + kTreeJoinThreads; i < left; i += kTreeJoinThreads)
+        if (tp.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
     __syncthreads();
     const int n = parts;
     const int head_blocks = p.key_heads * p.blocks;
     const int seq = item / head_blocks, hb = item - seq * head_blocks, kh = hb / p.blocks, block = hb - kh * p.blocks;
-    const int row = blockIdx.y * 32 + lane, group_row = block * 2 * kTreeRows + row, rows = min(2 * kTreeRows, p.group - block * 2 * kTreeRows);
-    if (row >= rows) return;
+    const int row = blockIdx.y * kTreeJoinRows + tid % kTreeJoinRows, group_row = block * 2 * kTreeRows + row;
+    const bool mine = row < min(2 * kTreeRows, p.group - block * 2 * kTreeRows);
     const float *first = tp.partial + (4 * int64_t(c) + (row >> 7)) * TreeShape<DP>::PART + (row & 127);
     auto part = [&](int i) { return first + (i == 0 ? 2 : 4 * int64_t(i)) * TreeShape<DP>::PART; };
-    float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, part(i)[DP * kTreeRows]);
-    float o[EACH], l = 0.f;
+    // every 16th part's maximum and sum to a group
+    float top = -INFINITY, l = 0.f;
+    for (int i = group; mine && i < n; i += GROUPS) {
+        const float m = part(i)[DP * kTreeRows], x = part(i)[DP * kTreeRows + kTreeRows], now = fmaxf(top, m);
+        l = l * join_weight(top, now) + x * join_weight(m, now);
+        top = now;
+    }
+    all_tops[group][tid % kTreeJoinRows] = top;
+    all_sums[group][tid % kTreeJoinRows] = l;
+    __syncthreads();
+    if (!mine) return;
+    top = -INFINITY;
+    for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, all_tops[i][tid % kTreeJoinRows]);
+    l = 0.f;
+    for (int i = 0; i < GROUPS; ++i) l = fmaf(all_sums[i][tid % kTreeJoinRows], join_weight(all_tops[i][tid % kTreeJoinRows], top), l);
+    float o[EACH];
 #pragma unroll
     for (int d = 0; d < EACH; ++d) o[d] = 0.f;
-#pragma unroll 2
-    for (int i = 0; i < n; ++i) {
-        const float *at = part(i);
-        const float share = join_weight(at[DP * kTreeRows], top);
-        l = fmaf(at[DP * kTreeRows + kTreeRows], share, l);
+    for (int i = 0; i < n; i += AHEAD) {
+        float x[AHEAD][EACH], m[AHEAD];
 #pragma unroll
-        for (int d = 0; d < EACH; ++d) o[d] = fmaf(at[(warp * EACH + d) * kTreeRows], share, o[d]);
+        for (int a = 0; a < AHEAD; ++a) {
+            m[a] = -INFINITY;
+            if (i + a < n) m[a] = part(i + a)[DP * kTreeRows];
+#pragma unroll
+            for (int d = 0; d < EACH; ++d) x[a][d] = i + a < n ? part(i + a)[(group * EACH + d) * kTreeRows] : 0.f;
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (i + a >= n) continue;
+            const float share = join_weight(m[a], top);
+#pragma unroll
+            for (int d = 0; d < EACH; ++d) o[d] = fmaf(x[a][d], share, o[d]);
+        }
     }
     int32_t draft;
     const int head = attention_row<true>(p, kh, group_row, draft);
     const bool nothing = l == 0.f;
-    const float inv = 1.f / l;
     T *dst = static_cast<T *>(p.o) + seq * p.o_n + draft * p.o_t + int64_t(head) * p.o_h;
+    if constexpr (EACH == 8) {
+        tree_write<T, 8>(dst, group * 8, p.dim_v, p.o_d, tp.vec_o, o, 1.f / l, nothing);
+    } else {
 #pragma unroll
-    for (int d = 0; d < EACH; ++d)
-        if (warp * EACH + d < p.dim_v) dst[(warp * EACH + d) * p.o_d] = from_f32<T>(nothing ? 0.f : o[d] * inv);
-    if (warp == 0 && p.lse)
+        for (int d = 0; d < EACH; ++d)
+            if (group * EACH + d < p.dim_v) dst[(group * EACH + d) * p.o_d] = from_f32<T>(nothing ? 0.f : o[d] * (1.f / l));
+    }
+    if (group == 0 && p.lse)
         p.lse[(int64_t(seq) * p.drafts + draft) * p.heads + head] = nothing ? -INFINITY : (top + (log2f(l) - AttentionBias<T>::value)) * 0.6931471805599453f;
 }
 

@@ -152,21 +152,26 @@ void encode_maps(const btc_tree_attention_s &op, TreeParams &tp, TreeMaps &m)
     }
 }
 
-template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, const TreeMaps &maps, int device, int ctas, cudaStream_t st)
+template <typename T, int DP, bool WIDE> btc_error_t launch_umma_rows(const TreeParams &p, const TreeMaps &maps, int device, int ctas, cudaStream_t st)
 {
     static std::atomic<bool> configured[64] = {};
     const int slot = device & 63;
     if (!configured[slot].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(tree_umma_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<DP>::SMEM) != cudaSuccess) {
+        if (cudaFuncSetAttribute(tree_umma_kernel<T, DP, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<DP>::SMEM) != cudaSuccess) {
             cudaGetLastError();
             return BTC_ERR_CUDA;
         }
         configured[slot].store(true, std::memory_order_relaxed);
     }
-    const btc_error_t rc = launch_early(tree_umma_kernel<T, DP>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p, maps.q, maps.k, maps.v);
+    const btc_error_t rc = launch_early(tree_umma_kernel<T, DP, WIDE>, dim3(unsigned(ctas)), kTreeThreads, TreeShape<DP>::SMEM, st, p, maps.q, maps.k, maps.v);
     if (rc != BTC_SUCCESS) return rc;
     const int rows = std::min(p.a.group, 2 * kTreeRows);
     return launch_early(tree_join_kernel<T, DP>, dim3(unsigned(ctas), unsigned((rows + kTreeJoinRows - 1) / kTreeJoinRows)), kTreeJoinThreads, 0, st, p, ctas);
+}
+
+template <typename T, int DP> btc_error_t launch_umma(const TreeParams &p, const TreeMaps &maps, int device, int ctas, cudaStream_t st)
+{
+    return p.a.group > kTreeRows ? launch_umma_rows<T, DP, true>(p, maps, device, ctas, st) : launch_umma_rows<T, DP, false>(p, maps, device, ctas, st);
 }
 
 }  // namespace

@@ -29,7 +29,7 @@ namespace btc {
 
 constexpr int kTreeTok = 128, kTreeRows = 128;
 constexpr int kTreeItemTiles = 1;            // what beginning and ending an item costs, in tiles
-constexpr int kTreeThreads = 384, kTreeLoaders = 96;
+constexpr int kTreeThreads = 384;
 constexpr int kTreeInfos = 8;                // tiles whose visible tokens are kept: more than the ring can be ahead of the softmax
 
 template <int DP> struct TreeShape {
@@ -82,9 +82,23 @@ struct TreeCursor {
     __device__ __forceinline__ int rows(const AttentionParams &p) const { return min(2 * kTreeRows, p.group - block * 2 * kTreeRows); }
 };
 
+// The order in which an item's n tiles of keys and values go through the ring: that in which they are used.  Two steps a tile: K0 V0 K1 V1
+// ..; one step: scores run two tiles ahead, K0 K1 V0 K2 V1 .. (values that come with their keys hold a place for two steps, and
+// the ring is then too short for the memory's latency).
+__device__ __forceinline__ int tree_place_k(int j, bool two) { return two ? 2 * j : (j == 0 ? 0 : 2 * j - 1); }
+__device__ __forceinline__ int tree_place_v(int j, int n, bool two) { return two || j == n - 1 ? 2 * j + 1 : 2 * j + 2; }
+__device__ __forceinline__ int tree_placed(int i, int n, bool two, int &kv)
+{
+    if (two) { kv = i & 1; return i >> 1; }
+    if (i == 0) { kv = 0; return 0; }
+    if (i == 2 * n - 1) { kv = 1; return n - 1; }
+    kv = (i & 1) ^ 1;
+    return kv ? (i - 2) >> 1 : (i + 1) >> 1;
+}
+
 struct TreeBarriers {
     uint64_t full[8], empty[8];              // ring of keys and values
-    uint64_t q_full, q_empty;
+    uint64_t q_full[2], q_empty[2];          // two places for 128 rows of queries, taken in turn
     uint64_t s_full[2], p_full[2], f_full[2];
     uint64_t pair[4];                        // the two warps that share rows
     uint64_t drain;
@@ -93,7 +107,7 @@ struct TreeBarriers {
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -165,7 +179,8 @@ __device__ __forceinline__ void tree_write(T *dst, int d0, int dim, int64_t stri
     }
 }
 
-template <typename T, int DP>
+// WIDE: items may have more than 128 rows; otherwise a thread keeps one output and has room for its scores
+template <typename T, int DP, bool WIDE>
 __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid_constant__ TreeParams tp, const __grid_constant__ CUtensorMap map_q,
                                                                     const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
@@ -191,10 +206,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     auto wait = [&](unsigned b, unsigned phase) -> bool { return __all_sync(0xffffffffu, mbar_wait_bounded(b, phase, abort_flag, nullptr, 0)); };
 
     if (tid == 0) {
-        for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), kTreeLoaders); mbar_init(bar(bars.empty[i]), 1); }
-        mbar_init(bar(bars.q_full), kTreeLoaders);
-        mbar_init(bar(bars.q_empty), 1);
-        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w]), 256); mbar_init(bar(bars.f_full[w]), 1); }
+        for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), 32); mbar_init(bar(bars.empty[i]), 1); }
+        for (int w = 0; w < 2; ++w) { mbar_init(bar(bars.q_full[w]), 32); mbar_init(bar(bars.q_empty[w]), 1); mbar_init(bar(bars.s_full[w]), 1); mbar_init(bar(bars.p_full[w]), 256); mbar_init(bar(bars.f_full[w]), 1); }
         for (int i = 0; i < 4; ++i) mbar_init(bar(bars.pair[i]), 64);
         mbar_init(bar(bars.drain), 1);
         abort_word = 0;
@@ -290,152 +303,140 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
     if (warp < 11) {
-        // ---- loaders ----
+        // ---- loaders: a copy of 128 tokens' keys or values to a warp, in turn; the first one also brings the queries ----
         constexpr int CHUNKS = DP / 8, STEP = 32 / CHUNKS;       // chunks of a row; rows of a warp's copy
         const int lw = warp - 8, sub = lane / CHUNKS, chunk = lane % CHUNKS;
-        const int bytes_k = max(0, min(16, (p.dim_k - chunk * 8) * 2)), bytes_v = max(0, min(16, (p.dim_v - chunk * 8) * 2));
         const unsigned in_row = unsigned((chunk >> 3) * PANEL);
-        int slot = 0, info = 0;
+        int turn = 0, info = 0, q_slot = 0, slot = 0;            // copies so far modulo 3; the next one's place in the ring
         unsigned phase = 0, q_phase = 0;
-        bool ok = true, first = true;
-        auto take = [&]() -> bool {                              // the next place of the ring is free
-            return wait(bar(bars.empty[slot]), phase ^ 1u);
-        };
-        // pages of the tokens lane, lane + 32, .. of the item's i-th tile; -1: not visible, or no page
-        auto look_up = [&](int i, int32_t (&page)[4]) {
+        bool ok = true;
+        while (ok && left > 0) {
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), row0 = cur.block * 2 * kTreeRows;
+            const bool two = WIDE && rows > kTreeRows;
+#pragma unroll 1
+            for (int w = 0; w < (two ? 2 : 1); ++w) {
+                const unsigned full = bar(bars.q_full[q_slot]), to = q_at + unsigned(q_slot) * TILE;
+                if (lw == 0) {
+                    if (!(ok = wait(bar(bars.q_empty[q_slot]), q_phase ^ 1u))) break;
+                    if (tp.box_q) {
+                        // a box: the heads that share a key head x some drafts, in the order of the rows (zeros behind the last draft)
+                        if (elect_one()) {
+                            mbar_arrive_expect_tx(full, unsigned(PANELS * tp.box_q) * p.sharing.d * 128u);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int t = (cur.span.first_tile + cur.tile + i) * kTreeTok + 32 * g + lane;
-                page[g] = -1;
-                if (t >= cur.span.begin && t < cur.span.end) {
-                    const int32_t n = p.table[cur.seq * p.table_n + int64_t(p.page.div(uint32_t(t))) * p.table_j];
-                    page[g] = n;
-                    if (rare(n < 0 || n >= p.pages)) {
+                            for (int pn = 0; pn < PANELS; ++pn)
+                                tma_load_box(to + unsigned(pn) * PANEL, &map_q, full, 64 * pn, 0, int(p.sharing.div(uint32_t(row0 + w * kTreeRows))), cur.key_head, cur.seq);
+                        } else {
+                            mbar_arrive(full);
+                        }
+                        __syncwarp();
+                    } else {
+                        const int bytes_k = max(0, min(16, (p.dim_k - chunk * 8) * 2));
+#pragma unroll 1
+                        for (int r = sub; r < kTreeRows; r += STEP) {
+                            const int row = w * kTreeRows + r;
+                            const T *src = static_cast<const T *>(p.q);
+                            const bool there = row < rows;
+                            if (there) {
+                                int32_t draft;
+                                const int64_t head = attention_row<true>(p, cur.key_head, row0 + row, draft);
+                                src += cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
+                            }
+                            const unsigned dst = to + in_row + unsigned(r) * 128u + unsigned(((chunk ^ r) & 7) << 4);
+                            if (tp.vec_q) {
+                                const int bytes = there ? bytes_k : 0;
+                                cp_async_part(dst, bytes ? src + chunk * 8 : static_cast<const T *>(p.q), bytes);
+                            } else {
+#pragma unroll 1
+                                for (int e = 0; e < 8; ++e) {
+                                    unsigned short x = 0;
+                                    if (there && chunk * 8 + e < p.dim_k) x = *reinterpret_cast<const unsigned short *>(src + (chunk * 8 + e) * p.q_d);
+                                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2u * unsigned(e)), "h"(x) : "memory");
+                                }
+                            }
+                        }
+                        if (tp.vec_q) mbar_arrive_on_copies(full); else mbar_arrive(full);
+                    }
+                }
+                if ((q_slot ^= 1) == 0) q_phase ^= 1u;
+            }
+            if (!ok) break;
+#pragma unroll 1
+            for (int i = 0; i < 2 * cnt; ++i) {
+                const bool my_turn = turn == lw;
+                if (++turn == 3) turn = 0;
+                const int here = slot;
+                const unsigned here_phase = phase;
+                if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                if (!my_turn) continue;
+                int kv;
+                const int j = tree_placed(i, cnt, two, kv), token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
+                // pages of the tokens lane, lane + 32, ..: -1 where the token is not visible or its entry is no page
+                int32_t page[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int t = token0 + 32 * g + lane;
+                    page[g] = -1;
+                    if (t >= cur.span.begin && t < cur.span.end) page[g] = p.table[cur.seq * p.table_n + int64_t(p.page.div(uint32_t(t))) * p.table_j];
+                }
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int t = token0 + 32 * g + lane;
+                    if (rare(page[g] >= p.pages || (page[g] < 0 && t >= cur.span.begin && t < cur.span.end))) {
                         if (p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
                         page[g] = -1;
                     }
                 }
-            }
-        };
-        while (ok && left > 0) {
-            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), row0 = cur.block * 2 * kTreeRows;
-            // queries
-            if (!first && !(ok = wait(bar(bars.q_empty), q_phase))) break;
-            if (!first) q_phase ^= 1u;
-            first = false;
-            const int groups = rows > kTreeRows ? 2 : 1;
-            if (tp.box_q) {
-                // a box: the heads that share a key head x some drafts, in the order of the rows (zeros behind the last draft)
-                if (lw == 0) {
-                    if (lane == 0) mbar_arrive_expect_tx(bar(bars.q_full), unsigned(groups * PANELS * tp.box_q) * p.sharing.d * 128u);
-                    else mbar_arrive(bar(bars.q_full));
+                if (!(ok = wait(bar(bars.empty[here]), here_phase ^ 1u))) break;
+                if (kv == 0) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const uint32_t seen = __ballot_sync(0xffffffffu, page[g] >= 0);
+                        if (lane == g) infos[(info + j) % kTreeInfos][g] = seen;
+                    }
+                }
+                const unsigned dst = ring_at + unsigned(here) * TILE, full = bar(bars.full[here]);
+                if (tp.box_kv && token0 >= cur.span.begin && token0 + kTreeTok <= cur.span.end) {
+                    // all tokens are visible: boxes of a page's rows, zeros where the page is none (its number lies outside)
+                    if (elect_one()) mbar_arrive_expect_tx(full, TILE);
+                    else mbar_arrive(full);
                     __syncwarp();
-                    if (lane < groups * PANELS) {
-                        const int w = lane / PANELS, pn = lane % PANELS;
-                        tma_load_box(q_at + unsigned(w) * TILE + unsigned(pn) * PANEL, &map_q, bar(bars.q_full), 64 * pn, 0,
-                                     int(p.sharing.div(uint32_t(row0 + w * kTreeRows))), cur.key_head, cur.seq);
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        // boxes that begin in these 32 tokens: one each 8, 16 or 32, or the first of 64 or 128
+                        if (g & (max(tp.box_kv, 32) / 32 - 1)) continue;
+#pragma unroll 1
+                        for (int o = 0; o < 32; o += tp.box_kv) {
+                            const int32_t n = __shfl_sync(0xffffffffu, page[g], o);
+                            const int t = token0 + 32 * g + o, row = t - int32_t(p.page.div(uint32_t(t)) * p.page.d);
+                            if (elect_one()) {
+#pragma unroll
+                                for (int pn = 0; pn < PANELS; ++pn)
+                                    tma_load_box4(dst + unsigned(pn) * PANEL + unsigned(32 * g + o) * 128u, kv == 0 ? &map_k : &map_v, full, 64 * pn, row, cur.key_head, n);
+                            }
+                            __syncwarp();
+                        }
                     }
                 } else {
-                    mbar_arrive(bar(bars.q_full));
-                }
-            } else {
-#pragma unroll 1
-                for (int i = lw * STEP; i < groups * kTreeRows; i += 3 * STEP) {
-                    const int r = i + sub;
-                    const T *src = static_cast<const T *>(p.q);
-                    const bool there = r < rows;
-                    if (there) {
-                        int32_t draft;
-                        const int64_t head = attention_row<true>(p, cur.key_head, row0 + r, draft);
-                        src += cur.seq * p.q_n + head * p.q_h + draft * p.q_t;
-                    }
-                    const unsigned dst = q_at + unsigned(r >> 7) * TILE + in_row + unsigned(r & 127) * 128u + unsigned(((chunk ^ r) & 7) << 4);
-                    if (tp.vec_q) {
-                        const int bytes = there ? bytes_k : 0;
-                        cp_async_part(dst, bytes ? src + chunk * 8 : static_cast<const T *>(p.q), bytes);
-                    } else {
-#pragma unroll 1
-                        for (int e = 0; e < 8; ++e) {
-                            unsigned short x = 0;
-                            if (there && chunk * 8 + e < p.dim_k) x = *reinterpret_cast<const unsigned short *>(src + (chunk * 8 + e) * p.q_d);
-                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst + 2u * unsigned(e)), "h"(x) : "memory");
-                        }
-                    }
-                }
-                if (tp.vec_q) mbar_arrive_on_copies(bar(bars.q_full)); else mbar_arrive(bar(bars.q_full));
-            }
-            // keys and values, tile by tile; the next tile's pages are looked up ahead
-            int32_t page[4];
-            look_up(0, page);
-            for (int i = 0; i < cnt; ++i) {
-                int32_t next_page[4] = {-1, -1, -1, -1};
-                if (i + 1 < cnt) look_up(i + 1, next_page);
-                const int token0 = (cur.span.first_tile + cur.tile + i) * kTreeTok;
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv) {
-                    if (!(ok = take())) break;
-                    if (kv == 0) {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const uint32_t seen = __ballot_sync(0xffffffffu, page[g] >= 0);
-                            if (lw == 0 && lane == g) infos[info][g] = seen;
-                        }
-                        if (++info == kTreeInfos) info = 0;
-                    }
-                    const unsigned dst = ring_at + unsigned(slot) * TILE;
-                    if (tp.box_kv && token0 >= cur.span.begin && token0 + kTreeTok <= cur.span.end) {
-                        // all tokens are visible: boxes of a page's rows, zeros where the page is none (its number lies outside)
-                        if (lw == 0) {
-                            if (lane == 0) mbar_arrive_expect_tx(bar(bars.full[slot]), TILE);
-                            else mbar_arrive(bar(bars.full[slot]));
-                            __syncwarp();
-                            const int boxes = kTreeTok / tp.box_kv;
-#pragma unroll
-                            for (int i = 0; i < PANELS; ++i) {
-                                const int which = lane + 32 * i, pn = which / boxes, o = (which - pn * boxes) * tp.box_kv;
-                                int32_t n = 0;
-#pragma unroll
-                                for (int g = 0; g < 4; ++g) {
-                                    const int32_t x = __shfl_sync(0xffffffffu, page[g], o & 31);
-                                    if ((o >> 5) == g) n = x;
-                                }
-                                if (pn < PANELS) {
-                                    const int t = token0 + o, row = t - int32_t(p.page.div(uint32_t(t)) * p.page.d);
-                                    tma_load_box4(dst + unsigned(pn) * PANEL + unsigned(o) * 128u, kv == 0 ? &map_k : &map_v, bar(bars.full[slot]), 64 * pn, row,
-                                                  cur.key_head, n);
-                                }
-                            }
-                        } else {
-                            mbar_arrive(bar(bars.full[slot]));
-                        }
-                        if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
-                        continue;
-                    }
                     const T *base = static_cast<const T *>(kv == 0 ? p.k : p.v) + cur.key_head * (kv == 0 ? p.k_head : p.v_head) + chunk * 8;
                     const uint32_t s_page = kv == 0 ? tp.k_page16 : tp.v_page16, s_slot = kv == 0 ? tp.k_slot16 : tp.v_slot16;
-                    const int bytes = kv == 0 ? bytes_k : bytes_v;
+                    const int bytes = max(0, min(16, ((kv == 0 ? p.dim_k : p.dim_v) - chunk * 8) * 2));
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         // in units of 16 bytes, so that 32 bits hold it: one exchange per row
                         const int t = token0 + 32 * g + lane;
                         const uint32_t at = page[g] < 0 ? ~0u : uint32_t(page[g]) * s_page + uint32_t(t - int32_t(p.page.div(uint32_t(t)) * p.page.d)) * s_slot;
-#pragma unroll
-                        for (int i = 0; i < (32 + 3 * STEP - 1) / (3 * STEP); ++i) {
-                            const int j = (3 * i + lw) * STEP;
-                            const uint32_t from = __shfl_sync(0xffffffffu, at, (j + sub) & 31);
+#pragma unroll 4
+                        for (int r = 0; r < 32; r += STEP) {
+                            const uint32_t from = __shfl_sync(0xffffffffu, at, r + sub);
                             const int n16 = from == ~0u ? 0 : bytes;
-                            if (j < 32)
-                                cp_async_part(dst + in_row + unsigned(32 * g + j + sub) * 128u + unsigned(((chunk ^ (j + sub)) & 7) << 4),
-                                              base + (n16 ? int64_t(from) * 8 : -chunk * 8), n16);
+                            cp_async_part(dst + in_row + unsigned(32 * g + r + sub) * 128u + unsigned(((chunk ^ (r + sub)) & 7) << 4),
+                                          base + (n16 ? int64_t(from) * 8 : -chunk * 8), n16);
                         }
                     }
-                    mbar_arrive_on_copies(bar(bars.full[slot]));
-                    if (++slot == SLOTS) { slot = 0; phase ^= 1u; }
+                    mbar_arrive_on_copies(full);
                 }
-                if (!ok) break;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) page[g] = next_page[g];
             }
+            info = (info + cnt) % kTreeInfos;
             left -= cnt;
             cur.next(p);
         }
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         const unsigned full0 = bar(bars.full[0]), empty0 = bar(bars.empty[0]);
         int base_slot = 0;                                       // place and round of the item's first keys in the ring
         unsigned base_phase = 0, q_phase = 0, p_phase[2] = {0, 0};
-        int parity = 0;                                          // of the item's first step
+        int parity = 0, q_slot = 0;                              // of the item's first step; next place of queries
         bool ok = true;
         auto place = [&](int i, unsigned &phase) {               // of the i-th tile copied since base
             int s = base_slot + i;
@@ -454,18 +455,25 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             return s % SLOTS;
         };
         while (ok && left > 0) {
-            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), shift = cur.rows(p) > kTreeRows ? 1 : 0, steps = cnt << shift;
-            ok = wait(bar(bars.q_full), q_phase);
-            q_phase ^= 1u;
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), shift = WIDE && cur.rows(p) > kTreeRows ? 1 : 0, steps = cnt << shift;
+            int q_slots[2];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                if (w > shift) break;
+                q_slots[w] = q_slot;
+                ok = ok && wait(bar(bars.q_full[q_slot]), q_phase);
+                if ((q_slot ^= 1) == 0) q_phase ^= 1u;
+            }
+            if (!ok) break;
             auto scores = [&](int i) -> bool {
                 const int w = shift ? i & 1 : 0, b = (parity + i) & 1;
                 unsigned phase;
-                const int s = place(2 * (i >> shift), phase);
+                const int s = place(tree_place_k(i >> shift, shift), phase);
                 if (!wait(full0 + 8u * s, phase)) return false;
                 tc_fence_after();
                 proxy_fence_async();
                 if (elect_one()) {
-                    const unsigned qs = q_at + unsigned(w) * TILE, ks = ring_at + unsigned(s) * TILE;
+                    const unsigned qs = q_at + unsigned(w ? q_slots[1] : q_slots[0]) * TILE, ks = ring_at + unsigned(s) * TILE;
 #pragma unroll
                     for (int pn = 0; pn < PANELS; ++pn)
 #pragma unroll
@@ -474,7 +482,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                                    umma_smem_desc(ks + pn * PANEL + k * 32, 16, 1024, 2), idesc_s, pn || k ? 1u : 0u);
                     umma_commit(bar(bars.s_full[b]));
                     if (w == shift) umma_commit(empty0 + 8u * s);
-                    if (i + 1 == steps) umma_commit(bar(bars.q_empty));
+                    if (i + shift + 1 >= steps) umma_commit(bar(bars.q_empty[w ? q_slots[1] : q_slots[0]]));
                 }
                 __syncwarp();
                 return true;
@@ -483,7 +491,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             for (int i = 0; ok && i < steps; ++i) {
                 const int w = shift ? i & 1 : 0, b = (parity + i) & 1;
                 unsigned phase;
-                const int s = place(2 * (i >> shift) + 1, phase);
+                const int s = place(tree_place_v(i >> shift, cnt, shift), phase);
                 if (!(ok = wait(full0 + 8u * s, phase))) break;
                 if (!(ok = wait(bar(bars.p_full[b]), p_phase[b]))) break;
                 p_phase[b] ^= 1u;
@@ -531,7 +539,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             return good;
         };
         while (ok && left > 0) {
-            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), shift = rows > kTreeRows ? 1 : 0, steps = cnt << shift;
+            const int cnt = int(min(int64_t(cur.span.tiles - cur.tile), left)), rows = cur.rows(p), shift = WIDE && rows > kTreeRows ? 1 : 0, steps = cnt << shift;
             const int row0 = cur.block * 2 * kTreeRows;
             // the row's mask, and how many drafts it sees
             auto load_mask = [&](int row, uint32_t (&mask)[4]) -> int {
@@ -550,9 +558,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 }
                 return drafts;
             };
-            float o0[HALF], o1[HALF], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, alpha = 1.f;
+            float o0[HALF], o1[WIDE ? HALF : 1], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, alpha = 1.f;
 #pragma unroll
-            for (int d = 0; d < HALF; ++d) o0[d] = o1[d] = 0.f;
+            for (int d = 0; d < HALF; ++d) o0[d] = 0.f;
+#pragma unroll
+            for (int d = 0; d < (WIDE ? HALF : 1); ++d) o1[d] = 0.f;
             // add F of step i to the output
             auto add = [&](float (&o)[HALF], int i, float m) -> bool {
                 const int b = (parity + i) & 1, w = shift ? i & 1 : 0;
@@ -606,16 +616,18 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                             vis[c] = drafts == 0 ? 0u : tree_visible(token0 + 64 * half + 32 * c, cur.span.cached, low, mask) & words[2 * half + c];
                     }
                     float top = -INFINITY;
-                    {
-                        uint32_t v[64];
-                        tmem_load64(s_at, v);
-                        tmem_load_wait();
-                        if (!masked) {
+                    uint32_t v[64];
+                    tmem_load64(s_at, v);
+                    tmem_load_wait();
+                    if (!masked) {
 #pragma unroll
-                            for (int e = 0; e < 64; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(v[e]) * p.scale_log2, __uint_as_float(v[e + 1]) * p.scale_log2));
-                        } else {
+                        for (int e = 0; e < 64; e += 2) top = fmaxf(top, fmaxf(__uint_as_float(v[e]) * p.scale_log2, __uint_as_float(v[e + 1]) * p.scale_log2));
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 64; ++e) top = (vis[e >> 5] >> (e & 31)) & 1 ? fmaxf(top, __uint_as_float(v[e]) * p.scale_log2) : top;
+                        for (int e = 0; e < 64; ++e) {
+                            // what is not visible has the probability zero
+                            if (!((vis[e >> 5] >> (e & 31)) & 1)) v[e] = p.scale_log2 < 0.f ? 0x7f800000u : 0xff800000u;
+                            top = fmaxf(top, __uint_as_float(v[e]) * p.scale_log2);
                         }
                     }
                     tops[i & 1][half][r] = top;
@@ -624,17 +636,17 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                     const float m = w ? m1 : m0, now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
                     next_alpha = m == now ? 1.f : ex2(m - now);
                     float sum[2] = {0.f, 0.f};
-                    // 16 tokens: S -> P in two parts, in the place of S; the next 16 are on their way meanwhile
-                    auto probabilities = [&](const uint32_t (&v)[16], int c, uint32_t seen, bool all) {
+                    // 16 tokens: S -> P in two parts, in the place of S
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
                         uint32_t out[16];
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) {
                             float x[2];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                x[h] = ex2(fmaf(__uint_as_float(v[e + h]), p.scale_log2, -base));
+                                x[h] = ex2(fmaf(__uint_as_float(v[16 * c + e + h]), p.scale_log2, -base));
                                 if (AttentionBias<T>::factor != 1.f) x[h] *= AttentionBias<T>::factor;
-                                if (!all) x[h] = (seen >> (e + h)) & 1 ? x[h] : 0.f;
                             }
                             sum[0] += x[0];
                             sum[1] += x[1];
@@ -645,29 +657,6 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                             out[8 + e / 2] = pack2(x[0] - a, x[1] - c2, T());
                         }
                         tmem_store16u(s_at + 16u * c, out);
-                    };
-                    uint32_t va[16], vb[16];
-                    tmem_load16(s_at, va);
-                    tmem_load_wait();
-                    if (!masked) {
-#pragma unroll
-                        for (int c = 0; c < 4; c += 2) {
-                            tmem_load16(s_at + 16u * (c + 1), vb);
-                            probabilities(va, c, 0, true);
-                            tmem_load_wait();
-                            if (c < 2) tmem_load16(s_at + 16u * (c + 2), va);
-                            probabilities(vb, c + 1, 0, true);
-                            if (c < 2) tmem_load_wait();
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            if (c > 0) {
-                                tmem_load16(s_at + 16u * c, va);
-                                tmem_load_wait();
-                            }
-                            probabilities(va, c, (c < 2 ? vis[0] : vis[1]) >> (16 * (c & 1)), false);
-                        }
                     }
                     tmem_store_wait();
                     const float l = (w ? l1 : l0) * next_alpha + (sum[0] + sum[1]);
@@ -675,11 +664,17 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 }
                 tc_fence_before();
                 mbar_arrive(bar(bars.p_full[b]));
-                if (i > 0 && !(ok = (shift && w == 0) ? add(o1, i - 1, m1) : add(o0, i - 1, m0))) break;
+                if (i > 0) {
+                    if constexpr (WIDE) ok = (shift && w == 0) ? add(o1, i - 1, m1) : add(o0, i - 1, m0);
+                    else ok = add(o0, i - 1, m0);
+                    if (!ok) break;
+                }
                 alpha = next_alpha;
             }
             if (!ok) break;
-            if (!(ok = shift ? add(o1, steps - 1, m1) : add(o0, steps - 1, m0))) break;
+            if constexpr (WIDE) ok = shift ? add(o1, steps - 1, m1) : add(o0, steps - 1, m0);
+            else ok = add(o0, steps - 1, m0);
+            if (!ok) break;
             parity = (parity + steps) & 1;
             const bool whole = cur.tile == 0 && cnt == cur.span.tiles;
             // the two warps' sums
@@ -714,7 +709,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 return true;
             };
             if (!(ok = finish(o0, m0, l0, 0))) break;
-            if (shift && !(ok = finish(o1, m1, l1, 1))) break;
+            if constexpr (WIDE)
+                if (shift && !(ok = finish(o1, m1, l1, 1))) break;
             if (!whole) parts[cur.tile == 0 ? 1 : 0] = cur.seq * head_blocks + cur.hb;
             info = (info + cnt) % kTreeInfos;
             left -= cnt;

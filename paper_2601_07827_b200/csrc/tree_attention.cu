@@ -46,6 +46,7 @@ bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
 bool umma_fits(const btc_tree_attention_s &op)
 {
     if (op.q.dtype == BTC_F32 || op.dp > 128) return false;
+    if (float(op.scale * kLog2E) == 0.f) return false;      // -inf for what is not visible would not survive the product
     for (const TensorDesc *t : {&op.k, &op.v}) {
         if (!rows_allow_vectors(*t, 8) || t->stride[0] < 0 || t->stride[1] < 0) return false;
         if (__int128(t->stride[0] / 8) * (t->extent[0] - 1) + __int128(t->stride[1] / 8) * (t->extent[1] - 1) >= int64_t(UINT32_MAX)) return false;

@@ -121,6 +121,14 @@ def test_trees(api, handle, case, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("scale", [0.0, -0.11, 1.5])
+def test_scales(api, handle, dtype, scale):
+    p = Problem(2, 11, 8, 2, 64, 64, 16, [200, 30], dtype, seed=12).gpu()
+    o, lse, _ = run(api, handle, p, scale=scale, window=50)
+    compare(p, o, lse, 50, scale)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_masks_of_any_kind(api, handle, dtype):
     """Rows that see nothing, only others, everything; a sequence without drafts; bits beyond the last draft."""
     n, t = 3, 37

@@ -25,7 +25,7 @@ struct btc_linear4_s {
 namespace {
 
 constexpr int64_t kMaxExtent = int64_t(1) << 24;           // of k, n and tokens: indices and counts stay in 32 bits
-constexpr int64_t kStagedBytes = 64 * 1024;                // of x at a time
+constexpr int64_t kStagedBytes = 64 * 1024;                // of x at a time: more leaves one CTA to an SM
 
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : (t == BTC_E4M3 ? 1 : 2); }
 int parts_of(const btc_linear4_s &op) { return op.x.dtype == BTC_F32 ? 3 : 1; }
@@ -35,17 +35,34 @@ int32_t log2_of(int32_t group) { return group == 0 ? 31 : 31 - __builtin_clz(uns
 // k per scale within a stretch, as a power of two
 int32_t stretch_group_log2(const btc_linear4_s &op) { return std::min(log2_of(op.group), log2_of(kL4Stretch * kL4K)); }
 
+// How rows and k are spread over CTAs (8 warps = 8 / wk row blocks x wk shares of k; `ranks` CTAs of a cluster split k once more).
+// Measured with weights from HBM, bf16, (wk, ranks), row blocks x stretches; best in brackets:
+//   1 token    384 x 16: (4, 1) 7.7 us [7.7], 256 x 56: (4, 2) 13.2 [12.4], 896 x 16: (1, 1) 20.2 [20.2], 1792 x 32: (1, 2) 62 [62], 128 x 8: (8, 1) 3.4 [3.4]
+//   8 tokens   384 x 16: (1, 4) 9.1 [9.1], 256 x 56: (2, 4) 14.5 [14.5], 896 x 16: (1, 1) 22.9 [22.9], 1792 x 32: (1, 2) 71 [71], 128 x 8: (8, 1) 4.5 [4.5]
+//   32 tokens  384 x 16: (1, 4) 19.8 [19.8], 256 x 56: (1, 8) 28.0 [28.0], 896 x 16: (1, 2) 56.7 [52.0], 1792 x 32: (1, 2) 176 [175], 64 x 4: (8, 2) 7.3 [7.2]
 void plan(btc_linear4_s &op)
 {
     const int64_t tokens = op.x.extent[0], sms = op.handle.sm_count;
-    op.nt = tokens <= 8 ? 1 : 2;
+    // more than 8 tokens, and more than 16, take wider products, so that a code becomes a number once for them (fp32 with its
+    // three parts up to 16)
+    op.nt = tokens <= 8 ? 1 : (tokens <= 16 || op.x.dtype == BTC_F32 ? 2 : 4);
+    const int64_t block = int64_t(op.nt) * parts_of(op) * 1024 * kL4Stretch;      // x of a stretch in shared memory
+    // splits of k: until there is a CTA for each SM (with short k for most of them)
+    const int64_t enough = op.stretches <= 16 ? sms * 7 / 10 : sms;
+    int64_t splits = 1;
+    while (op.row_blocks * splits / kL4Warps < enough && splits < op.stretches && splits < 64) splits *= 2;
+    // over a cluster's CTAs as far as that keeps the x that each of them brings small, the rest over warps
+    const int64_t most = tokens > 16 ? 8 : 4, x_bytes = std::min<int64_t>(tokens, 8 * op.nt) * op.x.extent[1] * int64_t(esize(op.x.dtype) == 4 ? 4 : 2);
     op.ranks = 1;
-    op.wk = 1;
-    while (op.wk < kL4Warps && op.row_blocks * op.wk / kL4Warps < 2 * sms && op.wk < op.stretches) op.wk *= 2;
+    if (splits == 1) {
+        if (op.stretches * block > kStagedBytes) op.ranks = 2;
+    } else {
+        while (op.ranks < most && op.ranks < splits && (x_bytes / op.ranks > 32 * 1024 || splits / op.ranks > kL4Warps)) op.ranks *= 2;
+    }
+    op.wk = int32_t(std::min<int64_t>(kL4Warps, std::max<int64_t>(1, splits / op.ranks)));
+    while (op.wk * block > kStagedBytes && op.wk > 1) op.wk /= 2;
     op.slice = int32_t((op.stretches + op.ranks - 1) / op.ranks);
-    const int64_t block = int64_t(op.nt) * parts_of(op) * 1024 * kL4Stretch, cap = kStagedBytes;
-    while (op.wk * block > cap && op.wk > 1) op.wk /= 2;
-    op.chunk = int32_t(std::min(round_up(op.slice, op.wk), std::max<int64_t>(op.wk, cap / block / op.wk * op.wk)));
+    op.chunk = int32_t(std::min(round_up(op.slice, op.wk), std::max<int64_t>(op.wk, kStagedBytes / block / op.wk * op.wk)));
     op.staged = size_t(op.chunk * block);
     op.shared = std::max(op.staged + size_t(kL4Warps) * kL4Stages * size_t(op.stretch_bytes), size_t(kL4Warps) * 8 * size_t(op.nt) * kL4Rows * 4);
 }
@@ -89,8 +106,10 @@ template <typename CODES, int PARTS, int NT, bool SHORT> btc_error_t launch_scal
 }
 template <typename CODES, int PARTS> btc_error_t launch_typed(const btc_linear4_s &op, const Linear4Params &p, dim3 blocks, cudaStream_t st)
 {
-    if (op.group == 32 || op.x_group == 32)
-        return op.nt == 1 ? launch_scaled<CODES, PARTS, 1, true>(op, p, blocks, st) : launch_scaled<CODES, PARTS, 2, true>(op, p, blocks, st);
+    const bool narrow = op.group == 32 || op.x_group == 32;
+    if constexpr (PARTS == 1)
+        if (op.nt == 4) return narrow ? launch_scaled<CODES, PARTS, 4, true>(op, p, blocks, st) : launch_scaled<CODES, PARTS, 4, false>(op, p, blocks, st);
+    if (narrow) return op.nt == 1 ? launch_scaled<CODES, PARTS, 1, true>(op, p, blocks, st) : launch_scaled<CODES, PARTS, 2, true>(op, p, blocks, st);
     return op.nt == 1 ? launch_scaled<CODES, PARTS, 1, false>(op, p, blocks, st) : launch_scaled<CODES, PARTS, 2, false>(op, p, blocks, st);
 }
 

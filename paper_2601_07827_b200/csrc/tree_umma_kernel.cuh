@@ -759,6 +759,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         }
     }
     tc_fence_before();
+    // after a wait gave up bulk copies may still be on their way; they land within a few microseconds
+    if (*abort_flag && warp >= 8 && warp < 11) __nanosleep(20000);
     __syncthreads();
     if (warp == 11) {
         if (*abort_flag) {

@@ -576,7 +576,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             for (int d = 0; d < HALF; ++d) o0[d] = 0.f;
 #pragma unroll
             for (int d = 0; d < (WIDE ? HALF : 1); ++d) o1[d] = 0.f;
-            // add F of step i to the output
+            // add F of step i, whose exponentials were taken against the maximum m, to the output
             auto add = [&](float (&o)[HALF], int i, float m) -> bool {
                 const int b = (parity + i) & 1, w = shift ? i & 1 : 0;
                 if (!wait(bar(bars.f_full[b]), f_phase[b])) return false;
@@ -616,6 +616,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 s_phase[b] ^= 1u;
                 tc_fence_after();
                 float next_alpha = 1.f;
+                // the maximum of the step before, whose F is added below: this step's softmax moves that of its rows on
+                const float before = WIDE && shift && w == 0 ? m1 : m0;
                 if (__any_sync(0xffffffffu, row < rows)) {
                     const uint32_t *words = infos[(info + j) % kTreeInfos];
                     const bool masked = (words[0] & words[1] & words[2] & words[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
@@ -688,8 +690,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 tc_fence_before();
                 mbar_arrive(bar(bars.p_full[b]));
                 if (i > 0) {
-                    if constexpr (WIDE) ok = (shift && w == 0) ? add(o1, i - 1, m1) : add(o0, i - 1, m0);
-                    else ok = add(o0, i - 1, m0);
+                    if constexpr (WIDE) ok = (shift && w == 0) ? add(o1, i - 1, before) : add(o0, i - 1, before);
+                    else ok = add(o0, i - 1, before);
                     if (!ok) break;
                 }
                 alpha = next_alpha;

@@ -137,9 +137,16 @@ __device__ __forceinline__ uint32_t tree_visible(int first, int cached, int low,
     return v;
 }
 
+// May rows differ in what they see of the tile that begins at token0?  At its drafts, and at the window's edge, where rows that see
+// more drafts begin later.
+__device__ __forceinline__ bool tree_differs(const AttentionParams &p, int token0, int cached)
+{
+    return token0 + kTreeTok > cached || (p.window > 0 && token0 < cached + p.drafts - p.window);
+}
+
 // Elements d0 .. d0 + COUNT - 1 of F for one row and tile by plain products over what the row sees.  A value that is infinite or NaN makes
-// the tensor core's F NaN in every row, its probability of zero included; in a tree such a draft may be invisible to
-// this row and visible to the next, so tiles with drafts whose F is not finite are computed again here.
+// the tensor core's F NaN in every row, its probability of zero included; where rows differ in what they see such a token may be invisible
+// to this row and visible to the next, so those tiles are computed again here when their F is not finite.
 template <typename T, int COUNT>
 __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const TreeCursor &cur, const uint32_t *seen, int token0, int low,
                                                uint32_t m0, uint32_t m1, uint32_t m2, uint32_t m3, int group_row, float base, int d0, float *out)
@@ -589,7 +596,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 if constexpr (HALF == 64) tmem_load64(f_at, v); else tmem_load32(f_at, v);
                 tmem_load_wait();
                 const int j = i >> shift, token0 = (cur.span.first_tile + cur.tile + j) * kTreeTok;
-                if (token0 + kTreeTok > cur.span.cached) {
+                if (tree_differs(p, token0, cur.span.cached)) {
                     bool odd = false;
 #pragma unroll
                     for (int e = 0; e < HALF; ++e) odd |= (v[e] & 0x7f800000u) == 0x7f800000u;
@@ -620,8 +627,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 const float before = WIDE && shift && w == 0 ? m1 : m0;
                 if (__any_sync(0xffffffffu, row < rows)) {
                     const uint32_t *words = infos[(info + j) % kTreeInfos];
-                    const bool masked = (words[0] & words[1] & words[2] & words[3]) != ~0u || token0 + kTreeTok > cur.span.cached ||
-                                        (p.window > 0 && token0 < cur.span.cached + p.drafts - p.window);
+                    const bool masked = (words[0] & words[1] & words[2] & words[3]) != ~0u || tree_differs(p, token0, cur.span.cached);
                     uint32_t vis[2] = {~0u, ~0u};
                     if (masked) {
                         uint32_t mask[4];

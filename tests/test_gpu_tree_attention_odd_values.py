@@ -94,3 +94,34 @@ def test_draft_in_a_tile_before_the_last(api, handle, case, dtype):
     p.gpu()
     o, lse, _ = run(api, handle, p)
     compare(p, clean, hit, o, lse)
+
+
+EDGE = [
+    # t, hq, hk, d, page, cached tokens of every second sequence, window (its edge lies in tiles without drafts)
+    (48, 4, 2, 64, 16, [400, 389], 140),
+    (64, 8, 2, 128, 16, [400, 700], 160),
+    (33, 3, 3, 128, 20, [300, 1111], 100),
+    (80, 8, 2, 64, 64, [1000, 530], 300),
+    (4, 8, 2, 64, 16, [400, 389], 140),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("chain", [True, False])
+@pytest.mark.parametrize("case", EDGE, ids=[str(i) for i in range(len(EDGE))])
+def test_cached_tokens_at_the_windows_edge(api, handle, case, chain, dtype):
+    """Rows that see more drafts begin later in the cache.  A chain: tokens that only its first rows see.  Rows that see every draft: tokens
+    at the edge that nobody sees."""
+    t, hq, hk, d, page, lengths, window = case
+    lengths = lengths * 20
+    sees = torch.ones(len(lengths), t, t, dtype=torch.bool)
+    p = Problem(len(lengths), t, hq, hk, d, d, page, lengths, dtype, seed=t + d, sees=sees.tril() if chain else sees)
+    odd = []
+    for n, length in enumerate(lengths):
+        first = length + 1 - window                      # what a row that sees one draft begins with
+        odd += [(n, first, 0, 0, d, math.nan), (n, first + 2, hk - 1, 3, d // 2, math.inf), (n, first + min(t, 6) - 2, 0, d // 2, d, -math.inf)]
+    clean, hit = spoil(p, odd, window)
+    assert hit.any() == chain
+    p.gpu()
+    o, lse, _ = run(api, handle, p, window=window)
+    compare(p, clean, hit, o, lse, window)

@@ -527,7 +527,8 @@ btc_error_t btc_add_norm_backward(btc_add_norm_t op, void *cuda_stream, const vo
  *   codes   DEVICE [rows, ceil(K / 2)] bytes, dense: k even in the lower four bits, k odd in the upper
  *   scales  DEVICE [rows, ceil(K / group)] of scale_type (F32, F16, BF16), dense
  *   zeros   DEVICE bytes [rows, ceil(K / group)], dense, or NULL as the operation was created
- * Weights enter the products unrounded, sums are fp32.  Infinite values of X give infinities or NaN.  The result does not depend on
+ * Weights enter the products unrounded, sums are fp32, of up to 64 products with whole numbers before their scale is applied: X may be up
+ * to 2^117 in modulus, whatever the scales.  Larger values, like infinite ones, may give infinities or NaN.  The result does not depend on
  * scheduling.  btc_linear4_workspace_size is the workspace of btc_linear4_execute (NULL is allowed where it is 0).
  * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA. */
 typedef struct btc_linear4_s *btc_linear4_t;

@@ -4,7 +4,8 @@
 //
 // Every code is read once: 2 T multiply-adds per half byte, bound by HBM for a few tokens.  The codes become f16 or
 // bf16 numbers (whole numbers of at most 15: exact), the tensor core adds up at most 64 products in fp32, and each
-// such sum is multiplied by its group's scale in fp32, so that no weight is rounded.
+// such sum is multiplied by its group's scale in fp32, so that no weight is rounded.  64 products with 15 fit fp32 as long as x is at
+// most 2^117.
 //
 // Layout ("packed"): stretches of 16 weight rows x 256 k, one after the other along k.  A stretch is its groups' scales
 // [group][8][2] (rows g and g + 8), its zeros likewise in bytes, and four blocks of 64 k, 512 bytes each: 16 bytes for each

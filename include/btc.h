@@ -343,7 +343,7 @@ enum {
     BTC_FLAG_BAD_SEQUENCE = 4,  /* a sequence number outside the table                               */
     BTC_FLAG_BAD_LENGTH = 8,    /* a length or token count that is negative or beyond the table row  */
     BTC_FLAG_POOL_EXHAUSTED = 16, /* fewer free pages than asked for                                 */
-    BTC_FLAG_TIMEOUT = 32       /* a bounded wait inside a kernel ran out: the outputs are incomplete */
+    BTC_FLAG_TIMEOUT = 32       /* a bounded wait inside a kernel ran out: output rows it could not complete are NaN */
 };
 
 /* Head norm and rotary positions of queries and keys, keys and values written into cache pages in the
@@ -431,6 +431,8 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
  *   Q [N, T, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, T, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
  *   D and Dv up to 256; T up to 128; table [N, M] I32; masks [N, T, ceil(T / 32)] I32.  lengths: DEVICE int32[N]; lse: DEVICE
  *   float[N * T * Hq] or NULL.
+ * Should a bounded wait inside a kernel run out, the rows of O and lse that it could not complete are NaN, with flags or without.
+ * btc_tree_attention_set_attr: key BTC_ATTR_POLL_LIMIT only (see there), read by later executes.
  * Errors: INVALID_ARGUMENT, EXTENT_MISMATCH, D_ALIASING, NOT_SUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, OUT_OF_MEMORY, CUDA. */
 typedef struct btc_tree_attention_s *btc_tree_attention_t;
 btc_error_t btc_create_tree_attention(btc_handle_t handle, btc_tensor_info_t Q, btc_tensor_info_t K, btc_tensor_info_t V,
@@ -438,6 +440,7 @@ btc_error_t btc_create_tree_attention(btc_handle_t handle, btc_tensor_info_t Q, 
                                       int32_t window, btc_tree_attention_t *out);
 btc_error_t btc_destroy_tree_attention(btc_tree_attention_t *op);
 btc_error_t btc_tree_attention_workspace_size(btc_tree_attention_t op, size_t *bytes);
+btc_error_t btc_tree_attention_set_attr(btc_tree_attention_t op, int32_t key, const void *value, size_t len);
 btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_stream, const void *Q, const void *K, const void *V,
                                        const int32_t *table, const int32_t *lengths, const int32_t *masks, void *O, float *lse,
                                        void *workspace, size_t workspace_bytes, int32_t *flags);

@@ -70,7 +70,8 @@ EXPORTED = [
     "btc_add_norm_backward",
     "btc_create_linear4", "btc_destroy_linear4", "btc_linear4_workspace_size", "btc_linear4_packed_size", "btc_linear4_pack",
     "btc_linear4_execute",
-    "btc_create_tree_attention", "btc_destroy_tree_attention", "btc_tree_attention_workspace_size", "btc_tree_attention_execute",
+    "btc_create_tree_attention", "btc_destroy_tree_attention", "btc_tree_attention_workspace_size", "btc_tree_attention_set_attr",
+    "btc_tree_attention_execute",
 ]
 
 _vp = ctypes.c_void_p
@@ -136,6 +137,7 @@ _lib.btc_linear4_execute.argtypes = [_vp] * 7 + [ctypes.c_size_t]
 _lib.btc_create_tree_attention.argtypes = [_vp] * 7 + [ctypes.c_double, _i32, ctypes.POINTER(_vp)]
 _lib.btc_destroy_tree_attention.argtypes = [ctypes.POINTER(_vp)]
 _lib.btc_tree_attention_workspace_size.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.btc_tree_attention_set_attr.argtypes = [_vp, _i32, _vp, ctypes.c_size_t]
 _lib.btc_tree_attention_execute.argtypes = [_vp] * 11 + [ctypes.c_size_t, _vp]
 for _name in EXPORTED:
     getattr(_lib, _name).restype = ctypes.c_int
@@ -570,6 +572,11 @@ class TreeAttention(_Operation):
             scale = float(Q.extents[-1]) ** -0.5 if Q.extents else 1.0
         _check(_lib.btc_create_tree_attention(handle._h, Q._t, K._t, V._t, table._t, masks._t, O._t, scale, window,
                                               ctypes.byref(self._op)), "btc_create_tree_attention")
+
+    def set_attr(self, key: int, value: int) -> None:
+        """ATTR_POLL_LIMIT: polls after which a wait inside the kernel gives up."""
+        v = ctypes.c_int32(value)
+        _check(_lib.btc_tree_attention_set_attr(self._op, key, ctypes.byref(v), 4), "btc_tree_attention_set_attr")
 
     def execute(self, stream: int, Q: int, K: int, V: int, table: int, lengths: int, masks: int, O: int, lse: int = 0,
                 workspace: int = 0, workspace_bytes: int = 0, flags: int = 0) -> None:

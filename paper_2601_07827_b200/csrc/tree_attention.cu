@@ -18,6 +18,7 @@ struct btc_tree_attention_s {
     int32_t window = 0;
     int32_t dp = 64, nt = 1;       // padded head size, blocks of 8 rows per item
     int64_t blocks = 1;            // items per key head
+    uint32_t poll_limit = kWaitPollLimit;
 };
 
 namespace {
@@ -243,6 +244,16 @@ btc_error_t btc_tree_attention_workspace_size(btc_tree_attention_t op, size_t *b
     return BTC_SUCCESS;
 }
 
+btc_error_t btc_tree_attention_set_attr(btc_tree_attention_t op, int32_t key, const void *value, size_t len)
+{
+    if (!op || !value || len != sizeof(int32_t) || key != BTC_ATTR_POLL_LIMIT) return BTC_ERR_INVALID_ARGUMENT;
+    int32_t v;
+    std::memcpy(&v, value, sizeof v);
+    if (v < 0) return BTC_ERR_INVALID_ARGUMENT;
+    op->poll_limit = uint32_t(v);
+    return BTC_SUCCESS;
+}
+
 btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_stream, const void *Q, const void *K, const void *V,
                                        const int32_t *table, const int32_t *lengths, const int32_t *masks, void *O, float *lse,
                                        void *workspace, size_t workspace_bytes, int32_t *flags)
@@ -296,6 +307,7 @@ btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_strea
         std::memset(static_cast<void *>(&tp), 0, sizeof tp);
         p.blocks = (p.group + 2 * kTreeRows - 1) / (2 * kTreeRows);
         tp.a = p;
+        tp.poll_limit = op->poll_limit;
         tp.partial = static_cast<float *>(workspace);
         tp.partial_item = reinterpret_cast<int32_t *>(tp.partial + ctas * 4 * umma_part_floats(*op));
         tp.k_page16 = uint32_t(p.k_page / 8); tp.k_slot16 = uint32_t(p.k_slot / 8);

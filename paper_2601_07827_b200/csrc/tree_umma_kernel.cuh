@@ -19,7 +19,8 @@
 //
 // Work: the list of (sequence, key head, block of rows) items in tiles is cut into equal contiguous shares, one per CTA, found on the
 // device from the lengths; what a CTA does not hold whole goes to the workspace and a second kernel joins it, in a fixed order.
-// Every wait is bounded; one that gives up ends the kernel and reports BTC_FLAG_TIMEOUT.
+// Every wait is bounded.  One that gives up ends the CTA, after its copies and products in flight; the rows of the items it had in hand become NaN, so that
+// nobody takes an incomplete result for a whole one, and BTC_FLAG_TIMEOUT reports it.
 //
 // Measured (replayed graphs, heads of 128): 32 requests of 64 to 8192 tokens, 128 rows: 102 us (240 MB), 256 rows: 194 us; 4 x 64 Ki tokens, 32
 // rows: 241 us (1.07 GB: 4.5 TB/s), 512 rows 1.07 ms (510 TFLOP/s of the two products).  What bounds it is the chain of a step in the softmax
@@ -55,7 +56,9 @@ struct TreeParams {
     // bulk tensor copies: rows of a box of keys and values (they divide the page), drafts of a box of queries; 0: 16-byte copies
     int32_t box_kv, box_q;
     uint32_t k_page16, k_slot16, v_page16, v_slot16;       // strides of the cache in 16 bytes
+    uint32_t poll_limit;                     // polls after which a wait gives up
 };
+constexpr int32_t kTreeLost = -2;            // in partial_item: a wait of this CTA gave up (-1: no such part)
 
 // visible range of a sequence in tiles of 128 tokens
 struct TreeSpan {
@@ -171,6 +174,25 @@ __device__ __noinline__ void tree_plain_values(const AttentionParams &p, const T
     }
 }
 
+// A wait gave up: NaN into all rows of the items of this CTA's share (256 threads; the joining kernel leaves what it has lost parts of NaN, too).
+template <typename T> __device__ __noinline__ void tree_spoil(const TreeParams &tp, TreeCursor cur, int64_t left)
+{
+    const AttentionParams &p = tp.a;
+    while (left > 0) {
+        const int rows = cur.rows(p), row0 = cur.block * 2 * kTreeRows;
+        for (int e = threadIdx.x; e < rows * p.dim_v; e += 256) {
+            const int r = e / p.dim_v, d = e - r * p.dim_v;
+            int32_t draft;
+            const int64_t head = attention_row<true>(p, cur.key_head, row0 + r, draft);
+            static_cast<T *>(p.o)[cur.seq * p.o_n + draft * p.o_t + head * p.o_h + d * p.o_d] = from_f32<T>(NAN);
+            if (d == 0 && p.lse) p.lse[(int64_t(cur.seq) * p.drafts + draft) * p.heads + head] = NAN;
+        }
+        left -= min(int64_t(cur.span.tiles - cur.tile), left);
+        cur.next(p);
+    }
+    if (threadIdx.x == 0) tp.partial_item[2 * blockIdx.x] = tp.partial_item[2 * blockIdx.x + 1] = kTreeLost;
+}
+
 // elements d0 .. d0 + N - 1 of an output row
 template <typename T, int N>
 __device__ __forceinline__ void tree_write(T *dst, int d0, int dim, int64_t stride, bool vec, const float (&o)[N], float scale, bool nothing)
@@ -208,6 +230,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     __shared__ int64_t share;
     __shared__ uint32_t infos[kTreeInfos][4];
     __shared__ float tops[2][2][kTreeRows];                     // [step's parity][half][row]
+    __shared__ uint32_t filled[10];                             // 1 + phase of the last copies into a place of the ring (0..7) and of queries (8, 9); 0: none
     volatile int *abort_flag = &abort_word;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int64_t *scan = reinterpret_cast<int64_t *>(raw_smem);      // until the shares are known
@@ -216,7 +239,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
     auto bar = [&](const uint64_t &b) { return unsigned(__cvta_generic_to_shared(&b)); };
     const int head_blocks = p.key_heads * p.blocks;
     // the same answer in all lanes: what follows are instructions of whole warps
-    auto wait = [&](unsigned b, unsigned phase) -> bool { return __all_sync(0xffffffffu, mbar_wait_bounded(b, phase, abort_flag, nullptr, 0)); };
+    auto wait = [&](unsigned b, unsigned phase) -> bool { return __all_sync(0xffffffffu, mbar_wait_bounded(b, phase, abort_flag, nullptr, 0, tp.poll_limit)); };
 
     if (tid == 0) {
         for (int i = 0; i < SLOTS; ++i) { mbar_init(bar(bars.full[i]), 32); mbar_init(bar(bars.empty[i]), 1); }
@@ -224,6 +247,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         for (int i = 0; i < 4; ++i) mbar_init(bar(bars.pair[i]), 64);
         mbar_init(bar(bars.drain), 1);
         abort_word = 0;
+        for (int i = 0; i < 10; ++i) filled[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 11) {
@@ -331,6 +355,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 const unsigned full = bar(bars.q_full[q_slot]), to = q_at + unsigned(q_slot) * TILE;
                 if (lw == 0) {
                     if (!(ok = wait(bar(bars.q_empty[q_slot]), q_phase ^ 1u))) break;
+                    if (lane == 0) filled[8 + q_slot] = 1 + q_phase;
                     if (tp.box_q) {
                         // a box: the heads that share a key head x some drafts, in the order of the rows (zeros behind the last draft)
                         if (elect_one()) {
@@ -400,6 +425,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                     }
                 }
                 if (!(ok = wait(bar(bars.empty[here]), here_phase ^ 1u))) break;
+                if (lane == 0) filled[here] = 1 + here_phase;
                 if (kv == 0) {
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
@@ -767,9 +793,15 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         }
     }
     tc_fence_before();
-    // after a wait gave up bulk copies may still be on their way; they land within a few microseconds
-    if (*abort_flag && warp >= 8 && warp < 11) __nanosleep(20000);
     __syncthreads();
+    if (rare(*abort_flag)) {
+        if (warp < 8) tree_spoil<T>(tp, start, share);
+        // copies that nobody waited for have to land before the CTA gives up its shared memory: the last ones into each place
+        if (warp == 8 && lane < 10 && filled[lane] != 0) {
+            const unsigned b = lane < 8 ? bar(bars.full[lane]) : bar(bars.q_full[lane - 8]);
+            for (unsigned n = 0; n < (1u << 16) && !mbar_try_wait(b, filled[lane] - 1); ++n) { }
+        }
+    }
     if (warp == 11) {
         if (*abort_flag) {
             if (elect_one()) umma_commit(bar(bars.drain));
@@ -790,7 +822,7 @@ __global__ void __launch_bounds__(kTreeJoinThreads) tree_join_kernel(const __gri
 {
     constexpr int GROUPS = kTreeJoinThreads / kTreeJoinRows, EACH = DP / GROUPS, AHEAD = 4;
     const AttentionParams &p = tp.a;
-    __shared__ int32_t parts;
+    __shared__ int32_t parts, lost_at;
     __shared__ float all_tops[GROUPS][kTreeJoinRows], all_sums[GROUPS][kTreeJoinRows];
     const int c = blockIdx.x, tid = threadIdx.x, group = tid / kTreeJoinRows;
     early_begin();
@@ -798,13 +830,18 @@ __global__ void __launch_bounds__(kTreeJoinThreads) tree_join_kernel(const __gri
     if (item < 0) return;
     const int left = ctas - c;
     const int32_t other = tid + 1 < left ? load_now(tp.partial_item + 2 * (c + tid + 1)) : -1;
-    if (tid == 0) parts = left;
+    if (tid == 0) { parts = left; lost_at = INT32_MAX; }
     __syncthreads();
-    if (tid + 1 < left && other != item) atomicMin(&parts, tid + 1);
-    for (int i = tid + 1 + kTreeJoinThreads; i < left; i += kTreeJoinThreads)
-        if (tp.partial_item[2 * (c + i)] != item) atomicMin(&parts, i);
+    auto ends = [&](int i, int32_t here) {                      // does the item end before CTA c + i?
+        if (here == item) return;
+        atomicMin(&parts, i);
+        if (here == kTreeLost) atomicMin(&lost_at, i);
+    };
+    if (tid + 1 < left) ends(tid + 1, other);
+    for (int i = tid + 1 + kTreeJoinThreads; i < left; i += kTreeJoinThreads) ends(i, tp.partial_item[2 * (c + i)]);
     __syncthreads();
     const int n = parts;
+    const bool lost = lost_at == n;                             // by a CTA in which a wait gave up, and which may have held a part
     const int head_blocks = p.key_heads * p.blocks;
     const int seq = item / head_blocks, hb = item - seq * head_blocks, kh = hb / p.blocks, block = hb - kh * p.blocks;
     const int row = blockIdx.y * kTreeJoinRows + tid % kTreeJoinRows, group_row = block * 2 * kTreeRows + row;
@@ -826,6 +863,7 @@ __global__ void __launch_bounds__(kTreeJoinThreads) tree_join_kernel(const __gri
     for (int i = 0; i < GROUPS; ++i) top = fmaxf(top, all_tops[i][tid % kTreeJoinRows]);
     l = 0.f;
     for (int i = 0; i < GROUPS; ++i) l = fmaf(all_sums[i][tid % kTreeJoinRows], join_weight(all_tops[i][tid % kTreeJoinRows], top), l);
+    if (rare(lost)) l = NAN;
     float o[EACH];
 #pragma unroll
     for (int d = 0; d < EACH; ++d) o[d] = 0.f;

@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
         for (int w = 0; w < warp; ++w) before += scan[(w + 1) * 32];
         __syncthreads();
         scan[tid + 1] = x + before;
+        proxy_fence_async();                                    // bulk copies will write where these sums lie
         __syncthreads();
     }
     const unsigned tmem = *reinterpret_cast<volatile uint32_t *>(&tmem_base_word);

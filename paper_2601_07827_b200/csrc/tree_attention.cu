@@ -25,6 +25,9 @@ namespace {
 
 constexpr double kLog2E = 1.4426950408889634;
 constexpr int64_t kMaxDrafts = 128;
+// Tokens of a table row that count: the kernels form a length and the drafts behind it, and the end of a tile, in 32 bits.
+constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 256;
+static_assert(kMaxTokens % kTreeTok == 0 && kMaxTokens + kMaxDrafts <= INT32_MAX, "");
 
 size_t esize(btc_dtype_t t) { return t == BTC_F32 ? 4 : 2; }
 
@@ -221,7 +224,7 @@ btc_error_t btc_create_tree_attention(btc_handle_t handle, btc_tensor_info_t Q, 
         op.blocks = (rows + 8 * op.nt - 1) / (8 * op.nt);
         if (__int128(n) * key_heads * op.blocks > INT32_MAX) return BTC_ERR_NOT_SUPPORTED;
         // tiles of all sequences: 38 bits of the kernel's prefix sum
-        if (__int128(n) * (std::min<int64_t>(t.extent[1] * k.extent[1], INT32_MAX) / kAttnTok + 1) >= (__int128(1) << 38)) return BTC_ERR_NOT_SUPPORTED;
+        if (__int128(n) * (std::min(t.extent[1] * k.extent[1], kMaxTokens) / kAttnTok + 1) >= (__int128(1) << 38)) return BTC_ERR_NOT_SUPPORTED;
         btc_tree_attention_s *kept = new (std::nothrow) btc_tree_attention_s(std::move(op));
         if (!kept) return BTC_ERR_OUT_OF_MEMORY;
         *out = kept;
@@ -294,7 +297,7 @@ btc_error_t btc_tree_attention_execute(btc_tree_attention_t op, void *cuda_strea
     p.columns = int32_t(op->table.extent[1]);
     p.window = op->window;
     p.page.set(op->k.extent[1]);
-    p.room = int32_t(std::min<int64_t>(op->table.extent[1] * op->k.extent[1], 0x7ffffff0));
+    p.room = int32_t(std::min(op->table.extent[1] * op->k.extent[1], kMaxTokens));
     const int64_t vec = int64_t(16 / es);
     p.vec_k = rows_allow_vectors(op->k, vec) && aligned_to(K, 16);
     p.vec_v = rows_allow_vectors(op->v, vec) && aligned_to(V, 16);

@@ -427,7 +427,8 @@ btc_error_t btc_paged_attention_execute(btc_paged_attention_t op, void *cuda_str
  * positions lengths[n] + (number of drafts the row sees) - window and later.  A row whose mask is empty is no draft: it sees nothing,
  * and gets O = 0 and lse = -inf, as does a row whose scores are all -inf.  Drafts beyond the table row's capacity are not visible
  * (BTC_FLAG_BAD_LENGTH; of a table row 2^31 - 256 tokens count at most); other bad lengths, pages that do not exist and what lies in
- * invisible places are treated as in btc_paged_attention_execute, and so are types, sums and infinities.
+ * invisible places are treated as in btc_paged_attention_execute, and so are types, sums and infinities.  Drafts that no row sees need
+ * neither pages nor room, and are not reported without them (a padded batch; sequences out of use: length 0, empty masks, no pages).
  *   Q [N, T, Hq, D], K [P, S, Hk, D], V [P, S, Hk, Dv], O [N, T, Hq, Dv]: one type (F32, F16, BF16); Hq a multiple of Hk;
  *   D and Dv up to 256; T up to 128; table [N, M] I32; masks [N, T, ceil(T / 32)] I32.  lengths: DEVICE int32[N]; lse: DEVICE
  *   float[N * T * Hq] or NULL.

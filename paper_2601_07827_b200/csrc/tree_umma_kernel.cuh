@@ -267,8 +267,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             TreeSpan span;
             span.set(p, length);
             mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
-            if (rare(AttentionSpan<true>::bad(p, length)))
-                if (blockIdx.x == 0 && p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+            if (blockIdx.x == 0 && p.flags && rare(AttentionSpan<true>::bad(p, s, length))) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
         int64_t x = mine;
 #pragma unroll
@@ -421,7 +420,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
                 for (int g = 0; g < 4; ++g) {
                     const int t = token0 + 32 * g + lane;
                     if (rare(page[g] >= p.pages || (page[g] < 0 && t >= cur.span.begin && t < cur.span.end))) {
-                        if (p.flags) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
+                        if (p.flags && t < cur.span.cached) atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
                         page[g] = -1;
                     }
                 }
@@ -481,6 +480,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             cur.next(p);
         }
         cp_async_wait_all();
+        if (lw == 2) report_drafts_without_page(p, lane);
     } else {
         // ---- products ----
         const unsigned idesc_s = umma16_instr_desc<T>(kTreeTok, false), idesc_f = umma16_instr_desc<T>(DP, true);

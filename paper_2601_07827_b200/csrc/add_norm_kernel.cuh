@@ -334,7 +334,8 @@ __global__ void __launch_bounds__(WARP ? 32 * kNormWarpRows : 1024) add_norm_bac
         fetch(row + step);
         sum = row_sum<WARP>(sum, room, turn);
         const float inv = rsqrtf(fmaf(sum.x, p.inv_dim, p.eps));
-        const float pull = -(sum.y * inv * p.inv_dim) * inv * inv;        // h pull = -n rms^-1 mean(g n)
+        // rms^-1 (g - n mean(g n)), the difference first: rms^-1 squared may be beyond fp32 where the result is not
+        const float mean = sum.y * inv * p.inv_dim;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             const int q = thread + j * threads;
@@ -343,8 +344,9 @@ __global__ void __launch_bounds__(WARP ? 32 * kNormWarpRows : 1024) add_norm_bac
             rest[j].get(b);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                dw[j][i] = fmaf(g[j][i], h[j][i] * inv, dw[j][i]);
-                o[i] = fmaf(p.w ? g[j][i] * a[i] : g[j][i], inv, h[j][i] * pull);
+                const float n = h[j][i] * inv;
+                dw[j][i] = fmaf(g[j][i], n, dw[j][i]);
+                o[i] = fmaf(n, -mean, p.w ? g[j][i] * a[i] : g[j][i]) * inv;
                 if (p.dh) o[i] += b[i];
             }
             if (q < p.chunks) {

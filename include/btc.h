@@ -497,7 +497,8 @@ btc_error_t btc_pages_copy(btc_pages_t op, void *cuda_stream, const int32_t *pai
  * S [T, G] F32: per group of `group` elements (32, 64 or 128; the last one may be shorter; 0: the row, G = 1) with largest
  * modulus a, S = max(a / 448, 2^-126) and Y the codes nearest to y / S.  A group that holds an infinity or NaN gets S = NaN
  * and codes of zero.  The norm takes the sum as it is before H's rounding; squares are added in fp32 (rows whose
- * sum of squares is beyond its range come out as zeros).  eps: 0 or at least 2^-126, finite in fp32.  D up to 16384.
+ * sum of squares is beyond its range come out as zeros; with eps = 0 rows whose squares vanish there, moduli below 2^-75, give infinities
+ * or NaN, as rows of zeros do).  eps: 0 or at least 2^-126, finite in fp32.  D up to 16384.
  * H may be the same memory as R, and Y as X, with the same strides.
  * btc_add_norm_backward: from the kept H (laid out like H, without R like X), dY (like Y) and dH (like H: what flows back
  * along the residual stream; NULL = zero) the gradients

@@ -33,3 +33,24 @@ def test_gradients_of_small_rows(T, D, dtype):
     assert torch.isfinite(edx.float()).all()
     check(dx, edx, UNIT[dtype] * edx.abs() + GRAD_CHAIN * E32 * size)
     check(dw, edw, norm_grad_chain(T) * E32 * moduli)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_whose_squares_vanish(dtype):
+    """With eps = 0 the reciprocal root is infinite: infinities, NaN for zeros, scales lost; with the smallest eps zeros and values times 2^63."""
+    api = helpers.api()
+    handle = api.Handle()
+    x = torch.full((2, 64), 2.0 ** -80, dtype=dtype, device="cuda")
+    x[1] = 0
+    i = info(api, handle, x)
+    for eps in (0.0, 2.0 ** -126):
+        y = torch.full_like(x, 7.0)
+        api.AddNorm(handle, i, i, eps=eps).execute(now(), at(x), 0, at(y))
+        q, s = torch.ones(2, 64, device="cuda").to(torch.float8_e4m3fn), torch.zeros(2, 2, device="cuda")
+        api.AddNorm(handle, i, info(api, handle, q), S=info(api, handle, s), group=32, eps=eps).execute(now(), at(x), 0, at(q), S=at(s))
+        codes = q.view(torch.uint8)
+        if eps == 0.0:
+            assert (y[0] == math.inf).all() and torch.isnan(y[1]).all() and torch.isnan(s).all() and not codes.any()
+        else:
+            assert (y[0] == 2.0 ** -17).all() and not y[1].any() and not codes[1].any()
+            assert (s[1] == 2.0 ** -126).all() and (q[0].float() == 448).all()

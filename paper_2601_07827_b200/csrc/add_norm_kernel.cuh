@@ -6,8 +6,11 @@
 // Bound by HBM: a row is read once into registers, its sum of squares goes through the warp and shared memory, and
 // everything that depends on it is written from those registers.  A thread holds `C` chunks of `CH` neighbouring
 // elements (16 bytes of x), chunk q = thread + j * threads, so that every access of a warp is contiguous.
-// Measured: 8192 rows of 8192 with the stream in fp32 and an 8-bit result 127 us (740 MB: 5.8 TB/s), 16384 rows of 4096 in bf16 forward
-// and backward 181 us (1074 MB: 5.9 TB/s), 16 rows of 4096 3.8 us.
+// Measured in replayed graphs: 8192 rows of 8192 with the stream in fp32 and an 8-bit result 119 us (740 MB: 6.2 TB/s), 16384 rows of 4096 in
+// bf16 forward and backward 175 us (1074 MB: 6.1 TB/s; floor 164), 8192 rows of 4096 with the stream in fp32 173 us (floor 143), 16 rows of 4096
+// 2.1 us.  A row has at most 1024 threads and so 64 registers in each: the backward pass of rows over 8192 spills 500 to 730 bytes a thread in 16 bits
+// with vectors (2048 rows of 16384 in bf16 with the forward pass 158 us, floor 82) and in fp32 (326 us, floor 164), of long rows of single elements
+// 820 to 1010 bytes, rows with the stream in fp32 90.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -107,7 +110,8 @@ template <int CH> __device__ __forceinline__ void store_e4m3(unsigned char *row,
 }
 
 // The scale of a group whose largest modulus has these bits, and its reciprocal.  The scale is a normal number, so that the
-// reciprocal is finite; a group that holds an infinity or NaN has the scale NaN and codes of zero.
+// reciprocal is finite; a group that holds an infinity or NaN has the scale NaN and codes of zero.  Both are products with rounded
+// reciprocals (1 / 448 and 1 / scale): a unit of fp32 more than divisions would give, 2^-20 of a code's step.
 __device__ __forceinline__ void e4m3_scale(uint32_t top, float &scale, float &inv)
 {
     const bool finite = top < 0x7f800000u;

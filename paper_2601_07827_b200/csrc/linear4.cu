@@ -41,6 +41,12 @@ int32_t stretch_group_log2(const btc_linear4_s &op) { return std::min(log2_of(op
 //   1 token    384 x 16: (4, 1) 7.7 us [7.7], 256 x 56: (4, 2) 13.2 [12.4], 896 x 16: (1, 1) 20.2 [20.2], 1792 x 32: (1, 2) 62 [62], 128 x 8: (8, 1) 3.4 [3.4]
 //   8 tokens   384 x 16: (1, 4) 9.1 [9.1], 256 x 56: (2, 4) 14.5 [14.5], 896 x 16: (1, 1) 22.9 [22.9], 1792 x 32: (1, 2) 71 [71], 128 x 8: (8, 1) 4.5 [4.5]
 //   32 tokens  384 x 16: (1, 4) 19.8 [19.8], 256 x 56: (1, 8) 28.0 [28.0], 896 x 16: (1, 2) 56.7 [52.0], 1792 x 32: (1, 2) 176 [175], 64 x 4: (8, 2) 7.3 [7.2]
+// The same rule for other types of x, over the same row blocks x stretches (384 x 16, 256 x 56, 896 x 16 gated, 1792 x 32 gated, 128 x 8):
+//   e4m3   1 token   7.0 12.7 18.5 67.9 3.7 us [7.2 12.1 18.6 64.4 3.8]    8 tokens  10.2 15.4 22.9 82.2 5.1 [9.1 15.4 22.9 75.8 5.1]
+//          32 tokens 21.0 31.2 61.9 198 10.5 [21.0 31.0 56.0 193 9.7]
+//   fp32   1 token   10.6 17.8 32.8 103 5.1 [10.6 17.7 30.4 103 4.8]       8 tokens  12.3 23.6 38.4 123 5.5 [12.1 20.5 36.0 123 5.5]
+//          32 tokens 32.1 59.8 109 369 9.2 [32.1 53.3 109 369 9.2]
+// (up to 15 % from the best; the choice of all pairs of 1, 2, 4, 8 was timed).
 void plan(btc_linear4_s &op)
 {
     const int64_t tokens = op.x.extent[0], sms = op.handle.sm_count;

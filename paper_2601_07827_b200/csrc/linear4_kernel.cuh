@@ -18,6 +18,10 @@
 // A warp takes 16 rows and copies stretches into a ring of its own with 16-byte cp.async (with loads into registers ahead of their
 // use a thread needs 160 of them, which leaves one CTA to an SM: 20 us instead of 8 for 6144 x 4096); x lies in shared memory in the
 // order in which the lanes take it.
+//
+// Measured (replayed graphs, weights from HBM): one token 6144 x 4096 in f16 6.8 us (13 MB), gated 28672 x 4096 for 8 tokens in bf16 24.9 us (64 MB: 2.6 TB/s),
+// gated 57344 x 8192 for 32 tokens 178 us in bf16 and 198 us in e4m3 (floor 37), for 1024 tokens 4.6 ms (the products alone 0.57 at the matrix rate): the
+// weights are made into numbers again for every 32 tokens.  8 tokens in fp32, gated 28672 x 4096: 39.5 us.
 #pragma once
 
 #include <cooperative_groups.h>

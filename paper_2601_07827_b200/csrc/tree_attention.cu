@@ -50,9 +50,13 @@ bool rows_allow_vectors(const TensorDesc &t, int64_t elements)
 bool umma_fits(const btc_tree_attention_s &op)
 {
     if (op.q.dtype == BTC_F32 || op.dp > 128) return false;
-    // Up to 16 rows to a key head the warp kernels read the cache once and are quicker (tcgen05 in brackets; heads of 128, bf16): 32 requests
-    // of 64 to 8192 tokens, 4 / 8 / 16 / 24 rows: 50 / 51 / 90 / 143 us [97 / 99 / 99 / 98], one of 1500: 13 / 13 / 18 / 20 [21 / 20 / 20 / 21],
-    // 4 x 64 Ki tokens: 167 / 167 / 255 / 480 [235 / 234 / 234 / 237]
+    // Up to 16 rows to a key head the warp kernels read the cache once and are quicker, or nearly (tcgen05 in brackets), 8 / 16 / 24 rows:
+    //   32 requests of 64 to 8192 tokens   heads of 128, bf16 53 / 93 / 146 us [82 / 82 / 82], f16 53 / 93 / 146 [92 / 92 / 92];
+    //                                      heads of 64, bf16 42 / 65 / 100 [68 / 69 / 68], f16 42 / 65 / 99 [74 / 76 / 75]; of 32, bf16 42 / 63 / 97 [67 / 67 / 67]
+    //   one of 1500                        heads of 128 13 / 18 / 20 [21 / 21 / 21]; of 64 12 / 16 / 17 [16 / 16 / 16]
+    //   4 x 64 Ki tokens                   heads of 128, bf16 178 / 264 / 516 [231 / 231 / 228], f16 179 / 271 / 509 [254 / 245 / 244];
+    //                                      heads of 64, bf16 138 / 183 / 351 [197 / 197 / 197]; of 32, f16 127 / 174 / 339 [206 / 207 / 207]
+    // (Heads of 96 take what heads of 128 take.  Between 9 and 16 rows of large heads the sides are 15 % apart, in either direction.)
     if (op.q.extent[1] * (op.q.extent[2] / op.k.extent[2]) <= 16) return false;
     if (float(op.scale * kLog2E) == 0.f) return false;      // -inf for what is not visible would not survive the product
     for (const TensorDesc *t : {&op.k, &op.v}) {

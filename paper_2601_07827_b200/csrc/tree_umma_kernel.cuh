@@ -22,10 +22,12 @@
 // Every wait is bounded.  One that gives up ends the CTA, after its copies and products in flight; the rows of the items it had in hand become NaN, so that
 // nobody takes an incomplete result for a whole one, and BTC_FLAG_TIMEOUT reports it.
 //
-// Measured (replayed graphs, heads of 128): 32 requests of 64 to 8192 tokens, 128 rows: 102 us (240 MB), 256 rows: 194 us; 4 x 64 Ki tokens, 32
-// rows: 241 us (1.07 GB: 4.5 TB/s), 512 rows 1.07 ms (510 TFLOP/s of the two products).  What bounds it is the chain of a step in the softmax
-// warps, about 4000 cycles: tensor memory to registers 600, the exchange of maxima 290, exponentials 1400 (64 a thread, 16 a cycle on an SM), F
-// 700 to 1000.  A 128 x 128 x 16 product takes 67 cycles, 24 of them a step.
+// Measured (replayed graphs, heads of 128): 32 requests of 64 to 8192 tokens, 128 rows: 89 us (240 MB), 256 rows: 183 us; 4 x 64 Ki tokens, 32
+// rows: 228 us in bf16, 243 in f16 (1.07 GB: 4.7 and 4.4 TB/s), 512 rows 1.06 ms (515 TFLOP/s of the two products), which under the power limit of
+// a run of seconds becomes 1.2 ms (455 TFLOP/s).  What bounds it is the chain of a step in the softmax warps, about 4000 cycles (228 us are 111 steps):
+// tensor memory to registers 600, the exchange of maxima 290, exponentials 1400 (64 a thread, 16 a cycle on an SM), F 700 to 1000.  A 128 x 128 x 16
+// product takes 67 cycles, 24 of them a step.  The softmax warps have 216 registers and spill 228 to 248 bytes a thread; a pass executes 0.6 million
+// local accesses of a warp (32 requests), 2 % of what the L1 could.
 #pragma once
 
 #include "paged_attention_kernel.cuh"
@@ -34,7 +36,7 @@
 namespace btc {
 
 constexpr int kTreeTok = 128, kTreeRows = 128;
-// what beginning and ending an item costs, in tiles (1, 3, 5: 118.5, 104.5, 106.9 us for 32 requests of 64 to 8192 tokens)
+// what beginning and ending an item costs, in tiles (1, 3, 5: 118.5, 104.5, 106.9 us for 32 requests of 64 to 8192 tokens, when a pass took 104)
 constexpr int kTreeItemTiles = 3;
 constexpr int kTreeThreads = 384;
 constexpr int kTreeInfos = 8;                // tiles whose visible tokens are kept: more than the ring can be ahead of the softmax

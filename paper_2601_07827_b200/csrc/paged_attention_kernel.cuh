@@ -155,18 +155,6 @@ __device__ __forceinline__ void cp_async_part(unsigned dst, const void *src, int
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// TREE: does any row of a sequence see one of its drafts first .. last - 1?  (Asked only where such a draft has no page or no room:
-// what no row sees needs neither.)
-__device__ __forceinline__ bool draft_seen(const int32_t *masks, int64_t m_t, int64_t m_w, int32_t drafts, int32_t first, int32_t last)
-{
-    bool seen = false;
-#pragma unroll 1
-    for (int32_t i = 0; i < drafts; ++i, masks += m_t)
-#pragma unroll 1
-        for (int32_t d = first; d < last; ++d) seen |= (uint32_t(masks[(d >> 5) * m_w]) >> (d & 31)) & 1u;
-    return seen;
-}
-
 // visible tokens [begin, end) of a sequence, and its tiles, which start at multiples of 16 tokens.  TREE: those that any draft
 // may see; the drafts lie behind the `cached` tokens.
 template <bool TREE> struct AttentionSpan {
@@ -186,20 +174,14 @@ template <bool TREE> struct AttentionSpan {
         first_tile = begin / kAttnTok;
         tiles = end / kAttnTok + (end % kAttnTok != 0) - first_tile;
     }
-    __device__ __forceinline__ static bool bad(const AttentionParams &p, int32_t seq, int32_t length)
-    {
-        if (length < 0 || length > p.room) return true;
-        if constexpr (TREE)
-            if (rare(length > p.room - p.drafts)) return draft_seen(p.masks + seq * p.m_n, p.m_t, p.m_w, p.drafts, p.room - length, p.drafts);
-        return false;
-    }
-    // Is it an error by itself that token t has no page?  (Drafts: see report_drafts_without_page.)
+    __device__ __forceinline__ static bool bad(const AttentionParams &p, int32_t length) { return length < 0 || length > p.room; }
+    // Is it an error by itself that token t has no page?  (Drafts: see report_drafts.)
     __device__ __forceinline__ bool needs_page(int32_t t) const { return !TREE || t < cached; }
 };
 
-// TREE: a warp reports missing pages of drafts, of every gridDim.x-th sequence.  Apart from the loops that look pages up, which have no
-// registers to spare for the masks.
-__device__ __forceinline__ void report_drafts_without_page(const AttentionParams &p, int lane)
+// TREE: a warp reports drafts without a page or without room, of every gridDim.x-th sequence, where a row sees them: what no row sees
+// needs neither.  Apart from the loops that look pages up, which have no registers to spare for the masks, and at their end.
+__device__ __forceinline__ void report_drafts(const AttentionParams &p, int lane)
 {
     if (!p.flags) return;
 #pragma unroll 1
@@ -207,10 +189,16 @@ __device__ __forceinline__ void report_drafts_without_page(const AttentionParams
         AttentionSpan<true> span;
         span.set(p, p.lengths[s]);
 #pragma unroll 1
-        for (int t = span.cached + lane; t < span.end; t += 32) {
-            const int32_t page = p.table[s * p.table_n + int64_t(p.page.div(uint32_t(t))) * p.table_j], d = t - span.cached;
-            if (rare(page < 0 || page >= p.pages) && draft_seen(p.masks + s * p.m_n, p.m_t, p.m_w, p.drafts, d, d + 1))
-                atomicOr(p.flags, int(BTC_FLAG_BAD_PAGE));
+        for (int d = lane; d < p.drafts; d += 32) {
+            const int32_t t = span.cached + d;
+            int32_t page = -1;
+            if (t < span.end) page = p.table[s * p.table_n + int64_t(p.page.div(uint32_t(t))) * p.table_j];
+            if (page >= 0 && page < p.pages) continue;
+            uint32_t seen = 0;
+            const int32_t *mask = p.masks + s * p.m_n + (d >> 5) * p.m_w;
+#pragma unroll 4
+            for (int i = 0; i < p.drafts; ++i, mask += p.m_t) seen |= uint32_t(*mask);
+            if ((seen >> (d & 31)) & 1u) atomicOr(p.flags, int(t < span.end ? BTC_FLAG_BAD_PAGE : BTC_FLAG_BAD_LENGTH));
         }
     }
 }
@@ -849,7 +837,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
             AttentionSpan<TREE> span;
             span.set(p, length);
             mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
-            if (blockIdx.x == 0 && p.flags && rare(AttentionSpan<TREE>::bad(p, s, length))) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+            if (blockIdx.x == 0 && p.flags && rare(AttentionSpan<TREE>::bad(p, length))) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
         int64_t x = mine;
 #pragma unroll
@@ -1052,7 +1040,7 @@ paged_attention_kernel(const __grid_constant__ AttentionParams p)
         }
     }
     if constexpr (TREE)
-        if (warp == 0) report_drafts_without_page(p, lane);
+        if (warp == 0) report_drafts(p, lane);
     // sequences with nothing to see
     for (int s = blockIdx.x; s < p.sequences; s += gridDim.x) {
         AttentionSpan<TREE> span;

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             TreeSpan span;
             span.set(p, length);
             mine += (int64_t(span.tiles) << 24) + (span.tiles > 0 ? 1 : 0);
-            if (blockIdx.x == 0 && p.flags && rare(AttentionSpan<true>::bad(p, s, length))) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
+            if (blockIdx.x == 0 && p.flags && rare(AttentionSpan<true>::bad(p, length))) atomicOr(p.flags, int(BTC_FLAG_BAD_LENGTH));
         }
         int64_t x = mine;
 #pragma unroll
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_umma_kernel(const __grid
             cur.next(p);
         }
         cp_async_wait_all();
-        if (lw == 2) report_drafts_without_page(p, lane);
+        if (lw == 2) report_drafts(p, lane);
     } else {
         // ---- products ----
         const unsigned idesc_s = umma16_instr_desc<T>(kTreeTok, false), idesc_f = umma16_instr_desc<T>(DP, true);

@@ -26,7 +26,7 @@
 // rows: 228 us in bf16, 243 in f16 (1.07 GB: 4.7 and 4.4 TB/s), 512 rows 1.06 ms (515 TFLOP/s of the two products), which under the power limit of
 // a run of seconds becomes 1.2 ms (455 TFLOP/s).  What bounds it is the chain of a step in the softmax warps, about 4000 cycles (228 us are 111 steps):
 // tensor memory to registers 600, the exchange of maxima 290, exponentials 1400 (64 a thread, 16 a cycle on an SM), F 700 to 1000.  A 128 x 128 x 16
-// product takes 67 cycles, 24 of them a step.  The softmax warps have 216 registers and spill 228 to 248 bytes a thread; a pass executes 0.6 million
+// product takes 67 cycles, 24 of them a step.  The softmax warps have 216 registers and spill 224 to 248 bytes a thread; a pass executes 0.6 million
 // local accesses of a warp (32 requests), 2 % of what the L1 could.
 #pragma once
 
